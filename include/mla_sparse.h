@@ -61,8 +61,17 @@ typedef enum {
   MLA_DTYPE_BF16 = 1,
   MLA_DTYPE_FP8_E4M3FN = 2, /* OCP E4M3FN: bias 7, max 448, no infinities */
   MLA_DTYPE_FP32 = 3,
-  MLA_DTYPE_INT32 = 4
+  MLA_DTYPE_INT32 = 4,
+  MLA_DTYPE_MXFP4 = 5 /* a latent pool in 4 bits: rows of MLA_MX4_ROW bytes, see below */
 } mla_dtype_t;
+
+/* A 4-bit latent row (OCP MX with E2M1 elements): the 512 codes of a token, two
+ * to a byte, the even column in the low half, then 16 exponent bytes, one for
+ * each 32 columns: value = E2M1 code * 2^(byte - 127); byte 255 is NaN.  The last
+ * dim of a descriptor of this type counts bytes.  Values of less than 2^-126
+ * (bytes 0 and 1) may read as 0.  The RoPE pool beside it holds bf16: 400 bytes
+ * a token. */
+#define MLA_MX4_ROW 272
 
 /* A strided view of device memory.  shape/stride beyond ndim are ignored;
  * strides are in elements and the innermost stride must be 1. */
@@ -311,6 +320,8 @@ int32_t mla_version(void);
  * contiguous payload (FETCH's residual work under sparse selection).
  *   chunk_block_table [NB] int32    logical block of the chunk -> pool block
  *   sel_token_ids     [K]  int32    logical tokens (block * 64 + t); -1 = empty
+ *                                   (ckv_pool may be [L, P, 64, 272] MXFP4: the
+ *                                   payload then holds its values, exactly)
  *   out_ckv [L, K, 512], out_kpe [L, K, 64] bf16, written: entry j is pool
  *                                   token table[s / 64] * 64 + s % 64 of slot
  *                                   j's id s, copied bit for bit; an empty
@@ -345,6 +356,99 @@ mla_status_t mla_fetch_splice(const mla_tensor_t* chunk_ckv, const mla_tensor_t*
                               const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
                               const mla_tensor_t* block_table, int64_t dst_start, int64_t delta,
                               float rope_base, int32_t pairing, void* stream);
+
+/*
+ * ---- A serving step's way into the paged cache: the tables and slots of a
+ * batch, rotary positions, the write of its new tokens.
+ *
+ * mla_batch_slots: block tables and slot maps from request lengths, on the GPU.
+ *   cached_lens [B], new_lens [B] int32   tokens of request b in the cache, and
+ *                                     to be added now (negative counts as 0)
+ *   free_blocks [F] int32             pool blocks that no request holds
+ *   block_table [B, NB] int32         in and out (rows may be strided): the first
+ *                                     ceil(cached / 64) entries of a row are the
+ *                                     request's blocks; the entries on from there
+ *                                     to ceil((cached + new) / 64) are written,
+ *                                     with free blocks in the order of the
+ *                                     requests (-1 where the list has run out);
+ *                                     no other entry is
+ *   slots, positions [T] int32        written: of the new tokens packed request
+ *                                     after request, the pool token (block * 64 +
+ *                                     row) and the position in its sequence.  -1
+ *                                     in slots for a token without a place (past
+ *                                     the table, no free block, a table entry
+ *                                     outside [0, 2^25)) and, in both, past the
+ *                                     last token
+ *   seq_lens [B] int32                written: cached + new
+ *   starts [B + 1] int32              written: each request's first packed token,
+ *                                     then their number
+ *   info [4] int32                    written: new tokens; blocks taken off the
+ *                                     list (its first entries); blocks missing;
+ *                                     tokens past T
+ * B at most 8192 (MLA_ERR_UNSUPPORTED).  A pure function of its inputs: calling
+ * it again, or replaying a graph that holds it, writes the same. */
+mla_status_t mla_batch_slots(const mla_tensor_t* cached_lens, const mla_tensor_t* new_lens,
+                             const mla_tensor_t* free_blocks, const mla_tensor_t* block_table,
+                             const mla_tensor_t* slots, const mla_tensor_t* positions,
+                             const mla_tensor_t* seq_lens, const mla_tensor_t* starts,
+                             const mla_tensor_t* info, void* stream);
+
+/* Rotary positions.  All fields count; mla_rope refuses a NULL opts. */
+typedef struct {
+  int32_t rot_offset; /* first rotated dim of a head                              */
+  int32_t rot_dim;    /* rotated dims d: even, 2 .. 256                            */
+  int32_t pairing;    /* 0: dims (2i, 2i+1) of the part, 1: (i, i + d/2)           */
+  int32_t scaling;    /* MLA_ROPE_*: how angles grow with the position             */
+  int32_t inverse;    /* 1: turn back, which is also the gradient's way: the
+                         transpose of the map, mscale included                     */
+  int32_t reserved;   /* must be zero                                              */
+  double base;        /* > 0 (YARN: > 1)                                           */
+  double factor;      /* LINEAR, YARN: s > 0                                       */
+  double beta_fast;   /* YARN: turns in orig_len from which a pair keeps its angle */
+  double beta_slow;   /* YARN: turns up to which a pair is slowed s times, > 0     */
+  double mscale;      /* multiplies the rotated part (1: none)                     */
+  int64_t orig_len;   /* YARN: the context the model was trained on, > 0           */
+} mla_rope_opts_t;
+
+enum { MLA_ROPE_PLAIN = 0, MLA_ROPE_LINEAR = 1, MLA_ROPE_YARN = 2 };
+
+/* mla_rope: pair i of every head of row t turns by positions[t] * w_i,
+ *   (x, y) -> mscale (x cos a - y sin a, x sin a + y cos a),
+ * the other dims are copied.
+ *   PLAIN   w_i = base^(-2i/d)
+ *   LINEAR  w_i = base^(-2i/d) / factor
+ *   YARN    w_i = base^(-2i/d) ((1 - r_i) + r_i / factor), r_i rising from 0 at
+ *           floor(i(beta_fast)) to 1 at ceil(i(beta_slow)), both kept within
+ *           0 .. d - 1, where i(b) = d/2 ln(orig_len / (2 pi b)) / ln(base) is
+ *           the pair that makes b turns in orig_len
+ *   x         [T, H, D] bf16 or fp32, rows may be strided
+ *   positions [T] int32, any value
+ *   out       [T, H, D] of x's type, written; may be x itself (same data and
+ *             strides), must not overlap it otherwise
+ * Angles are reduced in fp64, products are formed in fp32, each value is rounded
+ * once.  Rows need no alignment; 16-byte aligned ones with D, the offset and
+ * (half) the rotated part multiples of 16 bytes go in 16-byte accesses. */
+mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, const mla_tensor_t* out,
+                      const mla_rope_opts_t* opts, void* stream);
+
+/* mla_cache_append: new tokens into the paged cache.
+ *   ckv [T, 512], kpe [T, 64] bf16    rows may be strided (16-byte aligned)
+ *   slots [T] int32                   pool token of each (block * 64 + row), as
+ *                                     mla_batch_slots writes them; one outside
+ *                                     [0, 64 P) is skipped.  Slots must differ:
+ *                                     a slot given twice ends up with parts of
+ *                                     either token
+ *   ckv_pool [P, 64, 512] bf16 or [P, 64, 272] MXFP4, kpe_pool [P, 64, 64] bf16
+ *                                     contiguous, 16-byte aligned; the slots'
+ *                                     rows are written, no others
+ * bf16 rows are copied bit for bit.  MXFP4: with a the largest magnitude of 32
+ * columns, their exponent is floor(log2 a) - 2 within -125 .. 125, each code the
+ * nearest E2M1 value (halfway to the even code, at most 6), signs kept; columns
+ * among which one is infinite or NaN read back as NaN.  An fp8 pool, whose scale
+ * belongs to a whole block, is MLA_ERR_UNSUPPORTED. */
+mla_status_t mla_cache_append(const mla_tensor_t* ckv, const mla_tensor_t* kpe,
+                              const mla_tensor_t* slots, const mla_tensor_t* ckv_pool,
+                              const mla_tensor_t* kpe_pool, void* stream);
 
 /*
  * The closed-form cost model of the three redistribution primitives and the

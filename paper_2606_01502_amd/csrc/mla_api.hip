@@ -14,97 +14,14 @@
 #include <vector>
 
 #include "../../include/mla_sparse.h"
+#include "mla_host.h"
 #include "mla_plan.h"
 
 static_assert(mla::kPlanScratch == MLA_NOALLOC_SCRATCH_BYTES, "plans fit the allocation-free entry");
 
+using namespace mla::host;
+
 namespace {
-
-thread_local std::string g_last_error;
-
-mla_status_t fail(mla_status_t st, const std::string& msg) {
-  g_last_error = msg;
-  return st;
-}
-
-struct Extent {
-  uintptr_t lo, hi;  // [lo, hi) bytes touched
-};
-
-int dtype_size(int32_t dt) {
-  switch (dt) {
-    case MLA_DTYPE_BF16: return 2;
-    case MLA_DTYPE_FP8_E4M3FN: return 1;
-    case MLA_DTYPE_FP32: return 4;
-    case MLA_DTYPE_INT32: return 4;
-    default: return 0;
-  }
-}
-
-int64_t numel(const mla_tensor_t& t) {
-  int64_t n = 1;
-  for (int d = 0; d < t.ndim; ++d) n *= t.shape[d];
-  return n;
-}
-
-Extent extent(const mla_tensor_t& t) {
-  const int es = dtype_size(t.dtype);
-  if (numel(t) == 0) return {0, 0};
-  int64_t hi = 0;
-  for (int d = 0; d < t.ndim; ++d) hi += (t.shape[d] - 1) * t.stride[d];
-  const uintptr_t base = reinterpret_cast<uintptr_t>(t.data);
-  return {base, base + (uintptr_t)((hi + 1) * es)};
-}
-
-bool overlaps(const Extent& a, const Extent& b) {
-  if (a.lo == a.hi || b.lo == b.hi) return false;
-  return a.lo < b.hi && b.lo < a.hi;
-}
-
-// Common checks of one descriptor.  `name` is used in messages.
-mla_status_t check_tensor(const mla_tensor_t* t, const char* name, int32_t dtype, int ndim,
-                          bool allow_scale = false) {
-  if (!t) return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": null descriptor");
-  if (t->dtype != dtype)
-    return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": wrong dtype " + std::to_string(t->dtype));
-  if (t->ndim != ndim)
-    return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": expected " + std::to_string(ndim) +
-                                              " dims, got " + std::to_string(t->ndim));
-  for (int d = 0; d < ndim; ++d)
-    if (t->shape[d] < 0 || t->stride[d] < 0)
-      return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": negative shape or stride");
-  if (ndim > 0 && t->shape[ndim - 1] > 1 && t->stride[ndim - 1] != 1)
-    return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": innermost stride must be 1");
-  if (numel(*t) > 0 && !t->data)
-    return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": null data pointer");
-  if (!allow_scale && t->block_scale)
-    return fail(MLA_ERR_INVALID_ARGUMENT, std::string(name) + ": block_scale must be NULL");
-  return MLA_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Row-major contiguous with the given shape.
-bool contiguous(const mla_tensor_t& t, std::initializer_list<int64_t> shape) {
-  if (t.ndim != (int)shape.size()) return false;
-  int d = 0;
-  for (int64_t v : shape)
-    if (t.shape[d++] != v) return false;
-  int64_t st = 1;
-  for (int k = t.ndim - 1; k >= 0; --k) {
-    if (t.shape[k] > 1 && t.stride[k] != st) return false;
-    st *= t.shape[k];
-  }
-  return true;
-}
-
-// Rows of a [.., .., .., D] tensor are 16-byte aligned: base and every outer stride.
-bool rows_aligned(const mla_tensor_t& t, int es) {
-  if (!aligned16(t.data)) return false;
-  for (int d = 0; d + 1 < t.ndim; ++d)
-    if ((t.stride[d] * es) % 16 != 0) return false;
-  return true;
-}
 
 // Split-K workspace: one grow-only buffer per (device, stream).  The caller
 // keeps `lock` (which holds g_ws_mutex) until both kernels that use the
@@ -509,7 +426,8 @@ mla_status_t mla_fetch_gather(const mla_tensor_t* ckv_pool, const mla_tensor_t* 
   try {
     g_last_error.clear();
     mla_status_t st;
-    if ((st = check_tensor(ckv_pool, "ckv_pool", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
+    const bool mx4 = ckv_pool && ckv_pool->dtype == MLA_DTYPE_MXFP4;
+    if ((st = check_tensor(ckv_pool, "ckv_pool", mx4 ? MLA_DTYPE_MXFP4 : MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
     if ((st = check_tensor(kpe_pool, "kpe_pool", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
     if ((st = check_tensor(chunk_block_table, "chunk_block_table", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
     if ((st = check_tensor(sel_token_ids, "sel_token_ids", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
@@ -517,8 +435,10 @@ mla_status_t mla_fetch_gather(const mla_tensor_t* ckv_pool, const mla_tensor_t* 
     if ((st = check_tensor(out_kpe, "out_kpe", MLA_DTYPE_BF16, 3)) != MLA_OK) return st;
     const int64_t L = ckv_pool->shape[0], P = ckv_pool->shape[1];
     const int64_t NB = chunk_block_table->shape[0], K = sel_token_ids->shape[0];
-    if (!contiguous(*ckv_pool, {L, P, MLA_BLOCK, MLA_DLAT}) || !contiguous(*kpe_pool, {L, P, MLA_BLOCK, MLA_DPE}))
-      return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be contiguous [L, P, 64, 512] and [L, P, 64, 64]");
+    if (!contiguous(*ckv_pool, {L, P, MLA_BLOCK, mx4 ? MLA_MX4_ROW : MLA_DLAT}) ||
+        !contiguous(*kpe_pool, {L, P, MLA_BLOCK, MLA_DPE}))
+      return fail(MLA_ERR_INVALID_ARGUMENT,
+                  "pools must be contiguous [L, P, 64, 512] (MXFP4: [L, P, 64, 272]) and [L, P, 64, 64]");
     if (!contiguous(*chunk_block_table, {NB}) || !contiguous(*sel_token_ids, {K}))
       return fail(MLA_ERR_INVALID_ARGUMENT, "chunk_block_table and sel_token_ids must be contiguous");
     if (!contiguous(*out_ckv, {L, K, MLA_DLAT}) || !contiguous(*out_kpe, {L, K, MLA_DPE}))
@@ -546,7 +466,8 @@ mla_status_t mla_fetch_gather(const mla_tensor_t* ckv_pool, const mla_tensor_t* 
     p.n = K;
     p.n_ids = NB * MLA_BLOCK;
     p.L = (int32_t)L;
-    hipError_t e = mla::launch_fetch_gather(p, reinterpret_cast<hipStream_t>(stream));
+    const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+    hipError_t e = mx4 ? mla::launch_fetch_gather_mx4(p, hs) : mla::launch_fetch_gather(p, hs);
     if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("gather kernel launch: ") + hipGetErrorString(e));
     return MLA_OK;
   } catch (...) {

@@ -13,6 +13,7 @@ constexpr int kBlock = 64;   // tokens per cache block
 constexpr int kThreads = 256;             // merge / combine workgroup size
 constexpr int kMaxSlotsPerSplit = 1024;   // selected-slot range one workgroup handles
 constexpr int kMaxParts = 64;
+constexpr int kMx4Row = kDLat / 2 + kDLat / 32;  // a 4-bit latent row: codes, then scale bytes
 // split-K workspaces of at least this many fp32 row bytes store scaled fp16
 // rows (below it, as for a handful of rows, the shorter fp32 epilogue pays)
 constexpr uint64_t kWsHalfMinBytes = 1ull << 20;
@@ -152,6 +153,57 @@ struct FetchParams {
 
 hipError_t launch_fetch_gather(const FetchParams& p, hipStream_t s);
 hipError_t launch_fetch_splice(const FetchParams& p, hipStream_t s);
+
+hipError_t launch_fetch_gather_mx4(const FetchParams& p, hipStream_t s);  // 4-bit latent pools
+
+// Rotary positions of [T, H, D] rows: one workgroup takes wg_rows of the T * H
+// rows (on at most wg_toks tokens).
+constexpr int kRopeMaxPairs = 128;
+struct RopeParams {
+  const void* x;
+  void* out;
+  const int32_t* pos;             // [T]
+  int64_t x_s0, x_s1, out_s0, out_s1;  // element strides over (token, head)
+  int64_t rows;                   // T * H
+  int32_t H, at, rot, pairing;    // rotated dims at .. at + rot - 1
+  int32_t wg_rows, wg_toks;
+  int32_t row_units;              // units of a row (see the kernel)
+  int32_t fp32, vec;
+  Div by_H, by_units;
+  float mscale, sin_scale;        // factors of the cosine and the sine
+  double turns[kRopeMaxPairs];    // turns a position
+};
+hipError_t launch_rope(const RopeParams& p, hipStream_t s);
+
+// Block tables and slot maps of a batch.
+constexpr int kMaxSlotRequests = 8192;
+struct SlotsParams {
+  const int32_t* cached;       // [B]
+  const int32_t* fresh;        // [B] new tokens
+  const int32_t* free_blocks;  // [F]
+  int32_t* table;              // [B][NB], rows table_s0 apart
+  int32_t* slots;              // [T]
+  int32_t* positions;          // [T]
+  int32_t* seq_lens;           // [B]
+  int32_t* starts;             // [B + 1]
+  int32_t* info;               // [4]
+  int64_t table_s0, F, T;
+  int32_t B, NB;
+};
+hipError_t launch_slots(const SlotsParams& p, hipStream_t s);
+
+// New tokens into the paged cache: wave w takes tokens w * wave_toks and on.
+struct AppendParams {
+  const uint16_t* src_ckv;  // [T][512] bf16, rows ckv_s0 apart
+  const uint16_t* src_kpe;  // [T][64]
+  int64_t ckv_s0, kpe_s0;
+  const int32_t* slots;     // [T] pool tokens, others than 0 .. n_slots - 1 are skipped
+  uint8_t* ckv;             // pool rows of 1 KiB (bf16) or kMx4Row bytes
+  uint8_t* kpe;             // pool rows of 128 bytes
+  int64_t T, n_slots;
+  int32_t wave_toks, mx4;
+};
+hipError_t launch_append(const AppendParams& p, hipStream_t s);
 
 // Cache kinds of the partial kernel.
 constexpr int kKvBf16 = 0;

@@ -1,0 +1,162 @@
+// The latent cache in 4 bits, written and read back, and the write of new tokens
+// into a bf16 cache.
+//
+// A cached token's 512 latent values are 16 groups of 32 neighbours (OCP MX: E2M1
+// codes under a shared power of two).  With a the group's largest magnitude, its
+// scale is 2^(floor(log2 a) - 2), which puts a between 4 and 8 units (E2M1's
+// largest power of two is 4); each code is the nearest E2M1 value, halfway to the
+// even code, 6 where a value lies past 6 units.  A row is 272 bytes: 256 of codes,
+// the even column in the low half of a byte, then 16 scale exponents plus 127.
+// Exponents stay within -125 .. 125, so that every cached value is a normal bf16
+// number or 0; a group that holds an infinity or a NaN gets exponent byte 255 and
+// reads back as NaN.  The RoPE part stays in bf16: 400 bytes a token for 1152.
+//
+// Streams through HBM: a wave takes one token, 8 columns a lane (16 bytes read,
+// 4 written), so that a group is four lanes.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mla_kernels.h"
+#include "mla_mx4.h"
+
+namespace mla {
+namespace {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kRowWords = kMx4Row / 4;
+
+__device__ __forceinline__ int quad_max(int v) {
+  v = max(v, __shfl_xor(v, 1));
+  return max(v, __shfl_xor(v, 2));
+}
+
+// Eight bf16 values (two to a word) -> eight E2M1 codes of v / 2^(byte - 127).
+__device__ __forceinline__ uint32_t to_codes(u32x4_t v, int byte) {
+  // v / 2^e as fp32, exact: e is within -125 .. 125, and what underflows rounds to 0 either way
+  const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = (i & 1) ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16;
+    const float a = fabsf(__uint_as_float(w)) * inv;
+    const uint32_t q = (uint32_t)(a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) +
+                       (a >= 3.5f) + (a > 5.0f);
+    codes |= (q | (w >> 28 & 8u)) << (4 * i);
+  }
+  return codes;
+}
+
+template <bool MX4>
+__global__ __launch_bounds__(kThreads) void append_kernel(const AppendParams p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 6;
+  const int64_t t0 = wave * p.wave_toks;
+  const int n = (int)min((int64_t)p.wave_toks, p.T - t0);
+  constexpr int kAhead = 4;
+  for (int k0 = 0; k0 < n; k0 += kAhead) {
+    u32x4_t v[kAhead], w[kAhead];
+    int64_t row[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int64_t t = t0 + min(k0 + j, n - 1);  // past the end: loaded, not stored
+      const int32_t s = p.slots[t];
+      row[j] = k0 + j < n && s >= 0 && s < p.n_slots ? s : -1;
+      v[j] = *(const u32x4_t*)(p.src_ckv + t * p.ckv_s0 + 8 * lane);
+      if (lane < 8) w[j] = *(const u32x4_t*)(p.src_kpe + t * p.kpe_s0 + 8 * lane);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (row[j] < 0) continue;
+      if (lane < 8) *(u32x4_t*)(p.kpe + row[j] * (2 * kDPe) + 16 * lane) = w[j];
+      if constexpr (!MX4) {
+        *(u32x4_t*)(p.ckv + row[j] * (2 * kDLat) + 16 * lane) = v[j];
+      } else {
+        // magnitudes of bf16 numbers are ordered as their bits
+        int mag = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          mag = max(mag, max((int)(v[j][i] & 0x7FFFu), (int)(v[j][i] >> 16 & 0x7FFFu)));
+        mag = quad_max(mag);
+        // floor(log2 a) + 127 is the exponent field (0 for subnormal numbers, which
+        // the lower limit covers)
+        const bool bad = mag >= 0x7F80;
+        const int byte = min(max((mag >> 7) - 2, 2), 252);
+        uint32_t* const dst = (uint32_t*)(p.ckv + row[j] * kMx4Row);
+        dst[lane] = to_codes(v[j], byte);
+        // four groups' bytes to a word: lanes 0, 16, 32, 48 store them
+        uint32_t b = (uint32_t)(bad ? 255 : byte) << (lane >> 2 & 3) * 8;
+        b |= __shfl_xor(b, 4);
+        b |= __shfl_xor(b, 8);
+        if ((lane & 15) == 0) dst[kDLat / 8 + (lane >> 4)] = b;
+      }
+    }
+  }
+}
+
+// Gather of a selected token set out of a 4-bit pool: out row j of layer l = the
+// values of pool token sel[j] in bf16 (exact), a zero row for an empty slot.
+__global__ __launch_bounds__(kThreads) void gather_mx4_kernel(const FetchParams p) {
+  constexpr int kTok = 32;
+  const int64_t groups = (p.n + kTok - 1) / kTok;
+  const int64_t l = blockIdx.x / groups;
+  const int64_t j0 = (blockIdx.x - l * groups) * kTok;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int64_t src_row[kTok];
+  if (tid < kTok) {
+    int64_t row = -1;
+    const int64_t j = j0 + tid;
+    if (j < p.n) {
+      const int32_t s = p.sel[j];
+      if (s >= 0 && s < p.n_ids) {
+        const int32_t b = p.table[s / kBlock];
+        if (b >= 0 && b < p.P) row = (l * p.P + b) * kBlock + (s % kBlock);
+      }
+    }
+    src_row[tid] = row;
+  }
+  __syncthreads();
+  const uint32_t* const sc = (const uint32_t*)p.src_ckv;
+  const u32x4_t* const sk = (const u32x4_t*)p.src_kpe;
+  constexpr int kPass = kTok / 4;
+  uint32_t c[kPass], e[kPass];
+  u32x4_t w{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int it = 0; it < kPass; ++it) {
+    const int64_t r = src_row[4 * it + wave];
+    c[it] = r >= 0 ? __builtin_nontemporal_load(&sc[r * kRowWords + lane]) : 0u;
+    e[it] = r >= 0 ? __builtin_nontemporal_load(&sc[r * kRowWords + kDLat / 8 + (lane >> 4)]) : 0u;
+  }
+  const int64_t row = src_row[tid >> 3];
+  if (row >= 0) w = __builtin_nontemporal_load(&sk[row * 8 + (tid & 7)]);
+#pragma unroll
+  for (int it = 0; it < kPass; ++it) {
+    const int64_t i = j0 + 4 * it + wave;
+    if (i >= p.n) continue;
+    const float s = mx4_scale(e[it] >> ((lane >> 2 & 3) * 8) & 255u);
+    ((u32x4_t*)p.dst_ckv)[(l * p.n + i) * 64 + lane] = mx4x8_bf16(c[it], s);
+  }
+  const int64_t j = j0 + (tid >> 3);
+  if (j < p.n) ((u32x4_t*)p.dst_kpe)[(l * p.n + j) * 8 + (tid & 7)] = w;
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendParams& p, hipStream_t s) {
+  const int64_t waves = (p.T + p.wave_toks - 1) / p.wave_toks;
+  const int64_t grid = (waves + 3) / 4;
+  if (grid <= 0) return hipSuccess;
+  if (p.mx4) hipLaunchKernelGGL(append_kernel<true>, dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL(append_kernel<false>, dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_fetch_gather_mx4(const FetchParams& p, hipStream_t s) {
+  const int64_t grid = (int64_t)p.L * ((p.n + 31) / 32);
+  if (grid <= 0) return hipSuccess;
+  hipLaunchKernelGGL(gather_mx4_kernel, dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace mla

@@ -7,6 +7,7 @@ there is no fallback, and a missing library raises.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 import struct
@@ -23,12 +24,14 @@ MLA_ERR_UNSUPPORTED = -2
 MLA_ERR_HIP = -3
 MLA_ERR_OUT_OF_MEMORY = -4
 
-DTYPE_BF16, DTYPE_FP8_E4M3FN, DTYPE_FP32, DTYPE_INT32 = 1, 2, 3, 4
+DTYPE_BF16, DTYPE_FP8_E4M3FN, DTYPE_FP32, DTYPE_INT32, DTYPE_MXFP4 = 1, 2, 3, 4, 5
+MX4_ROW = 272  # bytes of a 4-bit latent row: 256 of codes, 16 scale exponents
 
 EXPORTS = ("mla_sparse_partial_attn", "mla_sparse_partial_attn_ex",
            "mla_sparse_partial_attn_tokens", "mla_merge_partials", "mla_merge_partials_ex",
            "mla_last_error", "mla_version", "mla_primitive_costs", "mla_fetch_gather",
-           "mla_fetch_splice", "mla_sparse_partial_attn_noalloc")
+           "mla_fetch_splice", "mla_sparse_partial_attn_noalloc", "mla_batch_slots", "mla_rope",
+           "mla_cache_append")
 
 
 class MlaError(RuntimeError):
@@ -79,6 +82,18 @@ class PartialOpts(ctypes.Structure):
 OUT_FP32, OUT_BF16_WIRE = 0, 1
 
 
+class RopeOpts(ctypes.Structure):
+    _fields_ = [("rot_offset", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("inverse", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("mscale", ctypes.c_double), ("orig_len", ctypes.c_int64)]
+
+
+ROPE_SCALINGS = ("none", "linear", "yarn")
+
+
 _lib = None
 
 
@@ -111,6 +126,12 @@ def load(path: str = LIB_PATH):
     lib.mla_fetch_splice.restype = ctypes.c_int
     lib.mla_fetch_splice.argtypes = [P, P, P, P, P, ctypes.c_int64, ctypes.c_int64,
                                      ctypes.c_float, ctypes.c_int32, vp]
+    lib.mla_batch_slots.restype = ctypes.c_int
+    lib.mla_batch_slots.argtypes = [P] * 9 + [vp]
+    lib.mla_rope.restype = ctypes.c_int
+    lib.mla_rope.argtypes = [P, P, P, ctypes.POINTER(RopeOpts), vp]
+    lib.mla_cache_append.restype = ctypes.c_int
+    lib.mla_cache_append.argtypes = [P] * 5 + [vp]
     lib.mla_primitive_costs.restype = ctypes.c_int
     lib.mla_primitive_costs.argtypes = [ctypes.POINTER(CostModel), ctypes.POINTER(CostCase),
                                         ctypes.POINTER(Cost)]
@@ -158,6 +179,15 @@ def describe(t: torch.Tensor | None, block_scale: torch.Tensor | None = None) ->
                                               *stride, *pad, bs))
 
 
+def _describe_latent(t, block_scale=None):
+    """describe() of a latent pool: a uint8 pool with rows of MX4_ROW bytes is
+    a 4-bit one (MXFP4), with rows of 512 an fp8 one."""
+    d = describe(t, block_scale)
+    if t.dtype == torch.uint8 and t.dim() and t.shape[-1] == MX4_ROW:
+        d.dtype = DTYPE_MXFP4
+    return d
+
+
 def _on_one_gpu(*tensors):
     """Raise ValueError unless every given tensor lives on one CUDA (HIP)
     device: the library reads and writes device memory only, and a host
@@ -168,6 +198,15 @@ def _on_one_gpu(*tensors):
         raise ValueError(f"tensors must be on the GPU, got {bad[0]}")
     if len(devs) > 1:
         raise ValueError(f"tensors must be on one device, got {sorted(map(str, devs))}")
+
+
+def _on_current_gpu(*tensors):
+    """_on_one_gpu, and that device is the current one, whose stream the call
+    goes to."""
+    _on_one_gpu(*tensors)
+    dev = next(t.device for t in tensors if t is not None)
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, which is not the current device")
 
 
 def _stream(stream):
@@ -273,7 +312,8 @@ def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=N
                  out_kpe=None, stream=None):
     """FETCH's scattered gather: the selected tokens of every layer, in slot
     order, as contiguous bf16 [L, K, 512] / [L, K, 64] (zero rows for empty
-    slots).  Pools are [L, P, 64, 512] / [L, P, 64, 64] bf16."""
+    slots).  Pools are [L, P, 64, 512] / [L, P, 64, 64] bf16, or the latent one
+    [L, P, 64, 272] in 4 bits (uint8), whose values are exact in bf16."""
     L = ckv_pool.shape[0]
     K = sel_token_ids.shape[0]
     if out_ckv is None:
@@ -282,8 +322,8 @@ def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=N
         out_kpe = torch.empty((L, K, DPE), dtype=torch.bfloat16, device=ckv_pool.device)
     _on_one_gpu(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv, out_kpe)
     lib = load()
-    d = [describe(t) for t in (ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv,
-                               out_kpe)]
+    d = [_describe_latent(ckv_pool)]
+    d += [describe(t) for t in (kpe_pool, chunk_block_table, sel_token_ids, out_ckv, out_kpe)]
     _check(lib, lib.mla_fetch_gather(*[_ref(x) for x in d], _stream(stream)))
     return out_ckv, out_kpe
 
@@ -299,6 +339,84 @@ def fetch_splice(chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table, dst_star
     d = [describe(t) for t in (chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table)]
     _check(lib, lib.mla_fetch_splice(*[_ref(x) for x in d], int(dst_start), int(delta),
                                      float(rope_base), int(pairing), _stream(stream)))
+
+
+SlotPlan = collections.namedtuple("SlotPlan", "slots positions seq_lens starts info")
+
+
+def prepare_batch_slots(cached_lens, new_lens, free_blocks, block_table, n_tokens=None, slots=None,
+                        positions=None, seq_lens=None, starts=None, info=None, stream=None):
+    """batch_slots with every argument fixed (see prepare_partial)."""
+    B, dev = cached_lens.shape[0], cached_lens.device
+    if slots is None:
+        if n_tokens is None:
+            raise ValueError("give n_tokens (the most new tokens of a call) or slots")
+        slots = torch.empty(n_tokens, dtype=torch.int32, device=dev)
+
+    def out(t, n):
+        return torch.empty(n, dtype=torch.int32, device=dev) if t is None else t
+    plan = SlotPlan(slots, out(positions, slots.shape[0]), out(seq_lens, B), out(starts, B + 1), out(info, 4))
+    _on_current_gpu(cached_lens, new_lens, free_blocks, block_table, *plan)
+    keep = (cached_lens, new_lens, free_blocks, block_table)
+    d = [describe(t) for t in (*keep, *plan)]
+    return _Prepared(load().mla_batch_slots, (*[_ref(x) for x in d], _stream(stream)), (d, keep), plan)
+
+
+def batch_slots(cached_lens, new_lens, free_blocks, block_table, n_tokens=None, slots=None,
+                positions=None, seq_lens=None, starts=None, info=None, stream=None):
+    """Block tables and slot maps of a batch from its lengths, on the GPU:
+    extends block_table [B, NB] in place with blocks of free_blocks, and
+    returns SlotPlan(slots, positions, seq_lens, starts, info) for the new
+    tokens packed request after request (see mla_batch_slots in the header).
+    n_tokens, or the length of a given slots, is the most tokens it holds."""
+    return prepare_batch_slots(cached_lens, new_lens, free_blocks, block_table, n_tokens, slots,
+                               positions, seq_lens, starts, info, stream)()
+
+
+def prepare_rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=10000.0,
+                 scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0, mscale=1.0,
+                 inverse=False, stream=None):
+    """rope with every argument fixed (see prepare_partial)."""
+    if x.dim() != 3:
+        raise ValueError("x must be [T, H, D]")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _on_current_gpu(x, positions, out)
+    o = RopeOpts(int(rot_offset), int(x.shape[2] - rot_offset if rot_dim is None else rot_dim),
+                 int(pairing), ROPE_SCALINGS.index(scaling), int(bool(inverse)), 0, float(base),
+                 float(factor), float(beta_fast), float(beta_slow), float(mscale), int(orig_len))
+    d = [describe(t) for t in (x, positions, out)]
+    return _Prepared(load().mla_rope, (*[_ref(t) for t in d], ctypes.byref(o), _stream(stream)),
+                     (d, o, x, positions), out)
+
+
+def rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=10000.0,
+         scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0, mscale=1.0,
+         inverse=False, stream=None):
+    """Rotary positions of x [T, H, D] (bf16 or fp32): dims rot_offset ..
+    rot_offset + rot_dim - 1 (default: to the end) of row t turn by
+    positions[t], the others are copied.  pairing 0: dims (2i, 2i+1), 1: (i,
+    i + rot_dim/2); scaling "none", "linear" (factor) or "yarn" (factor,
+    orig_len, beta_fast, beta_slow); out may be x.  inverse=True is the
+    transpose of the map, which takes gradients of out to gradients of x."""
+    return prepare_rope(x, positions, out, rot_offset, rot_dim, pairing, base, scaling, factor,
+                        orig_len, beta_fast, beta_slow, mscale, inverse, stream)()
+
+
+def prepare_cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):
+    """cache_append with every argument fixed (see prepare_partial)."""
+    _on_current_gpu(ckv, kpe, slots, ckv_pool, kpe_pool)
+    d = [describe(ckv), describe(kpe), describe(slots), _describe_latent(ckv_pool), describe(kpe_pool)]
+    return _Prepared(load().mla_cache_append, (*[_ref(t) for t in d], _stream(stream)),
+                     (d, ckv, kpe, slots), (ckv_pool, kpe_pool))
+
+
+def cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):
+    """Writes new tokens [T, 512] / [T, 64] (bf16) into the pools at slots
+    (block * 64 + row; others than the pool's are skipped): a bf16 latent pool
+    [P, 64, 512] as they are, a 4-bit one [P, 64, 272] (uint8) as E2M1 codes
+    under a power of two per 32 columns.  Returns the pools."""
+    return prepare_cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream)()
 
 
 def primitive_costs(mq, chunk_tokens, q_bytes=1152, p_bytes=1032, kv_bytes=1152, **model):

@@ -1,0 +1,241 @@
+"""What the entry points of a serving step refuse on the host, before anything
+is enqueued, and the references' own checks (CPU only)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import step as S
+from paper_2606_01502_amd import mla
+
+INVALID, UNSUPPORTED = mla.MLA_ERR_INVALID_ARGUMENT, mla.MLA_ERR_UNSUPPORTED
+I32, BF16, F32, U8 = torch.int32, torch.bfloat16, torch.float32, torch.uint8
+
+
+def z(*s, dt=BF16):
+    return torch.zeros(s, dtype=dt)
+
+
+def _ref(t):
+    if t is None:
+        return None
+    return ctypes.byref(mla._describe_latent(t) if t.dtype == U8 else mla.describe(t))
+
+
+# ---- the calls, as (valid arguments, call)
+def slots_args():
+    return dict(cached=z(3, dt=I32), new=z(3, dt=I32), free=z(9, dt=I32), table=z(3, 5, dt=I32),
+                slots=z(40, dt=I32), positions=z(40, dt=I32), seq=z(3, dt=I32), starts=z(4, dt=I32),
+                info=z(4, dt=I32))
+
+
+def slots_call(a):
+    lib = mla.load()
+    st = lib.mla_batch_slots(*[_ref(a[k]) for k in ("cached", "new", "free", "table", "slots", "positions",
+                                                    "seq", "starts", "info")], None)
+    return st, lib.mla_last_error().decode()
+
+
+def rope_args(**o):
+    x = z(4, 3, 96)
+    opts = dict(rot_offset=32, rot_dim=64, base=1e4, factor=8.0, beta_fast=32.0, beta_slow=1.0,
+                mscale=1.0, orig_len=4096)
+    opts.update(o)
+    return dict(x=x, pos=z(4, dt=I32), out=z(4, 3, 96), opts=mla.RopeOpts(**opts))
+
+
+def rope_call(a):
+    lib = mla.load()
+    st = lib.mla_rope(_ref(a["x"]), _ref(a["pos"]), _ref(a["out"]),
+                      ctypes.byref(a["opts"]) if a["opts"] is not None else None, None)
+    return st, lib.mla_last_error().decode()
+
+
+def append_args(mx4=True):
+    return dict(ckv=z(5, 512), kpe=z(5, 64), slots=z(5, dt=I32),
+                pool=z(2, 64, 272, dt=U8) if mx4 else z(2, 64, 512), kpe_pool=z(2, 64, 64))
+
+
+def append_call(a):
+    lib = mla.load()
+    st = lib.mla_cache_append(*[_ref(a[k]) for k in ("ckv", "kpe", "slots", "pool", "kpe_pool")], None)
+    return st, lib.mla_last_error().decode()
+
+
+def off(t, n):
+    flat = torch.zeros(t.numel() + n, dtype=t.dtype)
+    return flat[n:].view(t.shape)
+
+
+SLOTS = [
+    ("null", dict(info=None), INVALID, "info"),
+    ("int64", dict(cached=z(3, dt=torch.int64)), INVALID, "cached_lens: wrong dtype"),
+    ("strided", dict(new=z(6, dt=I32)[::2]), INVALID, "innermost stride"),
+    ("B of new_lens", dict(new=z(4, dt=I32)), INVALID, "starts [B + 1]"),
+    ("B of starts", dict(starts=z(3, dt=I32)), INVALID, "starts [B + 1]"),
+    ("B of table", dict(table=z(2, 5, dt=I32)), INVALID, "starts [B + 1]"),
+    ("table 1-d", dict(table=z(15, dt=I32)), INVALID, "block_table: expected 2 dims"),
+    ("T of positions", dict(positions=z(39, dt=I32)), INVALID, "positions"),
+    ("info", dict(info=z(3, dt=I32)), INVALID, "info: shape"),
+    ("table rows one memory", dict(table=z(1, 5, dt=I32).expand(3, 5)), INVALID, "rows overlap"),
+]
+
+
+@pytest.mark.parametrize("name,change,status,text", SLOTS, ids=[c[0] for c in SLOTS])
+def test_slots_refused(name, change, status, text):
+    a = slots_args()
+    a.update(change)
+    st, msg = slots_call(a)
+    assert st == status and text in msg, (st, msg)
+
+
+def test_slots_overlaps_refused():
+    a = slots_args()
+    a["positions"] = a["slots"]
+    st, msg = slots_call(a)
+    assert st == INVALID and "two outputs overlap" in msg
+    a = slots_args()
+    a["seq"] = a["cached"]
+    st, msg = slots_call(a)
+    assert st == INVALID and "overlaps an input" in msg
+
+
+def test_slots_too_many_requests():
+    B = 8193
+    a = dict(cached=z(B, dt=I32), new=z(B, dt=I32), free=z(1, dt=I32), table=z(B, 1, dt=I32),
+             slots=z(1, dt=I32), positions=z(1, dt=I32), seq=z(B, dt=I32), starts=z(B + 1, dt=I32),
+             info=z(4, dt=I32))
+    st, msg = slots_call(a)
+    assert st == UNSUPPORTED and "8192" in msg
+
+
+ROPE = [
+    ("opts null", dict(opts=None), "opts"),
+    ("x fp16", dict(x=torch.zeros(4, 3, 96, dtype=torch.float16)), "x: wrong dtype"),
+    ("x 2-d", dict(x=z(4, 96)), "x: expected 3 dims"),
+    ("out fp32 for bf16", dict(out=z(4, 3, 96, dt=F32)), "out: wrong dtype"),
+    ("out shape", dict(out=z(4, 3, 64)), "out: shape"),
+    ("positions int64", dict(pos=z(4, dt=torch.int64)), "positions: wrong dtype"),
+    ("positions length", dict(pos=z(3, dt=I32)), "positions"),
+    ("out rows overlap", dict(out=z(4, 1, 96).expand(4, 3, 96)), "rows overlap"),
+]
+ROPE += [(f"opts {k}={v}", dict(opts=rope_args(**{k: v, **more})["opts"]), text) for k, v, more, text in [
+    ("rot_dim", 63, {}, "rot_dim"), ("rot_dim", 0, {}, "rot_dim"), ("rot_dim", 258, {}, "rot_dim"),
+    ("rot_offset", 33, {}, "within the head"), ("rot_offset", -1, {}, "within the head"),
+    ("pairing", 2, {}, "pairing"), ("inverse", 2, {}, "inverse"), ("scaling", 3, {}, "scaling"),
+    ("reserved", 1, {}, "reserved"), ("base", 0.0, {}, "base"), ("base", float("inf"), {}, "base"),
+    ("mscale", float("nan"), {}, "mscale"), ("factor", 0.0, {"scaling": 1}, "factor"),
+    ("factor", float("nan"), {"scaling": 2}, "factor"), ("base", 1.0, {"scaling": 2}, "YARN"),
+    ("orig_len", 0, {"scaling": 2}, "YARN"), ("beta_slow", 0.0, {"scaling": 2}, "YARN"),
+    ("beta_slow", 33.0, {"scaling": 2}, "YARN"), ("beta_fast", float("inf"), {"scaling": 2}, "YARN")]]
+
+
+@pytest.mark.parametrize("name,change,text", ROPE, ids=[c[0] for c in ROPE])
+def test_rope_refused(name, change, text):
+    a = rope_args()
+    a.update(change)
+    st, msg = rope_call(a)
+    assert st == INVALID and text in msg, (st, msg)
+
+
+def test_rope_overlap_refused():
+    base = z(6, 3, 96)
+    a = rope_args()
+    a["x"], a["out"] = base[:4], base[1:5]
+    st, msg = rope_call(a)
+    assert st == INVALID and "out overlaps x" in msg
+    # the same memory under other strides is no rotation in place
+    sq = z(4, 4, 96)
+    a["x"], a["out"] = sq, sq.transpose(0, 1)
+    st, msg = rope_call(a)
+    assert st == INVALID and "out overlaps x" in msg
+
+
+APPEND = [
+    ("ckv fp32", dict(ckv=z(5, 512, dt=F32)), INVALID, "ckv: wrong dtype"),
+    ("kpe rows", dict(kpe=z(4, 64)), INVALID, "shapes must be"),
+    ("ckv width", dict(ckv=z(5, 272)), INVALID, "shapes must be"),
+    ("slots int64", dict(slots=z(5, dt=torch.int64)), INVALID, "slots: wrong dtype"),
+    ("slots length", dict(slots=z(6, dt=I32)), INVALID, "slots"),
+    ("fp8 pool", dict(pool=z(2, 64, 512, dt=U8)), UNSUPPORTED, "fp8"),
+    ("pool fp32", dict(pool=z(2, 64, 512, dt=F32)), INVALID, "ckv_pool: wrong dtype"),
+    ("pool strided", dict(pool=z(4, 64, 512)[::2]), INVALID, "contiguous"),
+    ("P differs", dict(kpe_pool=z(3, 64, 64)), INVALID, "contiguous"),
+    ("kpe pool dtype", dict(kpe_pool=z(2, 64, 64, dt=U8)), INVALID, "kpe_pool: wrong dtype"),
+    ("ckv unaligned", dict(ckv=off(z(5, 512), 1)), INVALID, "aligned"),
+    ("kpe row stride", dict(kpe=z(5, 65)[:, :64]), INVALID, "aligned"),
+    ("pool unaligned", dict(pool=off(z(2, 64, 272, dt=U8), 8)), INVALID, "pools must be 16-byte aligned"),
+]
+
+
+@pytest.mark.parametrize("name,change,status,text", APPEND, ids=[c[0] for c in APPEND])
+def test_append_refused(name, change, status, text):
+    a = append_args()
+    a.update(change)
+    st, msg = append_call(a)
+    assert st == status and text in msg, (st, msg)
+
+
+def test_append_overlap_refused():
+    a = append_args(mx4=False)
+    a["ckv"] = a["pool"].view(-1, 512)[:5]
+    st, msg = append_call(a)
+    assert st == INVALID and "overlaps" in msg
+
+
+def test_gather_of_a_4bit_pool_checks_its_rows():
+    lib = mla.load()
+    out = [z(1, 3, 512), z(1, 3, 64)]
+    for pool, text in ((z(1, 2, 64, 512, dt=U8), "wrong dtype"), (z(1, 4, 64, 272, dt=U8)[:, ::2], "272")):
+        st = lib.mla_fetch_gather(_ref(pool), _ref(z(1, 2, 64, 64)), _ref(z(2, dt=I32)), _ref(z(3, dt=I32)),
+                                  _ref(out[0]), _ref(out[1]), None)
+        assert st == INVALID and text in lib.mla_last_error().decode()
+
+
+def test_binding_refuses_host_tensors():
+    a = append_args()
+    with pytest.raises(ValueError, match="GPU"):
+        mla.cache_append(a["ckv"], a["kpe"], a["slots"], a["pool"], a["kpe_pool"])
+    with pytest.raises(ValueError, match="GPU"):
+        mla.rope(z(4, 3, 64), z(4, dt=I32))
+    s = slots_args()
+    with pytest.raises(ValueError, match="GPU"):
+        mla.batch_slots(s["cached"], s["new"], s["free"], s["table"], n_tokens=3)
+    with pytest.raises(ValueError, match="n_tokens"):
+        mla.batch_slots(s["cached"], s["new"], s["free"], s["table"])
+    with pytest.raises(ValueError):
+        mla.rope(z(4, 3, 64), z(4, dt=I32), scaling="other")
+
+
+# ---- the references
+def test_mx4_reference_round_trips_every_code():
+    """Every code under every exponent that the writer uses reads and writes
+    back as itself, where the group's largest magnitude is 4 or 6 units."""
+    codes = np.arange(16, dtype=np.uint8)
+    group = np.concatenate([codes, codes])
+    for e in (-125, -1, 0, 3, 125):
+        row = np.zeros(272, np.uint8)
+        c = np.tile(group, 16)
+        row[:256] = c[0::2] | (c[1::2] << 4)
+        row[256:] = e + 127
+        assert np.array_equal(S.mx4_encode(S.mx4_decode(row)), row)
+
+
+def test_mx4_reference_halfway_values():
+    """Halfway between two magnitudes goes to the even code; past 6 units to 6."""
+    x = np.zeros(512)
+    x[:11] = [4.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 5.01, 7.9, -0.25]
+    got = S.mx4_decode(S.mx4_encode(x))[:11]
+    assert np.array_equal(got, [4.0, 0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 6.0, 6.0, 0.0])
+
+
+def test_rope_reference_is_a_rotation():
+    x = np.random.default_rng(0).standard_normal((5, 2, 80))
+    kw = dict(at=16, d=64, base=1e4, scaling="yarn", factor=8.0, orig_len=4096)
+    for pairing in (0, 1):
+        y = S.rope(x, [0, 1, 77, -3, 2 ** 31 - 1], pairing=pairing, **kw)
+        assert np.allclose((y ** 2).sum(-1), (x ** 2).sum(-1)) and np.array_equal(y[0], x[0])
+        assert np.array_equal(y[..., :16], x[..., :16])
+        back = S.rope(y, [0, 1, 77, -3, 2 ** 31 - 1], pairing=pairing, inverse=True, **kw)
+        assert np.allclose(back, x)
