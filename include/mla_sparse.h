@@ -101,7 +101,11 @@ typedef struct {
  *                                     order) sends its q once; those jobs are
  *                                     scheduled next to each other
  *   ckv_pool          [P, 64, 512]    bf16 or fp8-e4m3fn (+block_scale), contiguous
- *   kpe_pool          [P, 64, 64]     same dtype as ckv_pool, contiguous
+ *                 or  [P, 64, 272]    MXFP4 (4 bits): one selection per job
+ *                                     ([R, K]) and 64-row tiles only
+ *                                     (MLA_ERR_UNSUPPORTED otherwise)
+ *   kpe_pool          [P, 64, 64]     same dtype as ckv_pool (bf16 beside MXFP4),
+ *                                     contiguous
  *                                     fp8: both descriptors carry a block_scale;
  *                                     passing the same array for both (one scale
  *                                     per block for the whole 576-wide entry) is
@@ -271,6 +275,51 @@ mla_status_t mla_sparse_partial_attn_tokens(const mla_tensor_t* q_lat, const mla
                                             const mla_tensor_t* out_lat,
                                             const mla_tensor_t* out_lse,
                                             const mla_partial_opts_t* opts, void* stream);
+
+/* Options of mla_window_attn. */
+typedef struct {
+  int32_t window;      /* tokens a row sees up to its own; 0: all of them          */
+  int32_t n_sink;      /* first tokens of the sequence that every row sees         */
+  int32_t n_splits;    /* split-K: splits of a tile's tokens (0 = automatic)       */
+  int32_t out_format;  /* MLA_OUT_FP32 or MLA_OUT_BF16_WIRE                        */
+  int32_t reserved[4]; /* must be zero                                             */
+} mla_window_opts_t;
+
+/*
+ * Attention through a sliding window with sinks, over the paged sequences of B
+ * requests: the local part of a step, beside the selected blocks of
+ * mla_sparse_partial_attn (whose partials it merges with), and with window 0
+ * causal attention over all of a cache.
+ *
+ *   q_lat [B, Mq, H, 512], q_pe [B, Mq, H, 64] bf16   as there, a q per request
+ *   ckv_pool, kpe_pool                as there: bf16, fp8-e4m3fn or MXFP4
+ *   block_table       [B, NB] int32   logical block of request b's sequence ->
+ *                                     pool block
+ *   seq_lens          [B] int32       tokens of the sequence, those of its query
+ *                                     rows among them
+ *   q_lens            [B] int32       query rows that request b has, its first
+ *                                     ones (NULL: all Mq); at most Mq count
+ *   out_lat, out_lse                  as there, in either form
+ *
+ * Row i < q_lens[b] sits at position p = seq_lens[b] - q_lens[b] + i and sees the
+ * tokens t <= p with t > p - window, or t < n_sink (window 0: all t <= p; n_sink
+ * then says nothing).  A row that sees no token, as the rows from q_lens[b] on
+ * and those at negative positions, is empty: out_lat 0, out_lse -inf (wire: (-inf,
+ * 0)).  Scores, weights and splits are those of mla_sparse_partial_attn, as are
+ * the layout rules, the limits of scale, the workspace and graph capture.  What the
+ * cache holds behind a sequence's last token is not used, whatever it is; blocks
+ * past NB, and those whose table entry is outside [0, P) (a window may let go of
+ * the blocks behind it), are left out.  A request's work is that of the blocks its
+ * rows see; plans are made for the NB blocks that the table is wide, so a table
+ * view as wide as the longest sequence serves best.  NB at most 2^25 blocks
+ * (MLA_ERR_UNSUPPORTED).
+ */
+mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
+                             const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
+                             const mla_tensor_t* block_table, const mla_tensor_t* seq_lens,
+                             const mla_tensor_t* q_lens, float scale, const mla_tensor_t* out_lat,
+                             const mla_tensor_t* out_lse, const mla_window_opts_t* opts,
+                             void* stream);
 
 /*
  * Log-sum-exp merge of n_parts partials of the same rows (the requester's

@@ -102,3 +102,29 @@ def mx4_decode(rows):
     byte = rows[..., 256:].astype(np.int64)
     s = np.where(byte == 255, np.nan, np.exp2(byte.astype(np.float64) - 127))
     return v * np.repeat(s, 32, axis=-1)
+
+
+def visible(n, pos, window, n_sink):
+    """Which of tokens 0 .. n - 1 a row at position pos sees."""
+    t = np.arange(n)
+    see = t <= pos
+    return see & ((t > pos - window) | (t < n_sink)) if window else see
+
+
+def attend(q, keys, values, see, scale):
+    """Attention of rows q [h, 576] over the tokens `see` of keys [n, 576] /
+    values [n, 512], all float64, in two passes.  Returns a dict of out [h,
+    512], lse, m, l [h]; sum_t p_t |v_t| (mag) and the largest sum |q| |k|
+    |scale| of a row's tokens (smag), which tolerances are made of."""
+    h = q.shape[0]
+    if not see.any():
+        return dict(out=np.zeros((h, values.shape[1])), lse=np.full(h, -np.inf), m=np.full(h, -np.inf),
+                    l=np.zeros(h), mag=np.zeros((h, values.shape[1])), smag=np.zeros(h))
+    k, v = keys[see], values[see]
+    s = scale * (q @ k.T)
+    m = s.max(1)
+    e = np.exp(s - m[:, None])
+    ell = e.sum(1)
+    p = e / ell[:, None]
+    return dict(out=p @ v, lse=m + np.log(ell), m=m, l=ell, mag=p @ np.abs(v),
+                smag=abs(scale) * (np.abs(q) @ np.abs(k).T).max(1))

@@ -118,6 +118,173 @@ int device_cus() {
   return cus;
 }
 
+bool shape_is(const mla_tensor_t* t, std::initializer_list<int64_t> s) {
+  int d = 0;
+  for (int64_t v : s)
+    if (t->shape[d++] != v) return false;
+  return true;
+}
+
+// The pools of an attention call: types, shapes, then layout.  The latent pool is
+// bf16, e4m3 (the RoPE pool alike, both with scales) or 4 bits (the RoPE pool bf16).
+mla_status_t check_pool_types(const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool) {
+  const int32_t kv_dtype = ckv_pool->dtype;
+  if (kv_dtype != MLA_DTYPE_BF16 && kv_dtype != MLA_DTYPE_FP8_E4M3FN && kv_dtype != MLA_DTYPE_MXFP4)
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: dtype must be bf16 or fp8-e4m3fn or mxfp4");
+  const bool fp8 = kv_dtype == MLA_DTYPE_FP8_E4M3FN;
+  mla_status_t st;
+  if ((st = check_tensor(ckv_pool, "ckv_pool", kv_dtype, 3, fp8)) != MLA_OK) return st;
+  const int32_t pe_dtype = kv_dtype == MLA_DTYPE_MXFP4 ? (int32_t)MLA_DTYPE_BF16 : kv_dtype;
+  if ((st = check_tensor(kpe_pool, "kpe_pool", pe_dtype, 3, fp8)) != MLA_OK) return st;
+  if (fp8 && (!ckv_pool->block_scale || !kpe_pool->block_scale))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "fp8 pools need block_scale");
+  return MLA_OK;
+}
+
+int64_t latent_row(const mla_tensor_t& ckv_pool) { return ckv_pool.dtype == MLA_DTYPE_MXFP4 ? MLA_MX4_ROW : MLA_DLAT; }
+
+mla_status_t check_pool_shapes(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
+  const int64_t P = ckv_pool.shape[0];
+  if (!shape_is(&ckv_pool, {P, MLA_BLOCK, latent_row(ckv_pool)}))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: shape must be [P, 64, 512] (MXFP4: [P, 64, 272])");
+  if (!shape_is(&kpe_pool, {P, MLA_BLOCK, MLA_DPE}))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "kpe_pool: shape must be [P, 64, 64] with the P of ckv_pool");
+  return MLA_OK;
+}
+
+mla_status_t check_pool_layout(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
+  const int64_t row = latent_row(ckv_pool);
+  if (ckv_pool.stride[0] != MLA_BLOCK * row || ckv_pool.stride[1] != row ||
+      kpe_pool.stride[0] != MLA_BLOCK * MLA_DPE || kpe_pool.stride[1] != MLA_DPE)
+    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be contiguous");
+  if (!aligned16(ckv_pool.data) || !aligned16(kpe_pool.data))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
+  return MLA_OK;
+}
+
+bool pairs_aligned(const mla_tensor_t& lse) {
+  return (reinterpret_cast<uintptr_t>(lse.data) & 7u) == 0 && lse.stride[0] % 2 == 0 && lse.stride[1] % 2 == 0 &&
+         lse.stride[2] % 2 == 0;
+}
+
+int cache_kind(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
+  if (ckv_pool.dtype == MLA_DTYPE_MXFP4) return mla::kKvMx4;
+  if (ckv_pool.dtype == MLA_DTYPE_BF16) return mla::kKvBf16;
+  return ckv_pool.block_scale == kpe_pool.block_scale ? mla::kKvFp8Shared : mla::kKvFp8Split;
+}
+
+// What selections and windows share of the kernel's parameters.
+mla::PartialParams common_params(const mla_tensor_t& q_lat, const mla_tensor_t& q_pe, const mla_tensor_t& ckv_pool,
+                                 const mla_tensor_t& kpe_pool, const mla_tensor_t& table, float scale,
+                                 const mla_tensor_t& out_lat, const mla_tensor_t& out_lse, bool wire) {
+  mla::PartialParams p{};
+  p.q_lat = (const uint16_t*)q_lat.data;
+  p.q_pe = (const uint16_t*)q_pe.data;
+  p.ql_s0 = q_lat.stride[0]; p.ql_s1 = q_lat.stride[1]; p.ql_s2 = q_lat.stride[2];
+  p.qp_s0 = q_pe.stride[0]; p.qp_s1 = q_pe.stride[1]; p.qp_s2 = q_pe.stride[2];
+  p.ckv = (const uint8_t*)ckv_pool.data;
+  p.kpe = (const uint8_t*)kpe_pool.data;
+  p.ckv_scale = ckv_pool.block_scale;
+  p.kpe_scale = kpe_pool.block_scale;
+  p.table = (const int32_t*)table.data;
+  p.table_s0 = table.stride[0];
+  p.P = ckv_pool.shape[0];
+  p.NB = (int32_t)table.shape[1];
+  p.Mq = (int32_t)q_lat.shape[1];
+  p.H = (int32_t)q_lat.shape[2];
+  p.rows = p.Mq * p.H;
+  p.by_H = mla::make_div(p.H);
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634074);
+  p.out_wire = wire ? 1 : 0;
+  p.out16 = (uint16_t*)out_lat.data;
+  p.out = (float*)out_lat.data;
+  p.out_s0 = out_lat.stride[0]; p.out_s1 = out_lat.stride[1]; p.out_s2 = out_lat.stride[2];
+  p.lse = (float*)out_lse.data;
+  p.lse_s0 = out_lse.stride[0]; p.lse_s1 = out_lse.stride[1]; p.lse_s2 = out_lse.stride[2];
+  return p;
+}
+
+// Chooses the plan, takes the split-K workspace and queues the kernels.  p holds
+// the tensors of a checked call; its plan is filled in here.
+mla_status_t enqueue(const mla::Planner& planner, mla::PartialParams& p, int64_t R, int kv, int sel_kind,
+                     bool no_alloc, hipStream_t hs) {
+  mla_status_t st;
+  if (planner.refused) return fail(MLA_ERR_UNSUPPORTED, planner.refused);
+  mla::Plan plan = planner.choose();
+  std::unique_lock<std::mutex> ws_lock;  // held until the combine is queued
+  void* ws = nullptr;
+  if (plan.S > 1 && no_alloc) {
+    const uint64_t need = planner.ws_size(plan.S);
+    if (need > (uint64_t)MLA_NOALLOC_SCRATCH_BYTES)
+      return fail(MLA_ERR_UNSUPPORTED,
+                  "this call's split-K partials need " + std::to_string(need) +
+                      " bytes, more than the " + std::to_string((long long)MLA_NOALLOC_SCRATCH_BYTES) +
+                      "-byte scratch array of the allocation-free entry point (fewer jobs or "
+                      "splits per call)");
+    if ((st = scratch_address(&ws)) != MLA_OK) return st;
+  } else if (plan.S > 1) {
+    st = get_workspace(hs, planner.ws_size(plan.S), &ws, ws_lock);
+    // Where the workspace cannot grow (the stream is being captured, or memory
+    // is short) the covering plan may do with less, often with none.
+    if (st != MLA_OK && planner.a.n_splits == 0 && planner.cover.S < plan.S) {
+      if (ws_lock.owns_lock()) ws_lock.unlock();
+      plan = planner.cover;
+      st = plan.S > 1 ? get_workspace(hs, planner.ws_size(plan.S), &ws, ws_lock) : MLA_OK;
+      if (st == MLA_OK) g_last_error.clear();
+    }
+    if (st != MLA_OK) return st;
+  }
+  const int row_groups = plan.row_groups;
+  const int64_t row_tiles = plan.row_tiles, S = plan.S, sps = plan.sps;
+  const bool by_id = plan.by_id;
+  if (R * row_tiles * S > INT32_MAX) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
+
+  p.n_splits = (int32_t)S;
+  p.slots_per_split = (int32_t)sps;
+  p.split_by_id = by_id ? 1 : 0;
+  p.long_lists = plan.long_lists ? 1 : 0;
+  // split-major numbering once a split's row tiles fill an XCD's share of
+  // the grid (below that the combine's reads of a tile's splits on one XCD
+  // are worth more than the shared block loads)
+  p.tiles_fast = by_id && row_tiles >= 8 ? 1 : 0;
+  p.row_tiles = (int32_t)row_tiles;
+  p.by_splits = mla::make_div(S);
+  p.by_tiles = mla::make_div(row_tiles);
+  p.by_rep = mla::make_div(p.q_rep);
+  p.by_K = mla::make_div(std::max<int64_t>(p.K, 1));
+  if (S > 1) {
+    const size_t n_part_rows = (size_t)R * S * p.rows;
+    p.ws_f16 = planner.ws_half(S);
+    const size_t o_bytes = planner.ws_rows_bytes(S);
+    p.ws_o32 = (float*)ws;
+    p.ws_o16 = (uint16_t*)ws;
+    p.ws_scale = (float*)((char*)ws + o_bytes);
+    p.ws_lse = p.ws_scale + n_part_rows;
+    p.ws_max = p.ws_lse + n_part_rows;
+  }
+  hipError_t e = mla::launch_partial(p, (int)R, kv, row_groups, sel_kind, hs);
+  if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("partial kernel launch: ") + hipGetErrorString(e));
+  if (S > 1) {
+    mla::CombineParams c{};
+    c.ws_f16 = p.ws_f16;
+    c.ws_o32 = p.ws_o32;
+    c.ws_o16 = p.ws_o16;
+    c.ws_scale = p.ws_scale;
+    c.ws_lse = p.ws_lse;
+    c.ws_max = p.ws_max;
+    c.R = (int32_t)R; c.S = (int32_t)S; c.Mq = p.Mq; c.H = p.H; c.rows = p.rows;
+    c.by_H = p.by_H;
+    c.by_rows = mla::make_div(p.rows);
+    c.out_wire = p.out_wire;
+    c.out16 = p.out16;
+    c.out = p.out; c.out_s0 = p.out_s0; c.out_s1 = p.out_s1; c.out_s2 = p.out_s2;
+    c.lse = p.lse; c.lse_s0 = p.lse_s0; c.lse_s1 = p.lse_s1; c.lse_s2 = p.lse_s2;
+    e = mla::launch_combine(c, hs);
+    if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("combine kernel launch: ") + hipGetErrorString(e));
+  }
+  return MLA_OK;
+}
+
 // The partial call; `tokens`: sel names single logical tokens (block * 64 +
 // t) rather than blocks; `no_alloc`: the split-K workspace is the static
 // scratch array (nothing is allocated; sizes beyond it are refused).
@@ -135,13 +302,8 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     if ((st = check_tensor(q_pe, "q_pe", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
     if (!ckv_pool || !kpe_pool) return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool/kpe_pool: null descriptor");
     const int32_t kv_dtype = ckv_pool->dtype;
-    if (kv_dtype != MLA_DTYPE_BF16 && kv_dtype != MLA_DTYPE_FP8_E4M3FN)
-      return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: dtype must be bf16 or fp8-e4m3fn");
-    const bool fp8 = kv_dtype == MLA_DTYPE_FP8_E4M3FN;
-    if ((st = check_tensor(ckv_pool, "ckv_pool", kv_dtype, 3, fp8)) != MLA_OK) return st;
-    if ((st = check_tensor(kpe_pool, "kpe_pool", kv_dtype, 3, fp8)) != MLA_OK) return st;
-    if (fp8 && (!ckv_pool->block_scale || !kpe_pool->block_scale))
-      return fail(MLA_ERR_INVALID_ARGUMENT, "fp8 pools need block_scale");
+    if ((st = check_pool_types(ckv_pool, kpe_pool)) != MLA_OK) return st;
+    const bool fp8 = kv_dtype == MLA_DTYPE_FP8_E4M3FN, mx4 = kv_dtype == MLA_DTYPE_MXFP4;
     if ((st = check_tensor(chunk_block_table, "chunk_block_table", MLA_DTYPE_INT32, 2)) != MLA_OK) return st;
     const bool per_row = !tokens && sel_block_ids && sel_block_ids->ndim == 3;
     const char* sel_name = tokens ? "sel_token_ids" : "sel_block_ids";
@@ -151,6 +313,10 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     if ((st = check_tensor(out_lat, "out_lat", wire ? MLA_DTYPE_BF16 : MLA_DTYPE_FP32, 4)) != MLA_OK)
       return st;
     if ((st = check_tensor(out_lse, "out_lse", MLA_DTYPE_FP32, wire ? 4 : 3)) != MLA_OK) return st;
+    if (mx4 && (tokens || per_row))
+      return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take one block selection per job");
+    if (mx4 && opts && opts->row_tile == 128)
+      return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take 64-row tiles");
     if (opts) {
       for (int i = 0; i < 5; ++i)
         if (opts->reserved[i]) return fail(MLA_ERR_INVALID_ARGUMENT, "opts.reserved must be zero");
@@ -167,19 +333,12 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     const int64_t Rq = q_lat->shape[0], Mq = q_lat->shape[1], H = q_lat->shape[2];
     const int64_t P = ckv_pool->shape[0];
     const int64_t NB = chunk_block_table->shape[1], K = sel_block_ids->shape[per_row ? 2 : 1];
-    auto shape_is = [](const mla_tensor_t* t, std::initializer_list<int64_t> s) {
-      int d = 0;
-      for (int64_t v : s)
-        if (t->shape[d++] != v) return false;
-      return true;
-    };
     if (q_lat->shape[3] != MLA_DLAT) return fail(MLA_ERR_INVALID_ARGUMENT, "q_lat: last dim must be 512");
     if (R > 0 ? (Rq < 1 || R % Rq != 0) : Rq != 0)
       return fail(MLA_ERR_INVALID_ARGUMENT,
                   "q_lat: its first dim R_q must divide the number of jobs R (job r reads q row r mod R_q)");
     if (!shape_is(q_pe, {Rq, Mq, H, MLA_DPE})) return fail(MLA_ERR_INVALID_ARGUMENT, "q_pe: shape must be [R_q, Mq, H, 64]");
-    if (!shape_is(ckv_pool, {P, MLA_BLOCK, MLA_DLAT})) return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: shape must be [P, 64, 512]");
-    if (!shape_is(kpe_pool, {P, MLA_BLOCK, MLA_DPE})) return fail(MLA_ERR_INVALID_ARGUMENT, "kpe_pool: shape must be [P, 64, 64] with the P of ckv_pool");
+    if ((st = check_pool_shapes(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
     if (chunk_block_table->shape[0] != R) return fail(MLA_ERR_INVALID_ARGUMENT, "chunk_block_table: shape must be [R, NB]");
     if (sel_block_ids->shape[0] != R || (per_row && sel_block_ids->shape[1] != Mq))
       return fail(MLA_ERR_INVALID_ARGUMENT, "sel_block_ids: shape must be [R, K] or [R, Mq, K]");
@@ -188,17 +347,12 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
       return fail(MLA_ERR_INVALID_ARGUMENT, "out_lse: shape must be [R, Mq, H]");
     if (wire && (!shape_is(out_lse, {R, Mq, H, 2}) || out_lse->stride[3] != 1))
       return fail(MLA_ERR_INVALID_ARGUMENT, "out_lse: the wire form takes [R, Mq, H, 2] (m, l) pairs");
-    if (ckv_pool->stride[0] != MLA_BLOCK * MLA_DLAT || ckv_pool->stride[1] != MLA_DLAT ||
-        kpe_pool->stride[0] != MLA_BLOCK * MLA_DPE || kpe_pool->stride[1] != MLA_DPE)
-      return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be contiguous");
-    if (!aligned16(ckv_pool->data) || !aligned16(kpe_pool->data))
-      return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
+    if ((st = check_pool_layout(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
     if (!rows_aligned(*q_lat, 2) || !rows_aligned(*q_pe, 2))
       return fail(MLA_ERR_INVALID_ARGUMENT, "q_lat/q_pe rows must be 16-byte aligned");
     if (!rows_aligned(*out_lat, wire ? 2 : 4))
       return fail(MLA_ERR_INVALID_ARGUMENT, "out_lat rows must be 16-byte aligned");
-    if (wire && ((reinterpret_cast<uintptr_t>(out_lse->data) & 7u) != 0 || out_lse->stride[0] % 2 ||
-                 out_lse->stride[1] % 2 || out_lse->stride[2] % 2))
+    if (wire && !pairs_aligned(*out_lse))
       return fail(MLA_ERR_INVALID_ARGUMENT, "out_lse (m, l) pairs must be 8-byte aligned");
     // |scale| <= 2^64 keeps scale * log2(e) and the scores of any bf16 or fp8
     // rows whose dot products stay below 2^63 finite in fp32
@@ -225,126 +379,127 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     const int64_t rows = Mq * H;
     if (R == 0 || rows == 0) return MLA_OK;
 
-    // row tiles and split-K
+    // row tiles and split-K (4-bit caches: 64-row tiles)
     const mla::Planner planner({R, Mq, H, NB, K, tokens, per_row, fp8, opts ? opts->n_splits : 0,
-                                opts ? opts->row_tile : 0, device_cus()});
-    if (planner.refused) return fail(MLA_ERR_UNSUPPORTED, planner.refused);
-    mla::Plan plan = planner.choose();
-    hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
-    std::unique_lock<std::mutex> ws_lock;  // held until the combine is queued
-    void* ws = nullptr;
-    if (plan.S > 1 && no_alloc) {
-      const uint64_t need = planner.ws_size(plan.S);
-      if (need > (uint64_t)MLA_NOALLOC_SCRATCH_BYTES)
-        return fail(MLA_ERR_UNSUPPORTED,
-                    "this call's split-K partials need " + std::to_string(need) +
-                        " bytes, more than the " + std::to_string((long long)MLA_NOALLOC_SCRATCH_BYTES) +
-                        "-byte scratch array of the allocation-free entry point (fewer jobs or "
-                        "splits per call)");
-      if ((st = scratch_address(&ws)) != MLA_OK) return st;
-    } else if (plan.S > 1) {
-      st = get_workspace(hs, planner.ws_size(plan.S), &ws, ws_lock);
-      // Where the workspace cannot grow (the stream is being captured, or memory
-      // is short) the covering plan may do with less, often with none.
-      if (st != MLA_OK && planner.a.n_splits == 0 && planner.cover.S < plan.S) {
-        if (ws_lock.owns_lock()) ws_lock.unlock();
-        plan = planner.cover;
-        st = plan.S > 1 ? get_workspace(hs, planner.ws_size(plan.S), &ws, ws_lock) : MLA_OK;
-        if (st == MLA_OK) g_last_error.clear();
-      }
-      if (st != MLA_OK) return st;
-    }
-    const int row_groups = plan.row_groups;
-    const int64_t row_tiles = plan.row_tiles, S = plan.S, sps = plan.sps;
-    const bool by_id = plan.by_id;
-    if (R * row_tiles * S > INT32_MAX) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
-
-    mla::PartialParams p{};
-    p.q_lat = (const uint16_t*)q_lat->data;
-    p.q_pe = (const uint16_t*)q_pe->data;
-    p.ql_s0 = q_lat->stride[0]; p.ql_s1 = q_lat->stride[1]; p.ql_s2 = q_lat->stride[2];
-    p.qp_s0 = q_pe->stride[0]; p.qp_s1 = q_pe->stride[1]; p.qp_s2 = q_pe->stride[2];
-    p.ckv = (const uint8_t*)ckv_pool->data;
-    p.kpe = (const uint8_t*)kpe_pool->data;
-    p.ckv_scale = ckv_pool->block_scale;
-    p.kpe_scale = kpe_pool->block_scale;
-    p.table = (const int32_t*)chunk_block_table->data;
-    p.table_s0 = chunk_block_table->stride[0];
+                                mx4 ? 64 : opts ? opts->row_tile : 0, device_cus(), mx4});
+    mla::PartialParams p = common_params(*q_lat, *q_pe, *ckv_pool, *kpe_pool, *chunk_block_table, scale, *out_lat,
+                                         *out_lse, wire);
     p.sel = (const int32_t*)sel_block_ids->data;
     p.sel_s0 = sel_block_ids->stride[0];
     p.sel_s1 = per_row ? sel_block_ids->stride[1] : 0;
-    p.P = P;
-    p.NB = (int32_t)NB;
     p.K = (int32_t)K;
-    p.Mq = (int32_t)Mq;
-    p.H = (int32_t)H;
-    p.rows = (int32_t)rows;
-    p.n_splits = (int32_t)S;
-    p.slots_per_split = (int32_t)sps;
-    p.split_by_id = by_id ? 1 : 0;
     p.q_jobs = (int32_t)std::max<int64_t>(Rq, 1);
     p.q_rep = (int32_t)(Rq > 0 ? R / Rq : 1);
-    p.long_lists = plan.long_lists ? 1 : 0;
-    // split-major numbering once a split's row tiles fill an XCD's share of
-    // the grid (below that the combine's reads of a tile's splits on one XCD
-    // are worth more than the shared block loads)
-    p.tiles_fast = by_id && row_tiles >= 8 ? 1 : 0;
-    p.row_tiles = (int32_t)row_tiles;
-    p.by_splits = mla::make_div(S);
-    p.by_tiles = mla::make_div(row_tiles);
-    p.by_H = mla::make_div(H);
-    p.by_rep = mla::make_div(p.q_rep);
-    p.by_K = mla::make_div(std::max<int64_t>(K, 1));
-    p.scale_log2 = (float)((double)scale * 1.4426950408889634074);
-    p.out_wire = wire ? 1 : 0;
-    p.out16 = (uint16_t*)out_lat->data;
-    p.out = (float*)out_lat->data;
-    p.out_s0 = out_lat->stride[0]; p.out_s1 = out_lat->stride[1]; p.out_s2 = out_lat->stride[2];
-    p.lse = (float*)out_lse->data;
-    p.lse_s0 = out_lse->stride[0]; p.lse_s1 = out_lse->stride[1]; p.lse_s2 = out_lse->stride[2];
-    if (S > 1) {
-      const size_t n_part_rows = (size_t)R * S * rows;
-      p.ws_f16 = planner.ws_half(S);
-      const size_t o_bytes = planner.ws_rows_bytes(S);
-      p.ws_o32 = (float*)ws;
-      p.ws_o16 = (uint16_t*)ws;
-      p.ws_scale = (float*)((char*)ws + o_bytes);
-      p.ws_lse = p.ws_scale + n_part_rows;
-      p.ws_max = p.ws_lse + n_part_rows;
-    }
-    const int kv = !fp8 ? mla::kKvBf16
-                 : (ckv_pool->block_scale == kpe_pool->block_scale ? mla::kKvFp8Shared
-                                                                   : mla::kKvFp8Split);
     const int sel_kind = tokens ? mla::kSelTokens : per_row ? mla::kSelPerRow : mla::kSelShared;
-    hipError_t e = mla::launch_partial(p, (int)R, kv, row_groups, sel_kind, hs);
-    if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("partial kernel launch: ") + hipGetErrorString(e));
-    if (S > 1) {
-      mla::CombineParams c{};
-      c.ws_f16 = p.ws_f16;
-      c.ws_o32 = p.ws_o32;
-      c.ws_o16 = p.ws_o16;
-      c.ws_scale = p.ws_scale;
-      c.ws_lse = p.ws_lse;
-      c.ws_max = p.ws_max;
-      c.R = (int32_t)R; c.S = (int32_t)S; c.Mq = (int32_t)Mq; c.H = (int32_t)H; c.rows = (int32_t)rows;
-      c.by_H = p.by_H;
-      c.by_rows = mla::make_div(rows);
-      c.out_wire = p.out_wire;
-      c.out16 = p.out16;
-      c.out = p.out; c.out_s0 = p.out_s0; c.out_s1 = p.out_s1; c.out_s2 = p.out_s2;
-      c.lse = p.lse; c.lse_s0 = p.lse_s0; c.lse_s1 = p.lse_s1; c.lse_s2 = p.lse_s2;
-      e = mla::launch_combine(c, hs);
-      if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("combine kernel launch: ") + hipGetErrorString(e));
-    }
-    return MLA_OK;
+    return enqueue(planner, p, R, cache_kind(*ckv_pool, *kpe_pool), sel_kind, no_alloc,
+                   reinterpret_cast<hipStream_t>(stream));
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");
   }
 }
 
+// The most half blocks that the rows of a 64-row tile of a window see: the window
+// of its first row and of those after it, and the sinks.
+int64_t window_halves(int64_t Mq, int64_t H, int64_t NB, int64_t window, int64_t n_sink) {
+  if (window == 0) return 2 * NB;
+  const int64_t n_i = std::min<int64_t>(Mq, (64 - 1) / H + 2);  // query rows that 64 rows meet
+  return std::min<int64_t>(2 * NB, (n_sink + 31) / 32 + (window + n_i - 2) / 32 + 2);
+}
+
+mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, const mla_tensor_t* ckv_pool,
+                         const mla_tensor_t* kpe_pool, const mla_tensor_t* block_table,
+                         const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,
+                         const mla_tensor_t* out_lat, const mla_tensor_t* out_lse, const mla_window_opts_t* opts,
+                         void* stream) {
+  auto bad = [](const std::string& m) { return fail(MLA_ERR_INVALID_ARGUMENT, m); };
+  mla_status_t st;
+  if ((st = check_tensor(q_lat, "q_lat", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
+  if ((st = check_tensor(q_pe, "q_pe", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
+  if (!ckv_pool || !kpe_pool) return bad("ckv_pool/kpe_pool: null descriptor");
+  if ((st = check_pool_types(ckv_pool, kpe_pool)) != MLA_OK) return st;
+  if ((st = check_tensor(block_table, "block_table", MLA_DTYPE_INT32, 2)) != MLA_OK) return st;
+  if ((st = check_tensor(seq_lens, "seq_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if (q_lens && (st = check_tensor(q_lens, "q_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if (!opts) return bad("opts: null pointer");
+  for (int i = 0; i < 4; ++i)
+    if (opts->reserved[i]) return bad("opts.reserved must be zero");
+  if (opts->window < 0) return bad("opts.window must be >= 0");
+  if (opts->n_sink < 0) return bad("opts.n_sink must be >= 0");
+  if (opts->n_splits < 0) return bad("opts.n_splits must be >= 0");
+  if (opts->out_format != MLA_OUT_FP32 && opts->out_format != MLA_OUT_BF16_WIRE)
+    return bad("opts.out_format must be MLA_OUT_FP32 or MLA_OUT_BF16_WIRE");
+  const bool wire = opts->out_format == MLA_OUT_BF16_WIRE;
+  if ((st = check_tensor(out_lat, "out_lat", wire ? MLA_DTYPE_BF16 : MLA_DTYPE_FP32, 4)) != MLA_OK) return st;
+  if ((st = check_tensor(out_lse, "out_lse", MLA_DTYPE_FP32, wire ? 4 : 3)) != MLA_OK) return st;
+
+  const int64_t B = block_table->shape[0], NB = block_table->shape[1], P = ckv_pool->shape[0];
+  const int64_t Mq = q_lat->shape[1], H = q_lat->shape[2];
+  if (!shape_is(q_lat, {B, Mq, H, MLA_DLAT})) return bad("q_lat: shape must be [B, Mq, H, 512] with the B of block_table");
+  if (!shape_is(q_pe, {B, Mq, H, MLA_DPE})) return bad("q_pe: shape must be [B, Mq, H, 64]");
+  if ((st = check_pool_shapes(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
+  if (!contiguous(*seq_lens, {B})) return bad("seq_lens: must be contiguous [B]");
+  if (q_lens && !contiguous(*q_lens, {B})) return bad("q_lens: must be contiguous [B]");
+  if (!shape_is(out_lat, {B, Mq, H, MLA_DLAT})) return bad("out_lat: shape must be [B, Mq, H, 512]");
+  if (!wire && !shape_is(out_lse, {B, Mq, H})) return bad("out_lse: shape must be [B, Mq, H]");
+  if (wire && (!shape_is(out_lse, {B, Mq, H, 2}) || out_lse->stride[3] != 1))
+    return bad("out_lse: the wire form takes [B, Mq, H, 2] (m, l) pairs");
+  if ((st = check_pool_layout(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
+  if (!rows_aligned(*q_lat, 2) || !rows_aligned(*q_pe, 2)) return bad("q_lat/q_pe rows must be 16-byte aligned");
+  if (!rows_aligned(*out_lat, wire ? 2 : 4)) return bad("out_lat rows must be 16-byte aligned");
+  if (wire && !pairs_aligned(*out_lse)) return bad("out_lse (m, l) pairs must be 8-byte aligned");
+  if (!rows_apart(*out_lat) || !rows_apart(*out_lse)) return bad("out_lat / out_lse: rows overlap");
+  if (!(std::fabs(scale) <= 18446744073709551616.0f)) return bad("scale must be finite with |scale| <= 2^64");
+  if (B > INT32_MAX || Mq * H > (1 << 24) || NB > (INT32_MAX >> 6) || P > (INT32_MAX >> 1))
+    return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the int32 index range");
+  const Extent outs[2] = {extent(*out_lat), extent(*out_lse)};
+  const bool fp8 = ckv_pool->dtype == MLA_DTYPE_FP8_E4M3FN;
+  auto scales = [&](const float* sc) -> Extent {
+    if (!fp8 || P == 0) return {0, 0};
+    return {(uintptr_t)sc, (uintptr_t)(sc + P)};
+  };
+  const Extent ins[9] = {extent(*q_lat), extent(*q_pe), extent(*ckv_pool), extent(*kpe_pool), extent(*block_table),
+                         extent(*seq_lens), q_lens ? extent(*q_lens) : Extent{0, 0}, scales(ckv_pool->block_scale),
+                         scales(kpe_pool->block_scale)};
+  if (overlaps(outs[0], outs[1])) return bad("out_lat and out_lse overlap");
+  for (const Extent& o : outs)
+    for (const Extent& i : ins)
+      if (overlaps(o, i)) return bad("an output overlaps an input");
+  if (B == 0 || Mq * H == 0) return MLA_OK;
+
+  // splits are cut on the GPU, out of what each tile's rows see; the plan goes by
+  // the most that can be
+  const int64_t K = (window_halves(Mq, H, NB, opts->window, opts->n_sink) + 1) / 2;
+  const mla::Planner planner({B, Mq, H, NB, K, false, false, fp8, opts->n_splits, 64, device_cus(),
+                              ckv_pool->dtype == MLA_DTYPE_MXFP4, mla::kWindowList / 2});
+  mla::PartialParams p = common_params(*q_lat, *q_pe, *ckv_pool, *kpe_pool, *block_table, scale, *out_lat, *out_lse, wire);
+  p.K = (int32_t)K;
+  p.q_jobs = (int32_t)B;
+  p.q_rep = 1;
+  p.win_lens = (const int32_t*)seq_lens->data;
+  p.win_qlens = q_lens ? (const int32_t*)q_lens->data : nullptr;
+  p.window = opts->window;
+  p.n_sink = opts->n_sink;
+  return enqueue(planner, p, B, cache_kind(*ckv_pool, *kpe_pool), mla::kSelWindow, false,
+                 reinterpret_cast<hipStream_t>(stream));
+}
+
 }  // namespace
 
 extern "C" {
+
+mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, const mla_tensor_t* ckv_pool,
+                             const mla_tensor_t* kpe_pool, const mla_tensor_t* block_table,
+                             const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,
+                             const mla_tensor_t* out_lat, const mla_tensor_t* out_lse,
+                             const mla_window_opts_t* opts, void* stream) {
+  try {
+    g_last_error.clear();
+    return window_call(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, scale, out_lat, out_lse, opts,
+                       stream);
+  } catch (...) {
+    return fail(MLA_ERR_HIP, "internal error");
+  }
+}
 
 const char* mla_last_error(void) { return g_last_error.c_str(); }
 

@@ -95,6 +95,11 @@ struct PartialParams {
   float* ws_scale;   // [R][S][rows]
   float* ws_lse;     // [R][S][rows]
   float* ws_max;     // [R][S][rows], the split's largest score (log2 units; wire form)
+  // windows: tokens of each request's sequence, query rows it has (null: Mq),
+  // tokens a row sees up to its own (0: all) and first tokens it always sees
+  const int32_t* win_lens;
+  const int32_t* win_qlens;
+  int32_t window, n_sink;
 };
 
 // Combine of the S split partials of every job into the caller's outputs.
@@ -209,6 +214,7 @@ hipError_t launch_append(const AppendParams& p, hipStream_t s);
 constexpr int kKvBf16 = 0;
 constexpr int kKvFp8Shared = 1;  // e4m3, one scale per block for ckv and kpe
 constexpr int kKvFp8Split = 2;   // e4m3, separate ckv and kpe scales per block
+constexpr int kKvMx4 = 3;        // 4-bit latent rows of kMx4Row bytes, bf16 RoPE rows
 
 // Per-row selections: the LDS counters of one workgroup's compaction live in
 // its stage area, NB * (query rows of the tile) 16-bit counters.
@@ -234,6 +240,11 @@ __host__ __device__ constexpr int ask_place(int stage) { return (stage & 1) * kA
 constexpr int kSelShared = 0;
 constexpr int kSelPerRow = 1;
 constexpr int kSelTokens = 2;
+// No selection: each query row sees the last tokens of its request's sequence,
+// and its first ones.
+constexpr int kSelWindow = 3;
+// half blocks that one split of a window lists
+constexpr int kWindowList = kPerRowListShort;
 
 // Launchers; return hipSuccess or the launch error.
 // row_groups: 2 (row tiles of 128 rows) or 1 (row tiles of 64 rows)

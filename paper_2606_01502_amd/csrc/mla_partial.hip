@@ -59,6 +59,7 @@
 #include <type_traits>
 
 #include "mla_kernels.h"
+#include "mla_mx4.h"
 
 namespace mla {
 namespace {
@@ -1440,8 +1441,10 @@ void partial_kernel(const PartialParams p) {
 // 36 KiB, fp8 six of 18 KiB of codes), the block list with its fp8 factors and
 // row masks, two buffers of weights P (4 KiB each) and the waves' exchange
 // area.  The query rows pass through the stages after the first two before any
-// tokens do (72 KiB).
-template <bool FP8, bool PR>
+// tokens do (72 KiB).  4-bit caches: the ring holds latent rows only, three
+// stages of 32 KiB of converted bf16, and a second ring four stages as they come
+// from memory: 8 KiB of codes, 512 bytes of exponents, 4 KiB of RoPE rows.
+template <bool FP8, bool PR, bool MX4 = false, bool WIN = false>
 struct Tile {
   static constexpr bool kFp8 = FP8;
   static constexpr int kThreads = 512;
@@ -1450,18 +1453,27 @@ struct Tile {
   static constexpr int kRopeRow = kDPe * kElt;               // RoPE row
   static constexpr int kTok = 32;                            // tokens of a stage
   static constexpr int kStageCkv = kTok * kRow;
-  static constexpr int kStage = kStageCkv + kTok * kRopeRow;
-  static constexpr int kNum = FP8 ? 6 : 4;
-  static constexpr int kLoads = FP8 ? 3 : 5;  // direct-to-LDS loads per wave per stage
-  static constexpr int kQ = 2 * kStage;       // the query rows' place: 64 rows of 1 KiB, then of 128 B
-  static constexpr int kCap = PR ? kPerRowListShort : kMaxSlotsPerSplit;
+  static constexpr int kStage = kStageCkv + (MX4 ? 0 : kTok * kRopeRow);
+  static constexpr int kNum = MX4 ? 3 : FP8 ? 6 : 4;
+  static constexpr int kLoads = FP8 || MX4 ? 3 : 5;  // direct-to-LDS loads per wave per stage
+  // the ring that the loads go to, its stages, and where a stage's RoPE rows lie in it
+  static constexpr int kIn = MX4 ? kNum * kStage : 0;
+  static constexpr int kInCodes = kTok * kDLat / 2, kInRope = MX4 ? kInCodes + kTok * 16 : kStageCkv;
+  static constexpr int kInStage = MX4 ? kInRope + kTok * kRopeRow : kStage;
+  static constexpr int kInNum = MX4 ? 4 : kNum;
+  // the stage that step i loads is i + kLead
+  static constexpr int kLead = MX4 ? kInNum : kNum - 1;
+  // the query rows' place: 64 rows of 1 KiB, then of 128 B
+  static constexpr int kQ = MX4 ? 0 : 2 * kStage;
+  static constexpr int kCap = PR || WIN ? kPerRowListShort : kMaxSlotsPerSplit;
   // per-row selections: the compaction's counters take up to kPerRowCounterBytes
   // from the start; what it writes lies past them (fp8: the rest in between)
-  static constexpr int kRing = kNum * kStage;
+  static constexpr int kRing = kNum * kStage + (MX4 ? kInNum * kInStage : 0);
   static constexpr int kList = PR ? (kPerRowCounterBytes + 255) / 256 * 256 : kRing;
   static constexpr int kScales = kList + kCap * 4;
   static constexpr int kMasks = kScales + (FP8 ? kCap * 12 : 0);
-  static constexpr int kWaveCnt = kMasks + (PR ? kCap * 8 : 0);
+  // (windows: the first token of each entry in the masks' place)
+  static constexpr int kWaveCnt = kMasks + (PR ? kCap * 8 : WIN ? kCap * 4 : 0);
   static constexpr int kP = FP8 && PR ? kRing : kWaveCnt + 256;
   static constexpr int kX = kP + 8192;       // row maxima [64 rows][2 token groups]
   static constexpr int kAsk = kX + 512;      // requests to raise a maximum, see ask_place
@@ -1471,6 +1483,12 @@ struct Tile {
 static_assert(Tile<false, true>::kTotal <= 160 * 1024 && Tile<true, true>::kTotal <= 160 * 1024 &&
                   Tile<true, false>::kTotal <= 160 * 1024 && Tile<false, false>::kTotal <= 160 * 1024,
               "LDS budget");
+static_assert(Tile<false, false, true>::kTotal <= 160 * 1024 && Tile<false, false, true, true>::kTotal <= 160 * 1024 &&
+                  Tile<false, false, false, true>::kTotal <= 160 * 1024 && Tile<true, false, false, true>::kTotal <= 160 * 1024,
+              "LDS budget");
+static_assert(Tile<false, false, true>::kIn >= 65536 + 8192, "the query rows fit the stages of converted rows");
+static_assert(Tile<false, false, false, true>::kCap == kWindowList && Tile<false, false, true, true>::kCap == kWindowList &&
+                  Tile<true, false, false, true>::kCap == kWindowList, "a window's list");
 static_assert(Tile<true, false>::kQ + 65536 + 8192 <= Tile<true, false>::kRing &&
                   Tile<false, false>::kQ + 65536 + 8192 <= Tile<false, false>::kRing,
               "the query rows fit the stages after the first");
@@ -1562,6 +1580,81 @@ __device__ __forceinline__ float xor32_max(float v) {
   const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
+// Windows (kSelWindow): the tokens that a tile's query rows see, as half blocks.
+// Row i of request r sits at position pos = len - qn + i of its sequence and sees
+// the tokens t <= pos with t > pos - window or t < n_sink.
+struct Window {
+  int n_tok;            // tokens the sequence's table holds
+  int hi_row, lo_row;   // of the lane's row: the last token it sees, the first in its window
+  int hi_all, lo_all;   // every row sees lo_all .. hi_all
+  int n_sink;
+};
+
+// The half blocks of split s (of S) that any row of query rows i0 .. i0 + n_i - 1
+// sees, in order: pool half blocks into list, their first tokens into first.  Those
+// whose table entry names no pool block are left out.  Returns their number.
+template <class L>
+__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int i0, int n_i, int i_lane,
+                                              Window& w, LDS uint8_t* smem, int tid) {
+  constexpr bool FP8 = L::kFp8;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  LDS int* list = (LDS int*)(smem + L::kList);
+  LDS int* first = (LDS int*)(smem + L::kMasks);
+  LDS float* scales = (LDS float*)(smem + L::kScales);
+  LDS int* wave_cnt = (LDS int*)(smem + L::kWaveCnt);
+  const int len = max(p.win_lens[r], 0);
+  const int qn = p.win_qlens ? min(max(p.win_qlens[r], 0), p.Mq) : p.Mq;
+  w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
+  w.n_sink = p.window ? p.n_sink : 0;
+  const int pos0 = len - qn;  // of query row 0
+  // (window 0: all tokens up to the row's own)
+  auto lo_of = [&](int pos) { return p.window ? (int)max((int64_t)pos - p.window + 1, (int64_t)0) : 0; };
+  auto hi_of = [&](int pos) { return min(pos, w.n_tok - 1); };
+  const bool on = i_lane < qn;
+  w.hi_row = on ? hi_of(pos0 + i_lane) : -1;
+  w.lo_row = lo_of(pos0 + i_lane);
+  const int i1 = i0 + n_i - 1, live = min(i1, qn - 1);  // the tile's last row, the last with a query
+  w.hi_all = i1 < qn ? hi_of(pos0 + i0) : -1;
+  w.lo_all = lo_of(pos0 + i1);
+  const int hi = live >= i0 ? hi_of(pos0 + live) : -1, lo = lo_of(pos0 + i0);
+  if (hi < 0) return 0;
+  const int b_lo = min(lo, hi) >> 5, b_hi = hi >> 5;
+  const int sinks = min((int)min(((int64_t)w.n_sink + 31) >> 5, (int64_t)b_lo), b_hi + 1);
+  const int n_all = sinks + b_hi - b_lo + 1;
+  const int e0 = (int)((int64_t)n_all * s / p.n_splits), e1 = (int)((int64_t)n_all * (s + 1) / p.n_splits);
+  const int n_e = min(e1 - e0, L::kCap);
+  int n_valid = 0;
+  for (int base = 0; base < n_e; base += L::kThreads) {
+    const int e = e0 + base + tid;
+    int b = -1, h = 0;
+    if (base + tid < n_e) {
+      h = e < sinks ? e : b_lo + (e - sinks);
+      const int bb = p.table[r * p.table_s0 + (h >> 1)];
+      if (bb >= 0 && bb < p.P) b = bb;
+    }
+    const uint64_t m = __ballot(b >= 0);
+    const int before = __popcll(m & ((1ull << lane) - 1ull));
+    if (lane == 0) wave_cnt[wave] = __popcll(m);
+    lds_barrier();
+    int off = n_valid, total = 0;
+#pragma unroll
+    for (int k = 0; k < L::kThreads / 64; ++k) {
+      const int c = wave_cnt[k];
+      off += (k < wave) ? c : 0;
+      total += c;
+    }
+    if (b >= 0) {
+      list[off + before] = 2 * b + (h & 1);
+      first[off + before] = h << 5;
+      if constexpr (FP8) put_fp8_factors(scales, off + before, p.ckv_scale[b], p.kpe_scale[b]);
+    }
+    n_valid += total;
+    lds_barrier();
+  }
+  return n_valid;
+}
+
 // Swizzles of a 64-row tile's stages (16-byte chunk c of latent row t in slot
 // c ^ key32(t), of RoPE row t in slot c ^ rope_key32(t)).  A key read takes
 // chunk 4 i + g of token 16 th + n for lane (n, g); the LDS serves 16 lanes of
@@ -1581,67 +1674,94 @@ __device__ __forceinline__ int rope_key32(int t) {
 }
 
 // The direct-to-LDS loads of a stage: 32 tokens, half h & 1 of listed block
-// h >> 1 (or 32 listed tokens).
+// h >> 1 (or 32 listed tokens; windows list half blocks).
 //   bf16: load j < 4 of wave w is latent row 4w + j (lane -> slot lane); load 4
 //         is RoPE rows 4w + (lane >> 3), slot lane & 7, by 32 lanes.
 //   fp8:  load j < 2 of wave w is latent rows 4w + 2j + (lane >> 5), slot
 //         lane & 31; load 2 is RoPE rows 4w + (lane >> 2), slot lane & 3, by 16
 //         lanes.
+//   4 bits: load 0 is the codes of rows 4w + (lane >> 4), 16 bytes a lane, load 1
+//         their exponents, a row by each of 4 lanes; load 2 the RoPE rows as bf16.
 // The latent loads of a wave share M0 and the scalar base: the instruction's
 // offset moves both the source and the place in LDS.  The lane's offset
 // differs between them by an XOR (the key of the row's low bits), held for each.
-template <bool FP8, bool TOK>
+// Windows: rows behind the sequence's last token may hold anything, a NaN among
+// it, which a weight of 0 does not take away; the last row there is stands in
+// for them.
+template <bool FP8, bool TOK, bool MX4 = false, bool WIN = false>
 struct Issue32 {
-  using L = Tile<FP8, false>;
+  using L = Tile<FP8, false, MX4, WIN>;
+  static constexpr int kSrcRow = MX4 ? kMx4Row : L::kRow;  // of a latent row in memory
   static constexpr int kLat = L::kLoads - 1;
   // (token selections, where registers are short, hold the first latent load's
   // offset only, the others being one XOR away, and fp8 ones the wave's part of
   // the RoPE load's)
   static constexpr int kHeld = TOK ? 1 : kLat;
   uint32_t lat[kHeld], rope;
-  const uint8_t* ckv;  // the wave's first row
+  const uint8_t* ckv;  // the wave's first row (windows: the half block's)
   const uint8_t* kpe;
   uint32_t lds_lat, lds_rope;  // LDS addresses of the wave's first rows
   // TOK: pool tokens of stage token 4w + (lane & 3) and (fp8) of the RoPE load's row
   int tok, tok_rope;
+  int last;  // WIN: the stage's last row that the sequence holds
 
   __device__ __forceinline__ Issue32(const PartialParams& p, int wave, int lane) {
     ckv = p.ckv;
     kpe = p.kpe;
     lds_lat = lds_rope = 0;
     tok = tok_rope = 0;
+    last = 31;
     const int b3 = (wave >> 1) & 1;           // bit 3 of the wave's rows
     const int kw = (b3 << 1) | (wave >> 2);   // their key32, less the low bits' part
     const int hi = lane >> 5;
+    if constexpr (MX4) {
+      lat[0] = (uint32_t)((WIN ? 0 : (lane >> 4) * kMx4Row) + ((lane & 15) << 4));
+      lat[1] = (uint32_t)(WIN ? 0 : lane * kMx4Row) + kDLat / 2;
+    } else {
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      lat[k] = FP8 ? (uint32_t)(hi * 512 + (((lane & 31) ^ (hi << 2) ^ kw ^ (k << 3)) << 4))
-                   : (uint32_t)((lane ^ kw ^ (k << 2)) << 4);
+      for (int k = 0; k < kHeld; ++k)
+        lat[k] = FP8 ? (uint32_t)((WIN ? 0 : hi * 512) + (((lane & 31) ^ (hi << 2) ^ kw ^ (k << 3)) << 4))
+                     : (uint32_t)((lane ^ kw ^ (k << 2)) << 4);
+    }
     rope = FP8 && TOK ? (uint32_t)(b3 << 5)
-         : FP8 ? (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (b3 << 1)) << 4))
-               : (uint32_t)((lane >> 3) * 128 + (((lane & 7) ^ ((((lane >> 4) & 1) << 1) | (b3 << 2))) << 4));
+         : FP8 ? (uint32_t)((WIN ? 0 : (lane >> 2) * 64) + (((lane & 3) ^ (b3 << 1)) << 4))
+               : (uint32_t)((WIN ? 0 : (lane >> 3) * 128) +
+                            (((lane & 7) ^ ((((lane >> 4) & 1) << 1) | (b3 << 2))) << 4));
   }
   // what aim() needs of the list for half block h, read ahead of it
   __device__ __forceinline__ void look(const LDS int* list, int h, int wave, int lane, int (&e)[2]) const {
-    e[0] = TOK ? list[h * 32 + 4 * wave + (lane & 3)] : list[h >> 1];
+    e[0] = TOK ? list[h * 32 + 4 * wave + (lane & 3)] : WIN ? list[h] : list[h >> 1];
     if constexpr (TOK && FP8) e[1] = list[h * 32 + 4 * wave + ((lane >> 2) & 3)];
+    // (the entries' first tokens lie past the list and the fp8 factors)
+    if constexpr (WIN) e[1] = list[h + (L::kMasks - L::kList) / 4];
   }
-  // points the loads at half block h and stage buf
-  __device__ __forceinline__ void aim(const PartialParams& p, const int (&e)[2], int h, uint32_t buf, int wave) {
+  // points the loads at half block h and stage buf; n_tok: the sequence's tokens (windows)
+  __device__ __forceinline__ void aim(const PartialParams& p, const int (&e)[2], int h, uint32_t buf, int wave, int n_tok) {
     if constexpr (TOK) {
       tok = e[0];
       tok_rope = e[1];
+    } else if constexpr (WIN) {
+      const int64_t b = __builtin_amdgcn_readfirstlane(e[0]);
+      ckv = p.ckv + b * (32 * kSrcRow);
+      kpe = p.kpe + b * (32 * L::kRopeRow);
+      last = min(31, n_tok - 1 - __builtin_amdgcn_readfirstlane(e[1]));
     } else {
       const int64_t b = (int64_t)__builtin_amdgcn_readfirstlane(e[0]) * 2 + (h & 1);
-      ckv = p.ckv + b * L::kStageCkv + wave * (4 * L::kRow);
+      ckv = p.ckv + b * (32 * kSrcRow) + wave * (4 * kSrcRow);
       kpe = p.kpe + b * (32 * L::kRopeRow) + wave * (4 * L::kRopeRow);
     }
-    lds_lat = __builtin_amdgcn_readfirstlane(buf + (uint32_t)wave * (4 * L::kRow));
-    lds_rope = __builtin_amdgcn_readfirstlane(buf + (uint32_t)L::kStageCkv + (uint32_t)wave * (4 * L::kRopeRow));
+    lds_lat = __builtin_amdgcn_readfirstlane(buf + (uint32_t)wave * (MX4 ? 4 * kDLat / 2 : 4 * L::kRow));
+    lds_rope = __builtin_amdgcn_readfirstlane(buf + (uint32_t)L::kInRope + (uint32_t)wave * (4 * L::kRopeRow));
   }
   __device__ __forceinline__ static void go(uint32_t off, const uint8_t* base, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                  :: "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+  }
+  // by the first lanes only
+  __device__ __forceinline__ static void go_lanes(uint32_t off, const uint8_t* base, uint32_t lds, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
+                 :: "v"(off), "s"(uniform(base)), "s"(__builtin_amdgcn_readfirstlane(lds)), "s"(lanes)
+                 : "memory", "m0");
   }
   __device__ __forceinline__ static void go64(const uint8_t* a, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
@@ -1650,9 +1770,27 @@ struct Issue32 {
   __device__ __forceinline__ uint32_t lat_of(int j) const {
     return (uint32_t)lds_opaque((int)lat[0]) ^ (uint32_t)(j << (FP8 ? 7 : 6));
   }
+  // WIN: the byte offset of the stage's row r, or of the last there is
+  __device__ __forceinline__ uint32_t row_off(int r, uint32_t bytes) const { return (uint32_t)min(r, last) * bytes; }
   // Load j; every lane of the wave is active where this is called.
-  __device__ __forceinline__ void load(const PartialParams& p, int j, int lane) const {
-    if (j < kLat) {
+  __device__ __forceinline__ void load(const PartialParams& p, int j, int wave, int lane) const {
+    if constexpr (WIN) {
+      const int l = lds_opaque(lane);  // (row offsets are formed here, not held)
+      if (j == kLat) {
+        constexpr int kPer = L::kRopeRow / 16;  // lanes a RoPE row
+        go_lanes(rope + row_off(4 * wave + l / kPer, L::kRopeRow), kpe, lds_rope, (1ull << (4 * kPer)) - 1);
+      } else if constexpr (MX4) {
+        if (j == 0) go(lat[0] + row_off(4 * wave + (l >> 4), kMx4Row), ckv, lds_lat);
+        else go_lanes(lat[1] + row_off(4 * wave + l, kMx4Row), ckv, lds_exp(wave), 15);
+      } else {
+        const int r = FP8 ? 4 * wave + 2 * j + (l >> 5) : 4 * wave + j;
+        go(lat[j] + row_off(r, L::kRow), ckv, lds_lat + (uint32_t)j * 1024u);
+      }
+    } else if constexpr (MX4) {
+      if (j == 0) go(lat[0], ckv, lds_lat);
+      else if (j == 1) go_lanes(lat[1], ckv, lds_exp(wave), 15);
+      else go_lanes(rope, kpe, lds_rope, 0xffffffffull);
+    } else if (j < kLat) {
       if constexpr (!TOK) {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3"
                      :: "v"(lat[j]), "s"(uniform(ckv)), "s"(__builtin_amdgcn_readfirstlane(lds_lat)), "i"(j * 1024)
@@ -1668,9 +1806,7 @@ struct Issue32 {
       // the first 32 (fp8: 16) lanes only
       constexpr uint64_t kLanes = FP8 ? 0xffffull : 0xffffffffull;
       if constexpr (!TOK) {
-        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
-                     :: "v"(rope), "s"(uniform(kpe)), "s"(__builtin_amdgcn_readfirstlane(lds_rope)), "s"(kLanes)
-                     : "memory", "m0");
+        go_lanes(rope, kpe, lds_rope, kLanes);
       } else {
         const uint32_t t = (uint32_t)(FP8 ? tok_rope : __shfl(tok, (lane >> 3) & 3));
         const uint32_t o = FP8 ? rope ^ ((uint32_t)(lds_opaque(lane) & 3) << 4) : rope & 0x70u;
@@ -1680,17 +1816,23 @@ struct Issue32 {
       }
     }
   }
+  // MX4: the place of the wave's exponents, behind the stage's codes
+  __device__ __forceinline__ uint32_t lds_exp(int wave) const {
+    return lds_lat + (uint32_t)(L::kInCodes - wave * (4 * kDLat / 2) + wave * 64);
+  }
 };
 
 template <int KV, int SEL, int NK>  // NK: row halves of 32 rows
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void tile64_kernel(const PartialParams p) {
-  constexpr bool FP8 = KV != kKvBf16;
+  constexpr bool FP8 = KV == kKvFp8Shared || KV == kKvFp8Split;
+  constexpr bool MX4 = KV == kKvMx4;
   constexpr bool PR = SEL == kSelPerRow;
   constexpr bool TOK = SEL == kSelTokens;
+  constexpr bool WIN = SEL == kSelWindow;
   constexpr bool kSplitScales = KV == kKvFp8Split;
-  using L = Tile<FP8, PR>;
-  __shared__ __attribute__((aligned(16))) uint8_t smem_raw[L::kTotal];
+  using L = Tile<FP8, PR, MX4, WIN>;
+  __shared__ __attribute__((aligned(MX4 ? 1024 : 16))) uint8_t smem_raw[L::kTotal];
   LDS uint8_t* smem = (LDS uint8_t*)smem_raw;
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
 
@@ -1735,7 +1877,7 @@ void tile64_kernel(const PartialParams p) {
   auto asks = [&](int stage) { return smem + L::kAsk + ask_place(stage); };
   const int row_wg0 = rt * 64;
   const int i0 = div_by(row_wg0, p.by_H);
-  const int n_i = PR ? div_by(min(row_wg0 + 64, p.rows) - 1, p.by_H) - i0 + 1 : 1;
+  const int n_i = PR || WIN ? div_by(min(row_wg0 + 64, p.rows) - 1, p.by_H) - i0 + 1 : 1;
   const int c_slot0 = PR && p.split_by_id ? 0 : slot0;
   const int c_nslots = PR && p.split_by_id ? p.K : nslots;
   int first_id = -1;
@@ -1744,7 +1886,7 @@ void tile64_kernel(const PartialParams p) {
       const int ii = p.split_by_id ? div_by(tid, p.by_K) : tid / c_nslots, j = tid - ii * c_nslots;
       first_id = p.sel[r * p.sel_s0 + (int64_t)(i0 + ii) * p.sel_s1 + c_slot0 + j];
     }
-  } else {
+  } else if constexpr (!WIN) {
     if (tid < nslots) first_id = p.sel[r * p.sel_s0 + slot0 + tid];
   }
 
@@ -1787,7 +1929,10 @@ void tile64_kernel(const PartialParams p) {
 
   int n_valid;
   int n_tok = 0;
-  if constexpr (PR) {
+  Window win{};
+  if constexpr (WIN) {
+    n_valid = compact_window<L>(p, r, s_idx, i0, n_i, div_by(row_wg0 + 16 * rq + n16, p.by_H), win, smem, tid);
+  } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                  p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
                                  masks, tid);
@@ -1798,23 +1943,32 @@ void tile64_kernel(const PartialParams p) {
     n_valid = compact_slots<L>(p, r, slot0, nslots, first_id, smem, tid);
   }
   if (!q_early) issue_q();
-  const int n = TOK ? (n_tok + 31) / 32 : 2 * n_valid;  // stages of tokens
+  const int n = TOK ? (n_tok + 31) / 32 : WIN ? n_valid : 2 * n_valid;  // stages of tokens
 
-  Issue32<FP8, TOK> is(p, wave, lane);
+  Issue32<FP8, TOK, MX4, WIN> is(p, wave, lane);
   int ahead[2] = {0, 0};  // the list entries of the stage to load next
-  auto aim = [&](int h) { is.aim(p, ahead, h, lds0 + (uint32_t)((h % L::kNum) * L::kStage), wave); };
+  auto aim = [&](int h) {
+    is.aim(p, ahead, h, lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage), wave, win.n_tok);
+  };
   auto issue = [&](int h) {
     if (h >= n) return;
     is.look(list, h, wave, lane, ahead);
     aim(h);
 #pragma unroll
-    for (int j = 0; j < L::kLoads; ++j) is.load(p, j, lane);
+    for (int j = 0; j < L::kLoads; ++j) is.load(p, j, wave, lane);
   };
   issue(0);
   issue(1);
-  // the query rows have landed
-  if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
-  else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  if constexpr (MX4) issue(2);
+  // the query rows have landed (4 bits: and stage 0, which is converted here)
+  if constexpr (MX4) {
+    if (n > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
+    else if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(L::kLoads));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  } else {
+    if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  }
   lds_barrier();
   // This wave's query rows as MFMA B operands, held for the whole kernel: steps
   // 0, 1 RoPE, 2 .. 17 latent, 32 dims each.  bf16: lane group g takes the
@@ -1831,6 +1985,45 @@ void tile64_kernel(const PartialParams p) {
     for (int ks = 0; ks < 2; ++ks) qb[ks] = lds_b128(qp + ((chunk(ks) ^ rope_key32<false>(t)) << 4));
 #pragma unroll
     for (int ks = 0; ks < 16; ++ks) qb[2 + ks] = lds_b128(qr + ((chunk(ks) ^ key32(t)) << 4));
+  }
+  // 4-bit caches: a wave converts the rows it loaded itself, 4 a stage, a lane 32
+  // columns of row 4 wave + (lane >> 4): one group, 4 chunks of 16 bytes.  Lanes of
+  // one LDS pass write the chunks of their groups in orders of their own (XOR
+  // r), so that these fall to different banks: with one order for all, four
+  // groups of a row meet on one.
+  // (The addresses are formed where they are used: registers are short.)
+  u32x4_t cv_codes{};
+  float cv_scale = 0.f;
+  uint32_t cv_put = 0;
+  auto cv_read = [&](int h) {
+    const int l = lds_opaque(lane);
+    const uint32_t a = lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage);
+    cv_codes = *(const LDS u32x4_t*)(uintptr_t)(a + (uint32_t)(wave * 1024 + l * 16));
+    cv_scale = mx4_scale(*(const LDS uint8_t*)(uintptr_t)(a + (uint32_t)(L::kInCodes + wave * 64 + l)));
+  };
+  // codes of chunk j ^ r to place j, and the place of chunk r: chunk 4 g + k of
+  // row t goes to slot (4 g + k) ^ key32(t)
+  auto cv_turn = [&](int h) {
+    const int l = lds_opaque(lane), x = l >> 4, g = l & 15, r = (g >> 2) ^ (x & 1);
+    u32x4_t c = cv_codes;
+    c = r & 1 ? u32x4_t{c[1], c[0], c[3], c[2]} : c;
+    c = r & 2 ? u32x4_t{c[2], c[3], c[0], c[1]} : c;
+    cv_codes = c;
+    const int kw = ((wave >> 1) & 1) << 1 | (wave >> 2);  // key32 less the low bits' part
+    cv_put = lds0 + (uint32_t)((h % L::kNum) * L::kStage + (4 * wave + x) * 1024 + ((g ^ x) << 6) + ((r ^ kw) << 4));
+  };
+  // (stages lie on whole kilobytes: bits 4 and 5 are the chunk's)
+  auto cv_write = [&](int j) {
+    *(LDS u32x4_t*)(uintptr_t)(cv_put ^ (uint32_t)(j << 4)) = mx4x8_bf16(cv_codes[j], cv_scale);
+  };
+  if constexpr (MX4) {
+    lds_barrier();  // every wave holds its query rows: their place takes tokens
+    if (n > 0) {
+      cv_read(0);
+      cv_turn(0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) cv_write(j);
+    }
   }
   if constexpr (L::kNum > 4) {
     lds_barrier();  // every wave holds its query rows: their place takes tokens
@@ -1868,7 +2061,7 @@ void tile64_kernel(const PartialParams p) {
     for (int i = 0; i < 4; ++i) k_off[i] = lds0 + (uint32_t)(t * L::kRow + (((4 * i + g) ^ key32(t)) << 4));
 #pragma unroll
     for (int i = 0; i < kRopeReads; ++i)
-      r_off[i] = lds0 + (uint32_t)(L::kStageCkv + t * L::kRopeRow + (((4 * i + g) ^ rope_key32<FP8>(t)) << 4));
+      r_off[i] = lds0 + (uint32_t)(L::kIn + L::kInRope + t * L::kRopeRow + (((4 * i + g) ^ rope_key32<FP8>(t)) << 4));
     // the value fragment of column tile d and 16 tokens kk.  bf16: two
     // transposing reads of 4 tokens x 16 columns per 16 lanes (lane i of group
     // q: tokens 8 (q >> 1) + (i >> 2) and 4 on, columns 16 (q & 1) + 4 (i & 3));
@@ -1908,6 +2101,7 @@ void tile64_kernel(const PartialParams p) {
   int x_stage = 0;
   float s_main = 1.f, s_ratio = 1.f, s_value = 1.f;  // fp8, of the stage whose scores are formed
   uint64_t s_mask = ~0ull;                            // per-row selections: its row mask
+  int s_first = 0;                                    // windows: its first token
   LDS const float* const tok_scales = (LDS const float*)(smem + L::kScales);
   // (element k of a lane's tile is token 16 th + 4 g + k of the stage)
   auto tok_scale4 = [&](int which, int h) -> f32x4_t {
@@ -1917,9 +2111,12 @@ void tile64_kernel(const PartialParams p) {
   auto put_p = [&]() {
     if (!act) return;
     f32x4_t e;
+    // (windows: a score of -inf weighs 0 also before the row's first token, while
+    // the maximum is -inf as well)
+    const float m_here = WIN ? fmaxf(m_run, -3.4e38f) : m_run;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      e[k] = __builtin_amdgcn_exp2f(x[k] - m_run);
+      e[k] = __builtin_amdgcn_exp2f(x[k] - m_here);
       if constexpr (PR) e[k] = on ? e[k] : 0.f;
     }
     psum = (e[0] + e[1]) + (e[2] + e[3]);
@@ -1955,6 +2152,16 @@ void tile64_kernel(const PartialParams p) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (4 * g + k >= n_here) s[k] = -INFINITY;
+      }
+    }
+    if constexpr (WIN) {
+      // stages that every row sees whole, most of a long window, go unmasked
+      const int t0 = __builtin_amdgcn_readfirstlane(s_first);
+      if (t0 + 31 > win.hi_all || (t0 < win.lo_all && t0 + 31 >= win.n_sink)) {
+        const int t = t0 + 16 * th + 4 * g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (t + k > win.hi_row || (t + k < win.lo_row && t + k >= win.n_sink)) s[k] = -INFINITY;
       }
     }
     return s;
@@ -2028,6 +2235,13 @@ void tile64_kernel(const PartialParams p) {
   // waits until stage i + 1's loads of this wave have landed (the next
   // kNum - 3 stages' may be in flight) and meets the other waves
   auto meet = [&](int i) {
+    if constexpr (MX4) {
+      // (4 bits: stage i + 2's, which step i converts; stage i + 3's may be in flight)
+      if (n - 3 - i >= 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(L::kLoads));
+      else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+      lds_barrier();
+      return;
+    }
     constexpr int kMore = L::kNum - 3;
     if (kMore >= 3 && n - 2 - i >= 3) __builtin_amdgcn_s_waitcnt(waitcnt_vm(3 * L::kLoads));
     else if (kMore >= 2 && n - 2 - i >= 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
@@ -2041,15 +2255,18 @@ void tile64_kernel(const PartialParams p) {
   // key reads in flight ahead of their products (fewer where the tokens' rows
   // take registers: a spilled query fragment would be read back in every stage,
   // with a wait for all loads in flight)
-  constexpr int kAhead = TOK && NK == 2 ? (FP8 ? (kSplitScales ? 2 : 3) : 5) : FP8 ? 3 : 6;
+  constexpr int kAhead = NK == 2 && TOK ? (FP8 ? (kSplitScales ? 2 : 3) : 5)
+                       : NK == 2 && WIN ? (MX4 ? 3 : FP8 ? (kSplitScales ? 2 : 3) : 5)
+                       : NK == 2 && MX4 ? 4 : FP8 ? 3 : 6;
   auto scores = [&](int i, auto mid) -> u32x2_t {
     constexpr bool kMid = decltype(mid)::value;
     const uint32_t st = (uint32_t)(((i + 1) % L::kNum) * L::kStage);
-    const int ih = i - 1 + L::kNum;  // the stage to load
+    const uint32_t st_in = MX4 ? (uint32_t)(((i + 1) % L::kInNum) * L::kInStage) : st;
+    const int ih = i + L::kLead;  // the stage to load
     bf16x8_t kr[kAhead + 1];
     bf16x8_t ka[4];  // fp8: converted ahead of their products
     auto key_read = [&](int j) {
-      if (j < kRopeReads) kr[j % (kAhead + 1)] = lds_b128(lds_at(r_off[j] + st));
+      if (j < kRopeReads) kr[j % (kAhead + 1)] = lds_b128(lds_at(r_off[j] + st_in));
       else kr[j % (kAhead + 1)] = lds_b128(lds_at(k_off[(j - kRopeReads) & 3] + st) + ((j - kRopeReads) >> 2) * 256);
     };
     auto half_of = [&](int j, int e) -> bf16x8_t {  // fp8: codes 8 e .. 8 e + 7 of read j
@@ -2099,16 +2316,25 @@ void tile64_kernel(const PartialParams p) {
             if (step + kAhead < kReads) key_read(step + kAhead);
           }
         }
-        if (kLd && step % 3 == 1 && step / 3 < L::kLoads) is.load(p, step / 3, lane);
+        if (kLd && step % 3 == 1 && step / 3 < L::kLoads) is.load(p, step / 3, wave, lane);
+        if constexpr (MX4) {
+          // stage i + 2 to bf16, for the scores of the next step
+          if (i + 2 < n) {
+            if (step == 2) cv_read(i + 2);
+            if (step == 6) cv_turn(i + 2);
+            if (step >= 7 && step <= 13 && (step & 1)) cv_write((step - 7) >> 1);
+          }
+        }
         // what the softmax and the value products of this step need
         if (step == 3) {
           if constexpr (FP8 && !TOK) {
-            const int b = (i + 1) >> 1;
+            const int b = WIN ? i + 1 : (i + 1) >> 1;
             s_value = scales[3 * b];
             s_main = scales[3 * b + 1];
             if constexpr (kSplitScales) s_ratio = scales[3 * b + 2];
           }
           if constexpr (PR) s_mask = masks[(i + 1) >> 1];
+          if constexpr (WIN) s_first = ((LDS const int*)(smem + L::kMasks))[i + 1];
         }
         // (tokens: after the stage's last load, which reads the same register)
         if (step == (TOK ? 15 : 5)) is.look(list, ih + 1, wave, lane, ahead);
@@ -2206,7 +2432,7 @@ void tile64_kernel(const PartialParams p) {
   };
 
   if (n > 0) {
-    is.look(list, L::kNum - 2, wave, lane, ahead);
+    is.look(list, L::kLead - 1, wave, lane, ahead);
     meet(-1);
     (void)scores(-1, std::false_type{});
     soft(0, 0);
@@ -2422,6 +2648,15 @@ static void launch_items(Kernel kernel, PartialParams p, int items, int threads,
   }
 }
 
+// 64-row tiles only: windows and 4-bit caches
+template <int KV, int SEL>
+static void launch_tile64(const PartialParams& p, int grid, hipStream_t s) {
+  if (p.rows <= 32)
+    launch_items(tile64_kernel<KV, SEL, 1>, p, grid, 512, s);
+  else
+    launch_items(tile64_kernel<KV, SEL, 2>, p, grid, 512, s);
+}
+
 template <int KV, int SEL = kSelShared>
 static void launch_kv(const PartialParams& p, int grid, int row_groups, hipStream_t s) {
   if (row_groups == 2) return launch_items(partial_kernel<2, KV, SEL>, p, grid, 256, s);
@@ -2438,7 +2673,18 @@ hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups,
                           hipStream_t s) {
   const int grid = R * p.row_tiles * p.n_splits;
   if (grid <= 0) return hipSuccess;
-  if (sel_kind == kSelPerRow) {
+  if (sel_kind == kSelWindow) {
+    if (kv == kKvMx4)
+      launch_tile64<kKvMx4, kSelWindow>(p, grid, s);
+    else if (kv == kKvFp8Shared)
+      launch_tile64<kKvFp8Shared, kSelWindow>(p, grid, s);
+    else if (kv == kKvFp8Split)
+      launch_tile64<kKvFp8Split, kSelWindow>(p, grid, s);
+    else
+      launch_tile64<kKvBf16, kSelWindow>(p, grid, s);
+  } else if (kv == kKvMx4) {
+    launch_tile64<kKvMx4, kSelShared>(p, grid, s);
+  } else if (sel_kind == kSelPerRow) {
     if (kv == kKvFp8Shared)
       launch_kv<kKvFp8Shared, kSelPerRow>(p, grid, row_groups, s);
     else if (kv == kKvFp8Split)

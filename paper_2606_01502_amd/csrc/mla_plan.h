@@ -18,6 +18,8 @@ struct PlanArgs {
   bool tokens, per_row, fp8;
   int32_t n_splits, row_tile;
   int64_t cus;
+  bool mx4 = false;  // a 4-bit cache
+  int64_t list = 0;  // entries one split's list holds (0: by the selection)
 };
 
 struct Plan {
@@ -111,7 +113,7 @@ struct Planner {
 
   // entries one split's list holds (per-row selections with an fp8 cache: a
   // shorter one, see the kernel's LDS layout)
-  int64_t list_cap() const { return a.per_row && a.fp8 ? kPerRowListShort : kMaxSlotsPerSplit; }
+  int64_t list_cap() const { return a.list ? a.list : a.per_row && a.fp8 ? kPerRowListShort : kMaxSlotsPerSplit; }
   // per-row selections whose tile slots all fit one list split by logical
   // block: every split then scans all slots and the rows that chose a block
   // in different slots still share its load
@@ -163,7 +165,8 @@ struct Planner {
          {{5.7, 2.38, 5.5e6}, {8.4, 2.64, 5.5e6}, {9.2, 2.49, 5.5e6}, {14.5, 4.89, 5.5e6}}}};
     const Rate& rate = kRate[a.tokens][a.fp8][rg == 2 ? 3 : rows <= 32 ? 0 : rows <= 64 ? 1 : 2];
     // (rows with selections of their own share blocks, nobody here knows which)
-    const double item_bytes = a.per_row ? 0.0 : blocks * kBlock * (kDLat + kDPe) * (a.fp8 ? 1 : 2);
+    const double token_bytes = a.mx4 ? kMx4Row + 2 * kDPe : (kDLat + kDPe) * (a.fp8 ? 1 : 2);
+    const double item_bytes = a.per_row ? 0.0 : blocks * kBlock * token_bytes;
     auto wave_us = [&](int64_t items) {
       return rate.fixed + std::max(blocks * rate.block, (double)items * item_bytes / rate.bytes);
     };

@@ -31,7 +31,7 @@ EXPORTS = ("mla_sparse_partial_attn", "mla_sparse_partial_attn_ex",
            "mla_sparse_partial_attn_tokens", "mla_merge_partials", "mla_merge_partials_ex",
            "mla_last_error", "mla_version", "mla_primitive_costs", "mla_fetch_gather",
            "mla_fetch_splice", "mla_sparse_partial_attn_noalloc", "mla_batch_slots", "mla_rope",
-           "mla_cache_append")
+           "mla_cache_append", "mla_window_attn")
 
 
 class MlaError(RuntimeError):
@@ -82,6 +82,11 @@ class PartialOpts(ctypes.Structure):
 OUT_FP32, OUT_BF16_WIRE = 0, 1
 
 
+class WindowOpts(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_splits", ctypes.c_int32),
+                ("out_format", ctypes.c_int32), ("reserved", ctypes.c_int32 * 4)]
+
+
 class RopeOpts(ctypes.Structure):
     _fields_ = [("rot_offset", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
                 ("pairing", ctypes.c_int32), ("scaling", ctypes.c_int32),
@@ -126,6 +131,8 @@ def load(path: str = LIB_PATH):
     lib.mla_fetch_splice.restype = ctypes.c_int
     lib.mla_fetch_splice.argtypes = [P, P, P, P, P, ctypes.c_int64, ctypes.c_int64,
                                      ctypes.c_float, ctypes.c_int32, vp]
+    lib.mla_window_attn.restype = ctypes.c_int
+    lib.mla_window_attn.argtypes = [P] * 7 + [ctypes.c_float, P, P, ctypes.POINTER(WindowOpts), vp]
     lib.mla_batch_slots.restype = ctypes.c_int
     lib.mla_batch_slots.argtypes = [P] * 9 + [vp]
     lib.mla_rope.restype = ctypes.c_int
@@ -239,9 +246,7 @@ class _Prepared:
         return self.result
 
 
-def _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids, scale,
-                  out_lat, out_lse, ckv_scale, kpe_scale, n_splits, row_tile, stream, wire=False):
-    R = chunk_block_table.shape[0]  # jobs; q may hold fewer rows (R_q dividing R)
+def _attn_outputs(R, q_lat, out_lat, out_lse, wire):
     _, Mq, H, _ = q_lat.shape
     if out_lat is None:
         out_lat = torch.empty((R, Mq, H, DLAT), dtype=torch.bfloat16 if wire else torch.float32,
@@ -249,13 +254,20 @@ def _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_
     if out_lse is None:
         out_lse = torch.empty((R, Mq, H, 2) if wire else (R, Mq, H), dtype=torch.float32,
                               device=q_lat.device)
+    return out_lat, out_lse
+
+
+def _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids, scale,
+                  out_lat, out_lse, ckv_scale, kpe_scale, n_splits, row_tile, stream, wire=False):
+    R = chunk_block_table.shape[0]  # jobs; q may hold fewer rows (R_q dividing R)
+    out_lat, out_lse = _attn_outputs(R, q_lat, out_lat, out_lse, wire)
     _on_one_gpu(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids, out_lat,
                 out_lse, ckv_scale, kpe_scale)
     opts = PartialOpts()
     opts.n_splits = int(n_splits)
     opts.row_tile = int(row_tile)
     opts.out_format = OUT_BF16_WIRE if wire else OUT_FP32
-    descs = (describe(q_lat), describe(q_pe), describe(ckv_pool, ckv_scale),
+    descs = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale),
              describe(kpe_pool, kpe_scale), describe(chunk_block_table), describe(sel_block_ids))
     outs = (describe(out_lat), describe(out_lse))
     args = tuple(_ref(d) for d in descs) + (ctypes.c_float(scale),) + \
@@ -306,6 +318,38 @@ def sparse_partial_attn(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_
                                         kpe_scale, n_splits, row_tile, stream, wire)
     _check(lib, _partial_fn(lib, tokens, no_alloc)(*args))
     return result
+
+
+def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
+                   q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None,
+                   n_splits=0, stream=None, wire=False):
+    """window_attn with every argument fixed (see prepare_partial)."""
+    out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
+    _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, *out, ckv_scale,
+                    kpe_scale)
+    o = WindowOpts(int(window), int(n_sink), int(n_splits), OUT_BF16_WIRE if wire else OUT_FP32)
+    d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale),
+         describe(kpe_pool, kpe_scale), describe(block_table), describe(seq_lens), describe(q_lens))
+    do = tuple(describe(t) for t in out)
+    args = (*[_ref(x) for x in d], ctypes.c_float(scale), *[_ref(x) for x in do], ctypes.byref(o),
+            _stream(stream))
+    keep = (d, do, o, q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, ckv_scale,
+            kpe_scale)
+    return _Prepared(load().mla_window_attn, args, keep, out)
+
+
+def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
+                q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None, n_splits=0,
+                stream=None, wire=False):
+    """Attention of each request's last q_lens[b] tokens (default: all Mq query
+    rows) over its paged sequence of seq_lens[b] tokens, each row seeing the
+    last `window` tokens up to its own (0: all) and the first n_sink.  Pools
+    are bf16, fp8 (uint8 with scales) or 4-bit (uint8 rows of MX4_ROW bytes,
+    the RoPE pool bf16).  Returns partials as sparse_partial_attn does, in
+    either form, for merge_partials or as they are."""
+    return prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window,
+                          n_sink, q_lens, out_lat, out_lse, ckv_scale, kpe_scale, n_splits, stream,
+                          wire)()
 
 
 def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=None,

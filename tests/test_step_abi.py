@@ -239,3 +239,114 @@ def test_rope_reference_is_a_rotation():
         assert np.array_equal(y[..., :16], x[..., :16])
         back = S.rope(y, [0, 1, 77, -3, 2 ** 31 - 1], pairing=pairing, inverse=True, **kw)
         assert np.allclose(back, x)
+
+
+# ---- windows and 4-bit caches
+def window_args(fp8=False, mx4=False, wire=False):
+    kv = U8 if fp8 or mx4 else BF16
+    s = torch.ones(8)
+    return dict(q_lat=z(2, 3, 16, 512), q_pe=z(2, 3, 16, 64), ckv=z(8, 64, 272 if mx4 else 512, dt=kv),
+                kpe=z(8, 64, 64, dt=U8 if fp8 else BF16), table=z(2, 5, dt=I32), lens=z(2, dt=I32),
+                q_lens=z(2, dt=I32), out=z(2, 3, 16, 512, dt=BF16 if wire else F32),
+                lse=z(*((2, 3, 16, 2) if wire else (2, 3, 16)), dt=F32), scale=0.1, s=s if fp8 else None,
+                opts=mla.WindowOpts(64, 4, 0, 1 if wire else 0))
+
+
+def window_call(a):
+    lib = mla.load()
+
+    def d(key, scale=None):
+        t = a[key]
+        if t is None:
+            return None
+        if key in ("ckv", "kpe") and t.dtype == U8:
+            return ctypes.byref(mla._describe_latent(t, scale))
+        return ctypes.byref(mla.describe(t))
+    st = lib.mla_window_attn(d("q_lat"), d("q_pe"), d("ckv", a["s"]), d("kpe", a["s"]), d("table"), d("lens"),
+                             d("q_lens"), ctypes.c_float(a["scale"]), d("out"), d("lse"),
+                             ctypes.byref(a["opts"]) if a["opts"] is not None else None, None)
+    return st, lib.mla_last_error().decode()
+
+
+def wopts(**kw):
+    o = mla.WindowOpts(64, 4, 0, 0)
+    for k, v in kw.items():
+        if k == "reserved":
+            o.reserved[3] = v
+        else:
+            setattr(o, k, v)
+    return o
+
+
+WINDOW = [
+    ("q_lat null", dict(q_lat=None), INVALID, "q_lat"),
+    ("ckv null", dict(ckv=None), INVALID, "ckv_pool"),
+    ("lens null", dict(lens=None), INVALID, "seq_lens"),
+    ("out null", dict(out=None), INVALID, "out_lat"),
+    ("opts null", dict(opts=None), INVALID, "opts"),
+    ("lens int64", dict(lens=z(2, dt=torch.int64)), INVALID, "seq_lens: wrong dtype"),
+    ("q_lens int64", dict(q_lens=z(2, dt=torch.int64)), INVALID, "q_lens: wrong dtype"),
+    ("lens length", dict(lens=z(3, dt=I32)), INVALID, "seq_lens"),
+    ("q_lens length", dict(q_lens=z(1, dt=I32)), INVALID, "q_lens"),
+    ("lens strided", dict(lens=z(4, dt=I32)[::2]), INVALID, "innermost stride"),
+    ("B of q", dict(q_lat=z(1, 3, 16, 512)), INVALID, "q_lat: shape"),
+    ("q_pe shape", dict(q_pe=z(2, 3, 16, 32)), INVALID, "q_pe: shape"),
+    ("ckv fp32", dict(ckv=z(8, 64, 512, dt=F32)), INVALID, "bf16 or fp8"),
+    ("fp8 without scales", dict(ckv=z(8, 64, 512, dt=U8), kpe=z(8, 64, 64, dt=U8)), INVALID, "block_scale"),
+    ("mx4 with an 8-bit RoPE pool", dict(ckv=z(8, 64, 272, dt=U8), kpe=z(8, 64, 64, dt=U8)), INVALID,
+     "kpe_pool: wrong dtype"),
+    ("mx4 strided", dict(ckv=z(16, 64, 272, dt=U8)[::2]), INVALID, "contiguous"),
+    ("mx4 unaligned", dict(ckv=off(z(8, 64, 272, dt=U8), 8)), INVALID, "16-byte"),
+    ("out dtype", dict(out=z(2, 3, 16, 512)), INVALID, "out_lat: wrong dtype"),
+    ("out shape", dict(out=z(2, 3, 15, 512, dt=F32)), INVALID, "out_lat: shape"),
+    ("lse shape", dict(lse=z(2, 3, 15, dt=F32)), INVALID, "out_lse: shape"),
+    ("out rows overlap", dict(out=z(1, 3, 16, 512, dt=F32).expand(2, 3, 16, 512)), INVALID, "rows overlap"),
+    ("lse rows overlap", dict(lse=z(1, 3, 16, dt=F32).expand(2, 3, 16)), INVALID, "rows overlap"),
+    ("q unaligned", dict(q_lat=off(z(2, 3, 16, 512), 1)), INVALID, "aligned"),
+    ("scale nan", dict(scale=float("nan")), INVALID, "scale"),
+    ("window", dict(opts=wopts(window=-1)), INVALID, "window"),
+    ("n_sink", dict(opts=wopts(n_sink=-1)), INVALID, "n_sink"),
+    ("n_splits", dict(opts=wopts(n_splits=-1)), INVALID, "n_splits"),
+    ("out_format", dict(opts=wopts(out_format=2)), INVALID, "out_format"),
+    ("reserved", dict(opts=wopts(reserved=1)), INVALID, "reserved"),
+    ("table too wide", dict(table=z(2, 1, dt=I32).expand(2, 2 ** 25 + 1)), INVALID, "innermost"),
+]
+
+
+@pytest.mark.parametrize("name,change,status,text", WINDOW, ids=[c[0] for c in WINDOW])
+def test_window_refused(name, change, status, text):
+    a = window_args()
+    a.update(change)
+    st, msg = window_call(a)
+    assert st == status and text in msg, (st, msg)
+
+
+def test_window_overlaps_refused():
+    a = window_args()
+    flat = torch.zeros(2 * 3 * 16 * 512 + 96)
+    a["out"], a["lse"] = flat[:-96].view(2, 3, 16, 512), flat[-192:-96].view(2, 3, 16)
+    st, msg = window_call(a)
+    assert st == INVALID and "out_lat and out_lse overlap" in msg
+    a = window_args()
+    a["lse"] = a["lens"].view(F32).view(1, 1, 2)[:, :, :0]
+    a["lse"] = torch.zeros(2 * 3 * 16)
+    a["lens"] = a["lse"].view(I32)[:2]
+    a["lse"] = a["lse"].view(2, 3, 16)
+    st, msg = window_call(a)
+    assert st == INVALID and "overlaps an input" in msg
+
+
+def test_partial_of_a_4bit_cache_refuses_what_it_does_not_do():
+    from tests import abi_cases as C
+    lib = mla.load()
+    for tokens, sel, tile, text in ((True, (2, 3), 0, "one block selection"), (False, (2, 3, 3), 0, "one block selection"),
+                                    (False, (2, 3), 128, "64-row")):
+        a = C.partial_args(torch.device("cpu"))
+        a["ckv"], a["sel"] = z(8, 64, 272, dt=U8), z(*sel, dt=I32)
+        a["opts"].row_tile = tile
+        descs = [mla._describe_latent(a["ckv"]) if k == "ckv" else mla.describe(a[k])
+                 for k in ("q_lat", "q_pe", "ckv", "kpe", "table", "sel")]
+        fn = lib.mla_sparse_partial_attn_tokens if tokens else lib.mla_sparse_partial_attn_ex
+        st = fn(*[ctypes.byref(d) for d in descs], ctypes.c_float(0.1), _ref(a["out_lat"]), _ref(a["out_lse"]),
+                ctypes.byref(a["opts"]), None)
+        assert st == UNSUPPORTED and text in lib.mla_last_error().decode()
