@@ -1822,6 +1822,41 @@ struct Issue32 {
   }
 };
 
+// 4-bit caches: the conversion of a stage's latent rows to bf16.  A wave takes four
+// rows at a time, a lane 32 columns of row row0 + (lane >> 4): one group, 4 chunks
+// of 16 bytes.  Chunk c = 4 g + j of row t (group g) sits in slot 16 j + (g ^
+// key32(t)): a 16-byte LDS write serves 8 neighbouring lanes a cycle, whose groups
+// then fall to different banks, and the four writes of a lane lie 256 bytes apart.
+// Read as a bf16 stage is, slot for slot, these rows have their columns in another
+// order, which the query rows follow (mx4_chunk) and the output's columns undo.
+// (With the bf16 stages' order, 4 g + j ^ key32(t), lanes had to write their chunks
+// in orders of their own: 24 instructions more a wave and stage, 2.5 us for 2.2 a
+// block of 64 rows.)
+__device__ __forceinline__ int mx4_chunk(int slot) { return 4 * (slot & 15) + (slot >> 4); }
+template <class L>
+struct Convert {
+  u32x4_t codes;
+  uint32_t exp;
+  uint32_t put;  // the lane's place in a stage, row row0 + (lane >> 4)
+  __device__ __forceinline__ Convert(int row0, int lane) {
+    const int x = lane >> 4, g = lane & 15;
+    const int key = (x << 2) | ((row0 >> 3) & 1) << 1 | ((row0 >> 4) & 1);  // key32(row0 + x)
+    put = (uint32_t)((row0 + x) * 1024 + ((g ^ key) << 4));
+  }
+  // of rows row0 .. row0 + 3 of the stage of codes at `in`
+  __device__ __forceinline__ void read(uint32_t in, int row0, int lane) {
+    codes = *(const LDS u32x4_t*)(uintptr_t)((uint32_t)(lane << 4) + (in + (uint32_t)(row0 * 256)));
+    exp = *(const LDS uint8_t*)(uintptr_t)((uint32_t)lane + (in + (uint32_t)(L::kInCodes + row0 * 16)));
+  }
+  // chunks j0 .. j1 - 1 to the stage at `out`
+  __device__ __forceinline__ void write(uint32_t out, int j0, int j1) const {
+    LDS uint8_t* const a = (LDS uint8_t*)(uintptr_t)(put + out);
+#pragma unroll
+    for (int j = j0; j < j1; ++j)
+      *(LDS u32x4_t*)(a + j * 256) = mx4x8_bf16(codes[j], __uint_as_float(exp << 23));
+  }
+};
+
 template <int KV, int SEL, int NK>  // NK: row halves of 32 rows
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void tile64_kernel(const PartialParams p) {
@@ -1980,50 +2015,29 @@ void tile64_kernel(const PartialParams p) {
     const int t = 16 * rq + n16;
     const LDS uint8_t* const qr = smem + L::kQ + t * 1024;
     const LDS uint8_t* const qp = smem + L::kQ + 65536 + t * 128;
+    // (4 bits: latent steps by the slots of a converted row, see mx4_chunk)
     auto chunk = [&](int ks) { return FP8 ? 8 * (ks >> 1) + 2 * g + (ks & 1) : 4 * ks + g; };
+    auto lat_chunk = [&](int ks) { return MX4 ? mx4_chunk(chunk(ks)) : chunk(ks); };
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) qb[ks] = lds_b128(qp + ((chunk(ks) ^ rope_key32<false>(t)) << 4));
 #pragma unroll
-    for (int ks = 0; ks < 16; ++ks) qb[2 + ks] = lds_b128(qr + ((chunk(ks) ^ key32(t)) << 4));
+    for (int ks = 0; ks < 16; ++ks) qb[2 + ks] = lds_b128(qr + ((lat_chunk(ks) ^ key32(t)) << 4));
   }
-  // 4-bit caches: a wave converts the rows it loaded itself, 4 a stage, a lane 32
-  // columns of row 4 wave + (lane >> 4): one group, 4 chunks of 16 bytes.  Lanes of
-  // one LDS pass write the chunks of their groups in orders of their own (XOR
-  // r), so that these fall to different banks: with one order for all, four
-  // groups of a row meet on one.
-  // (The addresses are formed where they are used: registers are short.)
-  u32x4_t cv_codes{};
-  float cv_scale = 0.f;
-  uint32_t cv_put = 0;
-  auto cv_read = [&](int h) {
-    const int l = lds_opaque(lane);
-    const uint32_t a = lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage);
-    cv_codes = *(const LDS u32x4_t*)(uintptr_t)(a + (uint32_t)(wave * 1024 + l * 16));
-    cv_scale = mx4_scale(*(const LDS uint8_t*)(uintptr_t)(a + (uint32_t)(L::kInCodes + wave * 64 + l)));
-  };
-  // codes of chunk j ^ r to place j, and the place of chunk r: chunk 4 g + k of
-  // row t goes to slot (4 g + k) ^ key32(t)
-  auto cv_turn = [&](int h) {
-    const int l = lds_opaque(lane), x = l >> 4, g = l & 15, r = (g >> 2) ^ (x & 1);
-    u32x4_t c = cv_codes;
-    c = r & 1 ? u32x4_t{c[1], c[0], c[3], c[2]} : c;
-    c = r & 2 ? u32x4_t{c[2], c[3], c[0], c[1]} : c;
-    cv_codes = c;
-    const int kw = ((wave >> 1) & 1) << 1 | (wave >> 2);  // key32 less the low bits' part
-    cv_put = lds0 + (uint32_t)((h % L::kNum) * L::kStage + (4 * wave + x) * 1024 + ((g ^ x) << 6) + ((r ^ kw) << 4));
-  };
-  // (stages lie on whole kilobytes: bits 4 and 5 are the chunk's)
-  auto cv_write = [&](int j) {
-    *(LDS u32x4_t*)(uintptr_t)(cv_put ^ (uint32_t)(j << 4)) = mx4x8_bf16(cv_codes[j], cv_scale);
+  // 4-bit caches: every wave converts the four rows of a stage that it loaded,
+  // beside its value products, when the LDS has room.  (One row half, 32 jobs x 1024
+  // blocks of 16 rows: the waves without scores of their own converting eight rows
+  // each while the others form theirs, 276 us.)
+  Convert<L> cv(4 * wave, lane);
+  // the ring's places of stages i, i + 1 and i + 2 of converted rows
+  uint32_t ring0 = lds0, ring1 = lds0 + L::kStage, ring2 = lds0 + 2 * L::kStage;
+  auto codes_of = [&](int h) { return lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage); };
+  auto convert_first = [&](int h, uint32_t out) {
+    cv.read(codes_of(h), 4 * wave, lane);
+    cv.write(out, 0, 4);
   };
   if constexpr (MX4) {
     lds_barrier();  // every wave holds its query rows: their place takes tokens
-    if (n > 0) {
-      cv_read(0);
-      cv_turn(0);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) cv_write(j);
-    }
+    if (n > 0) convert_first(0, ring0);
   }
   if constexpr (L::kNum > 4) {
     lds_barrier();  // every wave holds its query rows: their place takes tokens
@@ -2256,11 +2270,11 @@ void tile64_kernel(const PartialParams p) {
   // take registers: a spilled query fragment would be read back in every stage,
   // with a wait for all loads in flight)
   constexpr int kAhead = NK == 2 && TOK ? (FP8 ? (kSplitScales ? 2 : 3) : 5)
-                       : NK == 2 && WIN ? (MX4 ? 3 : FP8 ? (kSplitScales ? 2 : 3) : 5)
-                       : NK == 2 && MX4 ? 4 : FP8 ? 3 : 6;
+                       : NK == 2 && WIN ? (MX4 ? 4 : FP8 ? (kSplitScales ? 2 : 3) : 5)
+                       : NK == 2 && MX4 ? 5 : FP8 ? 3 : 6;
   auto scores = [&](int i, auto mid) -> u32x2_t {
     constexpr bool kMid = decltype(mid)::value;
-    const uint32_t st = (uint32_t)(((i + 1) % L::kNum) * L::kStage);
+    const uint32_t st = MX4 ? (kMid ? ring1 : ring0) - lds0 : (uint32_t)(((i + 1) % L::kNum) * L::kStage);
     const uint32_t st_in = MX4 ? (uint32_t)(((i + 1) % L::kInNum) * L::kInStage) : st;
     const int ih = i + L::kLead;  // the stage to load
     bf16x8_t kr[kAhead + 1];
@@ -2317,14 +2331,6 @@ void tile64_kernel(const PartialParams p) {
           }
         }
         if (kLd && step % 3 == 1 && step / 3 < L::kLoads) is.load(p, step / 3, wave, lane);
-        if constexpr (MX4) {
-          // stage i + 2 to bf16, for the scores of the next step
-          if (i + 2 < n) {
-            if (step == 2) cv_read(i + 2);
-            if (step == 6) cv_turn(i + 2);
-            if (step >= 7 && step <= 13 && (step & 1)) cv_write((step - 7) >> 1);
-          }
-        }
         // what the softmax and the value products of this step need
         if (step == 3) {
           if constexpr (FP8 && !TOK) {
@@ -2428,6 +2434,14 @@ void tile64_kernel(const PartialParams p) {
       // room for the tokens' scales would come too soon after it)
       if constexpr (NK == 1 && FP8 && TOK && kSoft) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 2");
       if (kSoft) soft(f, i + 1);
+      if constexpr (MX4 && kSoft) {
+        // (4 bits: stage i + 2 to bf16, for the scores of the next step)
+        if (i + 2 < n) {
+          if (f == 0) cv.read(codes_of(i + 2), 4 * wave, lane);
+          if (f == 1) cv.write(ring2, 0, 2);
+          if (f == 2) cv.write(ring2, 2, 4);
+        }
+      }
     }
   };
 
@@ -2435,6 +2449,9 @@ void tile64_kernel(const PartialParams p) {
     is.look(list, L::kLead - 1, wave, lane, ahead);
     meet(-1);
     (void)scores(-1, std::false_type{});
+    if constexpr (MX4) {
+      if (n > 1) convert_first(1, ring1);
+    }
     soft(0, 0);
     // (nothing is left over before the first step: products of zeros)
     vr[3] = VRing{};
@@ -2448,15 +2465,21 @@ void tile64_kernel(const PartialParams p) {
     }
     for (int i = 0; i + 1 < n; ++i) {
       meet(i);
-      v_st = (uint32_t)((i % L::kNum) * L::kStage);
+      v_st = MX4 ? ring0 - lds0 : (uint32_t)((i % L::kNum) * L::kStage);
       const u32x2_t ask = scores(i, std::true_type{});
       settle(i, ask);
       values(i, std::true_type{});
+      if constexpr (MX4) {
+        const uint32_t first = ring0;
+        ring0 = ring1;
+        ring1 = ring2;
+        ring2 = first;
+      }
     }
     const int i = n - 1;
     lds_barrier();
     const u32x2_t ask = *(LDS const u32x2_t*)(asks(i) + 8 * lane);
-    v_st = (uint32_t)((i % L::kNum) * L::kStage);
+    v_st = MX4 ? ring0 - lds0 : (uint32_t)((i % L::kNum) * L::kStage);
     if (n > 1) {
       pv_one(3, 0, true);
       pv_one(3, 1, false);
@@ -2555,6 +2578,8 @@ void tile64_kernel(const PartialParams p) {
   // swaps between lanes l, l ^ 16 (and l, l ^ 32 for 16-bit rows) give each
   // store instruction 64-byte runs of 16 rows: row 16 j + (lane & 15) of half k.
   const int q = lane >> 4;
+  // 4 bits: the column that slot 8 wave + c / 8 of a converted row holds
+  auto col_of = [&](int c) { return 8 * mx4_chunk(8 * wave + (c >> 3)) + (c & 7); };
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
     // the element offsets of this lane's two rows
@@ -2604,7 +2629,10 @@ void tile64_kernel(const PartialParams p) {
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          if (ok[j]) *(u32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * (q & 1) + 8 * (q >> 1)) = u[j];
+          if (ok[j]) {
+            if constexpr (MX4) *(u32x4_t*)(dst + off[j] + col_of(32 * d + 16 * (q & 1) + 8 * (q >> 1))) = u[j];
+            else *(u32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * (q & 1) + 8 * (q >> 1)) = u[j];
+          }
       }
     } else {
       float* const dst = direct ? p.out : p.ws_o32;
@@ -2623,7 +2651,10 @@ void tile64_kernel(const PartialParams p) {
           }
 #pragma unroll
           for (int j = 0; j < 2; ++j)
-            if (ok[j]) *(f32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1)) = u[j];
+            if (ok[j]) {
+              if constexpr (MX4) *(f32x4_t*)(dst + off[j] + col_of(32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1))) = u[j];
+              else *(f32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1)) = u[j];
+            }
         }
       }
     }

@@ -62,17 +62,17 @@ def test_splits_and_slots(splits, H):
     check(c, ql, qp, table, sel, n_splits=splits)
 
 
-def test_equals_a_bf16_cache_of_the_same_values():
-    """The values are exact in bf16: 64-row tiles of a bf16 pool that holds them
-    sum the same products in the same order."""
+def test_agrees_with_a_bf16_cache_of_the_same_values():
+    """The values are exact in bf16: a bf16 pool that holds them gives the same
+    partials but for the order of the scores' sums (columns are summed in another
+    order) and what the roundings of the weights make of it."""
     print("case: mx4 as bf16", flush=True)
     for H, Mq in ((16, 1), (64, 2)):
         c, ql, qp, table, sel = inputs(7, 3, Mq, H, 20, 14)
-        a = mla.sparse_partial_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(sel), SCALE, n_splits=2)
-        as16 = torch.from_numpy(c.lat).bfloat16().cuda()
-        b = mla.sparse_partial_attn(ql, qp, as16, c.kpe, T.i32(table), T.i32(sel), SCALE, n_splits=2, row_tile=64)
-        torch.cuda.synchronize()
-        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        check(c, ql, qp, table, sel, n_splits=2)
+        c.ckv = torch.from_numpy(c.lat).bfloat16().cuda()
+        assert np.array_equal(T.host(c.ckv), c.lat)
+        check(c, ql, qp, table, sel, n_splits=2, row_tile=64)
 
 
 def test_every_exponent_the_writer_uses():
