@@ -1442,8 +1442,11 @@ void partial_kernel(const PartialParams p) {
 // row masks, two buffers of weights P (4 KiB each) and the waves' exchange
 // area.  The query rows pass through the stages after the first two before any
 // tokens do (72 KiB).  4-bit caches: the ring holds latent rows only, three
-// stages of 32 KiB of converted bf16, and a second ring four stages as they come
-// from memory: 8 KiB of codes, 512 bytes of exponents, 4 KiB of RoPE rows.
+// stages of 32 KiB of converted bf16, and two more rings four stages as they come
+// from memory: 8 KiB of codes with 512 bytes of exponents, and 4 KiB of RoPE rows.
+// A stage's codes are converted a step before its RoPE rows are read, so that four
+// slots hold codes a step further ahead (with both a stage's 12.5 KiB in one slot
+// and loads two steps ahead, 32 jobs x 1024 blocks of 16 rows took 288 us).
 template <bool FP8, bool PR, bool MX4 = false, bool WIN = false>
 struct Tile {
   static constexpr bool kFp8 = FP8;
@@ -1458,17 +1461,20 @@ struct Tile {
   static constexpr int kLoads = FP8 || MX4 ? 3 : 5;  // direct-to-LDS loads per wave per stage
   // the ring that the loads go to, its stages, and where a stage's RoPE rows lie in it
   static constexpr int kIn = MX4 ? kNum * kStage : 0;
-  static constexpr int kInCodes = kTok * kDLat / 2, kInRope = MX4 ? kInCodes + kTok * 16 : kStageCkv;
-  static constexpr int kInStage = MX4 ? kInRope + kTok * kRopeRow : kStage;
+  static constexpr int kInCodes = kTok * kDLat / 2;
+  static constexpr int kInStage = MX4 ? kInCodes + kTok * 16 : kStage;
   static constexpr int kInNum = MX4 ? 4 : kNum;
-  // the stage that step i loads is i + kLead
-  static constexpr int kLead = MX4 ? kInNum : kNum - 1;
+  // the ring of RoPE rows (else they follow a stage's latent rows)
+  static constexpr int kInRope = MX4 ? kIn + kInNum * kInStage : kStageCkv;
+  static constexpr int kRopeStage = kTok * kRopeRow;
+  // the stage that step i loads is i + kLead (4 bits: its codes, and RoPE rows of the one before)
+  static constexpr int kLead = MX4 ? kInNum + 1 : kNum - 1;
   // the query rows' place: 64 rows of 1 KiB, then of 128 B
   static constexpr int kQ = MX4 ? 0 : 2 * kStage;
   static constexpr int kCap = PR || WIN ? kPerRowListShort : kMaxSlotsPerSplit;
   // per-row selections: the compaction's counters take up to kPerRowCounterBytes
   // from the start; what it writes lies past them (fp8: the rest in between)
-  static constexpr int kRing = kNum * kStage + (MX4 ? kInNum * kInStage : 0);
+  static constexpr int kRing = kNum * kStage + (MX4 ? kInNum * (kInStage + kRopeStage) : 0);
   static constexpr int kList = PR ? (kPerRowCounterBytes + 255) / 256 * 256 : kRing;
   static constexpr int kScales = kList + kCap * 4;
   static constexpr int kMasks = kScales + (FP8 ? kCap * 12 : 0);
@@ -1704,13 +1710,17 @@ struct Issue32 {
   // TOK: pool tokens of stage token 4w + (lane & 3) and (fp8) of the RoPE load's row
   int tok, tok_rope;
   int last;  // WIN: the stage's last row that the sequence holds
+  // 4 bits: of the RoPE rows, a stage behind the codes
+  const uint8_t* kpe_then;
+  int last_then;
 
   __device__ __forceinline__ Issue32(const PartialParams& p, int wave, int lane) {
     ckv = p.ckv;
     kpe = p.kpe;
     lds_lat = lds_rope = 0;
     tok = tok_rope = 0;
-    last = 31;
+    last = last_then = 31;
+    kpe_then = p.kpe;
     const int b3 = (wave >> 1) & 1;           // bit 3 of the wave's rows
     const int kw = (b3 << 1) | (wave >> 2);   // their key32, less the low bits' part
     const int hi = lane >> 5;
@@ -1736,7 +1746,13 @@ struct Issue32 {
     if constexpr (WIN) e[1] = list[h + (L::kMasks - L::kList) / 4];
   }
   // points the loads at half block h and stage buf; n_tok: the sequence's tokens (windows)
-  __device__ __forceinline__ void aim(const PartialParams& p, const int (&e)[2], int h, uint32_t buf, int wave, int n_tok) {
+  // (4 bits: rope_buf, the place of stage h - 1's RoPE rows)
+  __device__ __forceinline__ void aim(const PartialParams& p, const int (&e)[2], int h, uint32_t buf, uint32_t rope_buf,
+                                      int wave, int n_tok) {
+    if constexpr (MX4) {
+      kpe_then = kpe;
+      last_then = last;
+    }
     if constexpr (TOK) {
       tok = e[0];
       tok_rope = e[1];
@@ -1751,7 +1767,7 @@ struct Issue32 {
       kpe = p.kpe + b * (32 * L::kRopeRow) + wave * (4 * L::kRopeRow);
     }
     lds_lat = __builtin_amdgcn_readfirstlane(buf + (uint32_t)wave * (MX4 ? 4 * kDLat / 2 : 4 * L::kRow));
-    lds_rope = __builtin_amdgcn_readfirstlane(buf + (uint32_t)L::kInRope + (uint32_t)wave * (4 * L::kRopeRow));
+    lds_rope = __builtin_amdgcn_readfirstlane((MX4 ? rope_buf : buf + (uint32_t)L::kInRope) + (uint32_t)wave * (4 * L::kRopeRow));
   }
   __device__ __forceinline__ static void go(uint32_t off, const uint8_t* base, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
@@ -1771,14 +1787,17 @@ struct Issue32 {
     return (uint32_t)lds_opaque((int)lat[0]) ^ (uint32_t)(j << (FP8 ? 7 : 6));
   }
   // WIN: the byte offset of the stage's row r, or of the last there is
-  __device__ __forceinline__ uint32_t row_off(int r, uint32_t bytes) const { return (uint32_t)min(r, last) * bytes; }
+  __device__ __forceinline__ uint32_t row_off(int r, uint32_t bytes) const {
+    return (uint32_t)min(r, MX4 && bytes == L::kRopeRow ? last_then : last) * bytes;
+  }
   // Load j; every lane of the wave is active where this is called.
   __device__ __forceinline__ void load(const PartialParams& p, int j, int wave, int lane) const {
     if constexpr (WIN) {
       const int l = lds_opaque(lane);  // (row offsets are formed here, not held)
       if (j == kLat) {
         constexpr int kPer = L::kRopeRow / 16;  // lanes a RoPE row
-        go_lanes(rope + row_off(4 * wave + l / kPer, L::kRopeRow), kpe, lds_rope, (1ull << (4 * kPer)) - 1);
+        go_lanes(rope + row_off(4 * wave + l / kPer, L::kRopeRow), MX4 ? kpe_then : kpe, lds_rope,
+                 (1ull << (4 * kPer)) - 1);
       } else if constexpr (MX4) {
         if (j == 0) go(lat[0] + row_off(4 * wave + (l >> 4), kMx4Row), ckv, lds_lat);
         else go_lanes(lat[1] + row_off(4 * wave + l, kMx4Row), ckv, lds_exp(wave), 15);
@@ -1789,7 +1808,7 @@ struct Issue32 {
     } else if constexpr (MX4) {
       if (j == 0) go(lat[0], ckv, lds_lat);
       else if (j == 1) go_lanes(lat[1], ckv, lds_exp(wave), 15);
-      else go_lanes(rope, kpe, lds_rope, 0xffffffffull);
+      else go_lanes(rope, kpe_then, lds_rope, 0xffffffffull);
     } else if (j < kLat) {
       if constexpr (!TOK) {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3"
@@ -1983,24 +2002,33 @@ void tile64_kernel(const PartialParams p) {
   Issue32<FP8, TOK, MX4, WIN> is(p, wave, lane);
   int ahead[2] = {0, 0};  // the list entries of the stage to load next
   auto aim = [&](int h) {
-    is.aim(p, ahead, h, lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage), wave, win.n_tok);
+    const uint32_t rope_buf = MX4 ? lds0 + (uint32_t)(L::kInRope + ((h - 1) % L::kInNum) * L::kRopeStage) : 0u;
+    is.aim(p, ahead, h, lds0 + (uint32_t)(L::kIn + (h % L::kInNum) * L::kInStage), rope_buf, wave, win.n_tok);
   };
   auto issue = [&](int h) {
-    if (h >= n) return;
+    if (h - (MX4 ? 1 : 0) >= n) return;
     is.look(list, h, wave, lane, ahead);
     aim(h);
 #pragma unroll
-    for (int j = 0; j < L::kLoads; ++j) is.load(p, j, wave, lane);
+    for (int j = 0; j < L::kLoads; ++j) {
+      // (4 bits: codes of stage h, RoPE rows of stage h - 1)
+      if (!MX4 || (j < 2 ? h < n : h > 0)) is.load(p, j, wave, lane);
+    }
   };
   issue(0);
   issue(1);
-  if constexpr (MX4) issue(2);
-  // the query rows have landed (4 bits: and stage 0, which is converted here)
   if constexpr (MX4) {
-    if (n > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
-    else if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(L::kLoads));
+    issue(2);
+    issue(3);
+    // the query rows have landed and stage 0's codes: past them are 3 (RoPE rows 0,
+    // codes 1) and 3 more for each stage, or 1 where the codes end
+    if (n > 3) __builtin_amdgcn_s_waitcnt(waitcnt_vm(9));
+    else if (n > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(7));
+    else if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(4));
+    else if (n > 0) __builtin_amdgcn_s_waitcnt(waitcnt_vm(1));
     else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   } else {
+    // the query rows have landed
     if (n > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * L::kLoads));
     else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
   }
@@ -2075,7 +2103,7 @@ void tile64_kernel(const PartialParams p) {
     for (int i = 0; i < 4; ++i) k_off[i] = lds0 + (uint32_t)(t * L::kRow + (((4 * i + g) ^ key32(t)) << 4));
 #pragma unroll
     for (int i = 0; i < kRopeReads; ++i)
-      r_off[i] = lds0 + (uint32_t)(L::kIn + L::kInRope + t * L::kRopeRow + (((4 * i + g) ^ rope_key32<FP8>(t)) << 4));
+      r_off[i] = lds0 + (uint32_t)(L::kInRope + t * L::kRopeRow + (((4 * i + g) ^ rope_key32<FP8>(t)) << 4));
     // the value fragment of column tile d and 16 tokens kk.  bf16: two
     // transposing reads of 4 tokens x 16 columns per 16 lanes (lane i of group
     // q: tokens 8 (q >> 1) + (i >> 2) and 4 on, columns 16 (q & 1) + 4 (i & 3));
@@ -2250,8 +2278,12 @@ void tile64_kernel(const PartialParams p) {
   // kNum - 3 stages' may be in flight) and meets the other waves
   auto meet = [&](int i) {
     if constexpr (MX4) {
-      // (4 bits: stage i + 2's, which step i converts; stage i + 3's may be in flight)
-      if (n - 3 - i >= 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm(L::kLoads));
+      // (4 bits: stage i + 2's codes, which step i converts, and stage i + 1's RoPE
+      // rows, both loaded in step i - 3; what steps i - 2 and i - 1 loaded may be in
+      // flight, 2 for a stage's codes and 1 for its RoPE rows, as far as there are any)
+      if (i + 4 < n) __builtin_amdgcn_s_waitcnt(waitcnt_vm(6));
+      else if (i + 4 == n) __builtin_amdgcn_s_waitcnt(waitcnt_vm(4));
+      else if (i + 3 == n) __builtin_amdgcn_s_waitcnt(waitcnt_vm(1));
       else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
       lds_barrier();
       return;
@@ -2275,7 +2307,7 @@ void tile64_kernel(const PartialParams p) {
   auto scores = [&](int i, auto mid) -> u32x2_t {
     constexpr bool kMid = decltype(mid)::value;
     const uint32_t st = MX4 ? (kMid ? ring1 : ring0) - lds0 : (uint32_t)(((i + 1) % L::kNum) * L::kStage);
-    const uint32_t st_in = MX4 ? (uint32_t)(((i + 1) % L::kInNum) * L::kInStage) : st;
+    const uint32_t st_in = MX4 ? (uint32_t)(((i + 1) % L::kInNum) * L::kRopeStage) : st;
     const int ih = i + L::kLead;  // the stage to load
     bf16x8_t kr[kAhead + 1];
     bf16x8_t ka[4];  // fp8: converted ahead of their products
@@ -2293,7 +2325,7 @@ void tile64_kernel(const PartialParams p) {
     }
     u32x2_t ask{};
     if constexpr (kMid) ask = *(LDS const u32x2_t*)(asks(i) + 8 * lane);
-    const bool ld = ih < n;
+    const bool ld = ih - (MX4 ? 1 : 0) < n;
     if constexpr (kMid) pv_one(3, 0, true);
     if (ld) aim(ih);
     if constexpr (kMid) pv_one(3, 1, false);
@@ -2330,7 +2362,9 @@ void tile64_kernel(const PartialParams p) {
             if (step + kAhead < kReads) key_read(step + kAhead);
           }
         }
-        if (kLd && step % 3 == 1 && step / 3 < L::kLoads) is.load(p, step / 3, wave, lane);
+        if (kLd && step % 3 == 1 && step / 3 < L::kLoads) {
+          if (!MX4 || step / 3 == 2 || ih < n) is.load(p, step / 3, wave, lane);
+        }
         // what the softmax and the value products of this step need
         if (step == 3) {
           if constexpr (FP8 && !TOK) {
