@@ -282,7 +282,9 @@ typedef struct {
   int32_t n_sink;      /* first tokens of the sequence that every row sees         */
   int32_t n_splits;    /* split-K: splits of a tile's tokens (0 = automatic)       */
   int32_t out_format;  /* MLA_OUT_FP32 or MLA_OUT_BF16_WIRE                        */
-  int32_t reserved[4]; /* must be zero                                             */
+  int32_t row_tile;    /* rows per work item: 64 or 128 (0 = automatic; 4-bit
+                          caches: 64)                                              */
+  int32_t reserved[3]; /* must be zero                                             */
 } mla_window_opts_t;
 
 /*

@@ -398,11 +398,11 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
   }
 }
 
-// The most half blocks that the rows of a 64-row tile of a window see: the window
-// of its first row and of those after it, and the sinks.
+// The most half blocks that the rows of a tile (of 128 rows, or 64) of a window see:
+// the window of its first row and of those after it, and the sinks.
 int64_t window_halves(int64_t Mq, int64_t H, int64_t NB, int64_t window, int64_t n_sink) {
   if (window == 0) return 2 * NB;
-  const int64_t n_i = std::min<int64_t>(Mq, (64 - 1) / H + 2);  // query rows that 64 rows meet
+  const int64_t n_i = std::min<int64_t>(Mq, (128 - 1) / H + 2);  // query rows that 128 rows meet
   return std::min<int64_t>(2 * NB, (n_sink + 31) / 32 + (window + n_i - 2) / 32 + 2);
 }
 
@@ -421,8 +421,12 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   if ((st = check_tensor(seq_lens, "seq_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (q_lens && (st = check_tensor(q_lens, "q_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (!opts) return bad("opts: null pointer");
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 3; ++i)
     if (opts->reserved[i]) return bad("opts.reserved must be zero");
+  if (opts->row_tile != 0 && opts->row_tile != 64 && opts->row_tile != 128)
+    return bad("opts.row_tile must be 0, 64 or 128");
+  if (opts->row_tile == 128 && ckv_pool->dtype == MLA_DTYPE_MXFP4)
+    return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take 64-row tiles");
   if (opts->window < 0) return bad("opts.window must be >= 0");
   if (opts->n_sink < 0) return bad("opts.n_sink must be >= 0");
   if (opts->n_splits < 0) return bad("opts.n_splits must be >= 0");
@@ -469,8 +473,9 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   // splits are cut on the GPU, out of what each tile's rows see; the plan goes by
   // the most that can be
   const int64_t K = (window_halves(Mq, H, NB, opts->window, opts->n_sink) + 1) / 2;
-  const mla::Planner planner({B, Mq, H, NB, K, false, false, fp8, opts->n_splits, 64, device_cus(),
-                              ckv_pool->dtype == MLA_DTYPE_MXFP4, mla::kWindowList / 2});
+  const bool mx4 = ckv_pool->dtype == MLA_DTYPE_MXFP4;
+  const mla::Planner planner({B, Mq, H, NB, K, false, false, fp8, opts->n_splits, mx4 ? 64 : opts->row_tile,
+                              device_cus(), mx4, mla::kWindowList / 2});
   mla::PartialParams p = common_params(*q_lat, *q_pe, *ckv_pool, *kpe_pool, *block_table, scale, *out_lat, *out_lse, wire);
   p.K = (int32_t)K;
   p.q_jobs = (int32_t)B;

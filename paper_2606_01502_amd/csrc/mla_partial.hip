@@ -751,6 +751,136 @@ __device__ __forceinline__ int compact_tokens(const PartialParams& p, int r, int
   return n_tok;
 }
 
+// Windows (kSelWindow): the tokens that a tile's query rows see.  Row i of request r
+// sits at position pos0 + i of its sequence, i < qn, and sees the tokens t <= its
+// position with t > position - window or t < n_sink.
+struct Window {
+  int n_tok;            // tokens the sequence's table holds
+  int pos0, qn, window;
+  int n_sink;
+  int hi_all, lo_all;   // every row of the tile sees lo_all .. hi_all
+  // of query row i: the last token it sees (-1: none), and the first in its window
+  __device__ __forceinline__ int hi_of(int i) const { return i < qn ? min(pos0 + i, n_tok - 1) : -1; }
+  __device__ __forceinline__ int lo_of(int i) const {
+    return window ? (int)max((int64_t)pos0 + i - window + 1, (int64_t)0) : 0;
+  }
+  // whether some row of the tile may not see all of tokens t0 .. t0 + n - 1
+  __device__ __forceinline__ bool cuts(int t0, int n) const {
+    return t0 + n - 1 > hi_all || (t0 < lo_all && t0 + n - 1 >= n_sink);
+  }
+};
+
+// Of split s, the units of 2^SHIFT tokens (half blocks or blocks) that any of query
+// rows i0 .. i0 + n_i - 1 sees, in order: pool units into list, their first tokens
+// into the place of the row masks.  Those whose table entry names no pool block are
+// left out.  Returns their number.
+template <class L, int SHIFT>
+__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int i0, int n_i, int cap, Window& w,
+                                              LDS uint8_t* smem, int tid) {
+  constexpr bool FP8 = L::kFp8;
+  constexpr int kHalves = SHIFT == 5 ? 1 : 0;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  LDS int* list = (LDS int*)(smem + L::kList);
+  LDS int* first = (LDS int*)(smem + L::kMasks);
+  LDS float* scales = (LDS float*)(smem + L::kScales);
+  LDS int* wave_cnt = (LDS int*)(smem + L::kWaveCnt);
+  const int len = max(p.win_lens[r], 0);
+  w.qn = p.win_qlens ? min(max(p.win_qlens[r], 0), p.Mq) : p.Mq;
+  w.pos0 = len - w.qn;
+  w.window = p.window;
+  w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
+  w.n_sink = p.window ? p.n_sink : 0;
+  const int i1 = i0 + n_i - 1, live = min(i1, w.qn - 1);  // the tile's last row, the last with a query
+  w.hi_all = i1 < w.qn ? w.hi_of(i0) : -1;
+  w.lo_all = w.lo_of(i1);
+  const int hi = live >= i0 ? w.hi_of(live) : -1, lo = w.lo_of(i0);
+  if (hi < 0) return 0;
+  const int u_lo = min(lo, hi) >> SHIFT, u_hi = hi >> SHIFT;
+  const int sinks = (int)min(((int64_t)w.n_sink + (1 << SHIFT) - 1) >> SHIFT, (int64_t)u_lo);
+  const int n_all = sinks + u_hi - u_lo + 1;
+  const int e0 = (int)((int64_t)n_all * s / p.n_splits), e1 = (int)((int64_t)n_all * (s + 1) / p.n_splits);
+  const int n_e = min(e1 - e0, cap);
+  int n_valid = 0;
+  for (int base = 0; base < n_e; base += L::kThreads) {
+    const int e = e0 + base + tid;
+    int b = -1, u = 0;
+    if (base + tid < n_e) {
+      u = e < sinks ? e : u_lo + (e - sinks);
+      const int bb = p.table[r * p.table_s0 + (u >> kHalves)];
+      if (bb >= 0 && bb < p.P) b = bb;
+    }
+    const uint64_t m = __ballot(b >= 0);
+    const int before = __popcll(m & ((1ull << lane) - 1ull));
+    if (lane == 0) wave_cnt[wave] = __popcll(m);
+    lds_barrier();
+    int off = n_valid, total = 0;
+#pragma unroll
+    for (int k = 0; k < L::kThreads / 64; ++k) {
+      const int c = wave_cnt[k];
+      off += (k < wave) ? c : 0;
+      total += c;
+    }
+    if (b >= 0) {
+      list[off + before] = kHalves ? 2 * b + (u & 1) : b;
+      first[off + before] = u << SHIFT;
+      if constexpr (FP8) put_fp8_factors(scales, off + before, p.ckv_scale[b], p.kpe_scale[b]);
+    }
+    n_valid += total;
+    lds_barrier();
+  }
+  return n_valid;
+}
+
+// The loads of a window's block in the 128-row kernel, into the stage layout of
+// issue_load: rows behind the sequence's last token may hold anything, a NaN among
+// it, which a weight of 0 does not take away; the last row there is stands in for
+// them.
+template <bool FP8>
+struct WinIssue {
+  using L = Layout<FP8>;
+  const uint8_t* ckv;  // the block
+  const uint8_t* kpe;
+  uint32_t buf;        // LDS address of the stage
+  int last;            // the block's last row that the sequence holds
+  __device__ __forceinline__ void aim(const PartialParams& p, int b_in, int first, int n_tok, LDS uint8_t* stage) {
+    const int64_t b = __builtin_amdgcn_readfirstlane(b_in);
+    ckv = p.ckv + b * L::kStageCkv;
+    kpe = p.kpe + b * (L::kStage - L::kStageCkv);
+    buf = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)stage);
+    last = min(kBlock - 1, n_tok - 1 - __builtin_amdgcn_readfirstlane(first));
+  }
+  __device__ __forceinline__ void load(int j, int wave, int lane_in) const {
+    int lane;
+    asm volatile("v_mov_b32 %0, %1" : "=v"(lane) : "v"(lane_in));
+    uint32_t off, dst;
+    const uint8_t* base = ckv;
+    if constexpr (!FP8) {
+      if (j < 16) {
+        const int t = 16 * wave + j;
+        off = (((uint32_t)lane ^ (uint32_t)bf16_key(j)) << 4) + ((uint32_t)min(t, last) << 10);
+        dst = (uint32_t)(t * 1024);
+      } else {
+        const int k = wave * 2 + (j - 16), t = 8 * k + (lane >> 3);
+        off = (uint32_t)(min(t, last) * 128) + (uint32_t)((((lane & 7) ^ ((t >> 1) & 7))) << 4);
+        dst = (uint32_t)(L::kStageCkv + k * 1024);
+        base = kpe;
+      }
+    } else if (j < 8) {
+      const int k = wave * 8 + j, t = 2 * k + (lane >> 5);
+      off = (uint32_t)min(t, last) * 512u + (uint32_t)(((lane & 31) ^ fp8_key(t)) << 4);
+      dst = (uint32_t)(k * 1024);
+    } else {
+      const int t = 16 * wave + (lane >> 2);
+      off = (uint32_t)min(t, last) * 64u + (uint32_t)(((lane & 3) ^ fp8_rope_key(t)) << 4);
+      dst = (uint32_t)(L::kStageCkv + wave * 1024);
+      base = kpe;
+    }
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(buf + dst)) : "memory", "m0");
+  }
+};
+
 // ---- the 128-row kernel, and the 64-row one of long per-row lists.
 //
 // RG row groups of 16 per wave: wave w computes rows 16*RG*w .. 16*RG*(w+1)-1
@@ -771,12 +901,13 @@ void partial_kernel(const PartialParams p) {
   constexpr bool FP8 = KV != kKvBf16;
   constexpr bool PR = SEL == kSelPerRow;   // a block selection per query row
   constexpr bool TOK = SEL == kSelTokens;  // token selections, 64 to a virtual block
+  constexpr bool WIN = SEL == kSelWindow;  // no selection: the tokens each row sees
   constexpr bool kSplitScales = KV == kKvFp8Split;
   using L = Layout<FP8>;
   constexpr int kTau4 = kBlock / 16;   // 16-token tiles per block
   constexpr int kKSteps = kBlock / 32;  // 32-token PV k-steps per block
   constexpr int kRowsWg = 64 * RG;
-  __shared__ __attribute__((aligned(16))) uint8_t smem_raw[PR ? L::kTotalPerRow : L::kTotal];
+  __shared__ __attribute__((aligned(16))) uint8_t smem_raw[PR || WIN ? L::kTotalPerRow : L::kTotal];
   LDS uint8_t* smem = (LDS uint8_t*)smem_raw;
   LDS uint8_t* const stage0 = smem;
 
@@ -829,7 +960,7 @@ void partial_kernel(const PartialParams p) {
   // (split s takes blocks s, s + S, ... from every slot), so that rows which
   // chose one block in different slots share its load, or by slot range when
   // a tile's slots may not fit one list
-  const int n_i = PR ? div_by(min((rt + 1) * kRowsWg, p.rows) - 1, p.by_H) - i0 + 1 : 1;
+  const int n_i = PR || WIN ? div_by(min((rt + 1) * kRowsWg, p.rows) - 1, p.by_H) - i0 + 1 : 1;
   const int c_slot0 = PR && p.split_by_id ? 0 : slot0;
   const int c_nslots = PR && p.split_by_id ? p.K : nslots;
   // the slot id this thread compacts first
@@ -839,7 +970,7 @@ void partial_kernel(const PartialParams p) {
       const int ii = p.split_by_id ? div_by(tid, p.by_K) : tid / c_nslots, j = tid - ii * c_nslots;
       first_id = p.sel[r * p.sel_s0 + (int64_t)(i0 + ii) * p.sel_s1 + c_slot0 + j];
     }
-  } else {
+  } else if constexpr (!WIN) {
     if (tid < nslots) first_id = p.sel[r * p.sel_s0 + slot0 + tid];
   }
 
@@ -869,7 +1000,10 @@ void partial_kernel(const PartialParams p) {
   // per-row selections: the union over the tile's query rows, with row masks)
   int n_valid;
   int n_tok = 0;  // token selections: the listed tokens (n_valid counts virtual blocks)
-  if constexpr (PR) {
+  Window win{};
+  if constexpr (WIN) {
+    n_valid = compact_window<L, 6>(p, r, s_idx, i0, n_i, L::kPerRowCap, win, smem, tid);
+  } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                    p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
                                    masks, tid);
@@ -899,6 +1033,13 @@ void partial_kernel(const PartialParams p) {
 #pragma unroll
       for (int j = 0; j < L::kLoads; ++j) ti.load(p, j, wave, lane);
     }
+  } else if constexpr (WIN) {
+    for (int h = 0; h < n_valid && h < L::kLead; ++h) {
+      WinIssue<FP8> wi;
+      wi.aim(p, list[h], ((LDS const int*)(smem + L::kMasks))[h], win.n_tok, stage0 + h * L::kStage);
+#pragma unroll
+      for (int j = 0; j < L::kLoads; ++j) wi.load(j, wave, lane);
+    }
   } else {
     for (int h = 0; h < n_valid && h < L::kLead; ++h)
       issue_stage<FP8>(p, list[h], stage0 + h * L::kStage, wave, lane);
@@ -919,9 +1060,14 @@ void partial_kernel(const PartialParams p) {
   // per-row selections: the bit of each of the lane's rows in the entry masks
   // (rows past the end of the job are never stored; any bit will do)
   int row_bit[RG];
+  int hi_row[RG], lo_row[RG];  // windows: what the lane's rows see
 #pragma unroll
   for (int rg = 0; rg < RG; ++rg) {
     const int row = row_wg0 + wave * 16 * RG + rg * 16 + n16;
+    if constexpr (WIN) {
+      hi_row[rg] = win.hi_of(div_by(row, p.by_H));
+      lo_row[rg] = win.lo_of(div_by(row, p.by_H));
+    }
     row_bit[rg] = PR ? min(max(div_by(row, p.by_H) - i0, 0), 63) : 0;
   }
 #pragma unroll
@@ -947,6 +1093,13 @@ void partial_kernel(const PartialParams p) {
       const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(m >> 32));
       const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)m);
       emask = ((uint64_t)hi << 32) | (uint64_t)lo;
+    }
+    int t_first = 0;  // windows: the block's first token
+    WinIssue<FP8> wi{};
+    if constexpr (WIN) {
+      LDS const int* const first = (LDS const int*)(smem + L::kMasks);
+      t_first = __builtin_amdgcn_readfirstlane(first[h]);
+      if (b_next >= 0) wi.aim(p, b_next, first[hn], win.n_tok, stage0 + (hn % L::kNum) * L::kStage);
     }
     __builtin_amdgcn_sched_barrier(0);
     // fp8: the scores are accumulated as ratio * (q_pe . kpe codes) +
@@ -1111,6 +1264,8 @@ void partial_kernel(const PartialParams p) {
                 ti.tok = list[hn * kBlock + 16 * wave + (lane & 15)];
                 ti.buf = (uint32_t)(uintptr_t)next_buf;
                 ti.load(p, step >> 1, wave, lane);
+              } else if constexpr (WIN) {
+                wi.load(step >> 1, wave, lane);
               } else {
                 issue_load<true>(p, b_next, next_buf, wave, lane, step >> 1);
               }
@@ -1138,8 +1293,13 @@ void partial_kernel(const PartialParams p) {
           // after the products of tile t (RG = 2) or tile t itself (RG = 1):
           // the read of tile t of step + 2; then the two loads
           if (rg == RG - 1 && step + 2 < 18) key_frag(step + 2, tau, kr[(step + 2) % 3][tau]);
-          if (step < 9 && b_next >= 0 && j == kPer - 3) bi.load(p, 2 * step, wave, lane);
-          if (step < 9 && b_next >= 0 && j == kPer - 2) bi.load(p, 2 * step + 1, wave, lane);
+          if constexpr (WIN) {
+            if (step < 9 && b_next >= 0 && j == kPer - 3) wi.load(2 * step, wave, lane);
+            if (step < 9 && b_next >= 0 && j == kPer - 2) wi.load(2 * step + 1, wave, lane);
+          } else {
+            if (step < 9 && b_next >= 0 && j == kPer - 3) bi.load(p, 2 * step, wave, lane);
+            if (step < 9 && b_next >= 0 && j == kPer - 2) bi.load(p, 2 * step + 1, wave, lane);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
         }
@@ -1196,6 +1356,14 @@ void partial_kernel(const PartialParams p) {
           for (int k = 0; k < 4; ++k)
             if (16 * tau + 4 * lg + k >= n_here) acc[rg][tau][k] = -INFINITY;
         }
+        if constexpr (WIN) {
+          if (win.cuts(t_first, kBlock)) {
+            const int t = t_first + 16 * tau + 4 * lg;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (t + k > hi_row[rg] || (t + k < lo_row[rg] && t + k >= win.n_sink)) acc[rg][tau][k] = -INFINITY;
+          }
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) bm = fmaxf(bm, acc[rg][tau][k]);
       }
@@ -1236,8 +1404,10 @@ void partial_kernel(const PartialParams p) {
     auto p_pair = [&](int rg, int tau, int k0) {
       // (an exact 0 for rows that do not attend this entry, also before
       // their first attended entry, when m_run is still -inf)
-      float e0 = __builtin_amdgcn_exp2f(acc[rg][tau][k0] - m_run[rg]);
-      float e1 = __builtin_amdgcn_exp2f(acc[rg][tau][k0 + 1] - m_run[rg]);
+      // (windows: a score of -inf weighs 0 also while the maximum is -inf)
+      const float m = WIN ? fmaxf(m_run[rg], -3.4e38f) : m_run[rg];
+      float e0 = __builtin_amdgcn_exp2f(acc[rg][tau][k0] - m);
+      float e1 = __builtin_amdgcn_exp2f(acc[rg][tau][k0 + 1] - m);
       if constexpr (PR) {
         e0 = on[rg] ? e0 : 0.f;
         e1 = on[rg] ? e1 : 0.f;
@@ -1586,81 +1756,6 @@ __device__ __forceinline__ float xor32_max(float v) {
   const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
-// Windows (kSelWindow): the tokens that a tile's query rows see, as half blocks.
-// Row i of request r sits at position pos = len - qn + i of its sequence and sees
-// the tokens t <= pos with t > pos - window or t < n_sink.
-struct Window {
-  int n_tok;            // tokens the sequence's table holds
-  int hi_row, lo_row;   // of the lane's row: the last token it sees, the first in its window
-  int hi_all, lo_all;   // every row sees lo_all .. hi_all
-  int n_sink;
-};
-
-// The half blocks of split s (of S) that any row of query rows i0 .. i0 + n_i - 1
-// sees, in order: pool half blocks into list, their first tokens into first.  Those
-// whose table entry names no pool block are left out.  Returns their number.
-template <class L>
-__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int i0, int n_i, int i_lane,
-                                              Window& w, LDS uint8_t* smem, int tid) {
-  constexpr bool FP8 = L::kFp8;
-  const int lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  LDS int* list = (LDS int*)(smem + L::kList);
-  LDS int* first = (LDS int*)(smem + L::kMasks);
-  LDS float* scales = (LDS float*)(smem + L::kScales);
-  LDS int* wave_cnt = (LDS int*)(smem + L::kWaveCnt);
-  const int len = max(p.win_lens[r], 0);
-  const int qn = p.win_qlens ? min(max(p.win_qlens[r], 0), p.Mq) : p.Mq;
-  w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
-  w.n_sink = p.window ? p.n_sink : 0;
-  const int pos0 = len - qn;  // of query row 0
-  // (window 0: all tokens up to the row's own)
-  auto lo_of = [&](int pos) { return p.window ? (int)max((int64_t)pos - p.window + 1, (int64_t)0) : 0; };
-  auto hi_of = [&](int pos) { return min(pos, w.n_tok - 1); };
-  const bool on = i_lane < qn;
-  w.hi_row = on ? hi_of(pos0 + i_lane) : -1;
-  w.lo_row = lo_of(pos0 + i_lane);
-  const int i1 = i0 + n_i - 1, live = min(i1, qn - 1);  // the tile's last row, the last with a query
-  w.hi_all = i1 < qn ? hi_of(pos0 + i0) : -1;
-  w.lo_all = lo_of(pos0 + i1);
-  const int hi = live >= i0 ? hi_of(pos0 + live) : -1, lo = lo_of(pos0 + i0);
-  if (hi < 0) return 0;
-  const int b_lo = min(lo, hi) >> 5, b_hi = hi >> 5;
-  const int sinks = min((int)min(((int64_t)w.n_sink + 31) >> 5, (int64_t)b_lo), b_hi + 1);
-  const int n_all = sinks + b_hi - b_lo + 1;
-  const int e0 = (int)((int64_t)n_all * s / p.n_splits), e1 = (int)((int64_t)n_all * (s + 1) / p.n_splits);
-  const int n_e = min(e1 - e0, L::kCap);
-  int n_valid = 0;
-  for (int base = 0; base < n_e; base += L::kThreads) {
-    const int e = e0 + base + tid;
-    int b = -1, h = 0;
-    if (base + tid < n_e) {
-      h = e < sinks ? e : b_lo + (e - sinks);
-      const int bb = p.table[r * p.table_s0 + (h >> 1)];
-      if (bb >= 0 && bb < p.P) b = bb;
-    }
-    const uint64_t m = __ballot(b >= 0);
-    const int before = __popcll(m & ((1ull << lane) - 1ull));
-    if (lane == 0) wave_cnt[wave] = __popcll(m);
-    lds_barrier();
-    int off = n_valid, total = 0;
-#pragma unroll
-    for (int k = 0; k < L::kThreads / 64; ++k) {
-      const int c = wave_cnt[k];
-      off += (k < wave) ? c : 0;
-      total += c;
-    }
-    if (b >= 0) {
-      list[off + before] = 2 * b + (h & 1);
-      first[off + before] = h << 5;
-      if constexpr (FP8) put_fp8_factors(scales, off + before, p.ckv_scale[b], p.kpe_scale[b]);
-    }
-    n_valid += total;
-    lds_barrier();
-  }
-  return n_valid;
-}
-
 // Swizzles of a 64-row tile's stages (16-byte chunk c of latent row t in slot
 // c ^ key32(t), of RoPE row t in slot c ^ rope_key32(t)).  A key read takes
 // chunk 4 i + g of token 16 th + n for lane (n, g); the LDS serves 16 lanes of
@@ -1984,8 +2079,12 @@ void tile64_kernel(const PartialParams p) {
   int n_valid;
   int n_tok = 0;
   Window win{};
+  int hi_row = -1, lo_row = 0;  // of the lane's score row
   if constexpr (WIN) {
-    n_valid = compact_window<L>(p, r, s_idx, i0, n_i, div_by(row_wg0 + 16 * rq + n16, p.by_H), win, smem, tid);
+    n_valid = compact_window<L, 5>(p, r, s_idx, i0, n_i, L::kCap, win, smem, tid);
+    const int i_row = div_by(row_wg0 + 16 * rq + n16, p.by_H);
+    hi_row = win.hi_of(i_row);
+    lo_row = win.lo_of(i_row);
   } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                  p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
@@ -2199,11 +2298,11 @@ void tile64_kernel(const PartialParams p) {
     if constexpr (WIN) {
       // stages that every row sees whole, most of a long window, go unmasked
       const int t0 = __builtin_amdgcn_readfirstlane(s_first);
-      if (t0 + 31 > win.hi_all || (t0 < win.lo_all && t0 + 31 >= win.n_sink)) {
+      if (win.cuts(t0, 32)) {
         const int t = t0 + 16 * th + 4 * g;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (t + k > win.hi_row || (t + k < win.lo_row && t + k >= win.n_sink)) s[k] = -INFINITY;
+          if (t + k > hi_row || (t + k < lo_row && t + k >= win.n_sink)) s[k] = -INFINITY;
       }
     }
     return s;
@@ -2713,13 +2812,19 @@ static void launch_items(Kernel kernel, PartialParams p, int items, int threads,
   }
 }
 
-// 64-row tiles only: windows and 4-bit caches
+// 64-row tiles: 4-bit caches, and windows of others
 template <int KV, int SEL>
 static void launch_tile64(const PartialParams& p, int grid, hipStream_t s) {
   if (p.rows <= 32)
     launch_items(tile64_kernel<KV, SEL, 1>, p, grid, 512, s);
   else
     launch_items(tile64_kernel<KV, SEL, 2>, p, grid, 512, s);
+}
+
+template <int KV>
+static void launch_window(const PartialParams& p, int grid, int row_groups, hipStream_t s) {
+  if (row_groups == 2) return launch_items(partial_kernel<2, KV, kSelWindow>, p, grid, 256, s);
+  launch_tile64<KV, kSelWindow>(p, grid, s);
 }
 
 template <int KV, int SEL = kSelShared>
@@ -2742,11 +2847,11 @@ hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups,
     if (kv == kKvMx4)
       launch_tile64<kKvMx4, kSelWindow>(p, grid, s);
     else if (kv == kKvFp8Shared)
-      launch_tile64<kKvFp8Shared, kSelWindow>(p, grid, s);
+      launch_window<kKvFp8Shared>(p, grid, row_groups, s);
     else if (kv == kKvFp8Split)
-      launch_tile64<kKvFp8Split, kSelWindow>(p, grid, s);
+      launch_window<kKvFp8Split>(p, grid, row_groups, s);
     else
-      launch_tile64<kKvBf16, kSelWindow>(p, grid, s);
+      launch_window<kKvBf16>(p, grid, row_groups, s);
   } else if (kv == kKvMx4) {
     launch_tile64<kKvMx4, kSelShared>(p, grid, s);
   } else if (sel_kind == kSelPerRow) {

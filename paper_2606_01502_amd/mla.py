@@ -84,7 +84,8 @@ OUT_FP32, OUT_BF16_WIRE = 0, 1
 
 class WindowOpts(ctypes.Structure):
     _fields_ = [("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_splits", ctypes.c_int32),
-                ("out_format", ctypes.c_int32), ("reserved", ctypes.c_int32 * 4)]
+                ("out_format", ctypes.c_int32), ("row_tile", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 3)]
 
 
 class RopeOpts(ctypes.Structure):
@@ -322,12 +323,13 @@ def sparse_partial_attn(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_
 
 def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
                    q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None,
-                   n_splits=0, stream=None, wire=False):
+                   n_splits=0, stream=None, wire=False, row_tile=0):
     """window_attn with every argument fixed (see prepare_partial)."""
     out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
     _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, *out, ckv_scale,
                     kpe_scale)
-    o = WindowOpts(int(window), int(n_sink), int(n_splits), OUT_BF16_WIRE if wire else OUT_FP32)
+    o = WindowOpts(int(window), int(n_sink), int(n_splits), OUT_BF16_WIRE if wire else OUT_FP32,
+                   int(row_tile))
     d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale),
          describe(kpe_pool, kpe_scale), describe(block_table), describe(seq_lens), describe(q_lens))
     do = tuple(describe(t) for t in out)
@@ -340,7 +342,7 @@ def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale
 
 def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
                 q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None, n_splits=0,
-                stream=None, wire=False):
+                stream=None, wire=False, row_tile=0):
     """Attention of each request's last q_lens[b] tokens (default: all Mq query
     rows) over its paged sequence of seq_lens[b] tokens, each row seeing the
     last `window` tokens up to its own (0: all) and the first n_sink.  Pools
@@ -349,7 +351,7 @@ def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, w
     either form, for merge_partials or as they are."""
     return prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window,
                           n_sink, q_lens, out_lat, out_lse, ckv_scale, kpe_scale, n_splits, stream,
-                          wire)()
+                          wire, row_tile)()
 
 
 def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=None,

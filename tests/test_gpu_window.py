@@ -253,3 +253,64 @@ def test_no_rows():
     assert out.shape == (2, 0, 4, 512)
     out, lse = run(c, ql, qp, table[:, :0], [5, 6])  # a table of no blocks
     assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+# ---------------------------------------------------------------- both tiles
+@pytest.mark.parametrize("tile", [64, 128])
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "fp8split"])
+def test_both_tiles(kv, tile):
+    """128-row tiles take whole blocks, 64-row tiles half blocks: windows, sinks
+    and ends around both, ragged rows, splits."""
+    print(f"case: tiles {kv} {tile}", flush=True)
+    c, ql, qp, table = inputs(121, 3, 9, 40, 7, kv)
+    lens, q_lens = [440, 60, 129], [9, 3, 7]
+    for window, sinks in ((0, 0), (1, 0), (33, 1), (64, 64), (65, 33), (300, 70), (2 ** 31 - 1, 2 ** 31 - 1)):
+        check(c, ql, qp, table, lens, q_lens, window=window, n_sink=sinks, row_tile=tile)
+    check(c, ql, qp, table, lens, q_lens, window=200, n_sink=4, row_tile=tile, n_splits=3, wire=True)
+    check(c, ql, qp, table, lens, row_tile=tile, wire=True)
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 193, 256])
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_lengths_in_128_row_tiles(kv, n):
+    print(f"case: length 128 {kv} {n}", flush=True)
+    c, ql, qp, table = inputs(n, 1, 2, 70, 4, kv)
+    check(c, ql, qp, table, [n], row_tile=128)
+    check(c, ql, qp, table, [n], row_tile=128, n_splits=3)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "fp8split"])
+def test_garbage_in_128_row_tiles(kv):
+    """What lies behind a sequence, in padding rows and in blocks a window has let
+    go of, in 128-row tiles."""
+    print(f"case: garbage 128 {kv}", flush=True)
+    c, ql, qp, table = inputs(131, 3, 6, 30, 4, kv)
+    lens, q_lens = [71, 256, 130], [6, 2, 4]
+    kw = dict(window=60, n_sink=2, row_tile=128)
+    want = run(c, ql, qp, table, lens, q_lens, **kw)
+    check(c, ql, qp, table, lens, q_lens, **kw)
+    for b in range(3):
+        for t in range(lens[b], 256):
+            c.ckv[table[b, t // 64], t % 64] = {"bf16": torch.nan, "fp8": 0x7F, "fp8split": 0xFF}[kv]
+            c.kpe[table[b, t // 64], t % 64] = torch.inf if kv == "bf16" else 0x7F
+        ql[b, q_lens[b]:] = torch.nan
+        qp[b, q_lens[b]:] = torch.inf
+    t2 = table.copy()
+    t2[1, 1], t2[1, 2] = -1, 10 ** 6
+    for tab in (table, t2):
+        got = run(c, ql, qp, tab, lens, q_lens, **kw)
+        assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    bad = table.copy()
+    bad[0, 1], bad[2, 0] = -1, c.lat.shape[0]
+    got = run(c, ql, qp, bad, lens, q_lens, row_tile=128)
+    assert torch.isfinite(got[0]).all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8split"])
+def test_long_and_many_tiles_of_128_rows(kv):
+    print(f"case: long 128 {kv}", flush=True)
+    c, ql, qp, table = inputs(141, 1, 2, 65, 600, kv)
+    check(c, ql, qp, table, [600 * 64 - 13], n_splits=1, row_tile=128)
+    c, ql, qp, table = inputs(142, 1, 300, 16, 10, kv)
+    check(c, ql, qp, table, [600], window=129, n_sink=4, rows=range(0, 300, 17), row_tile=128)
+    check(c, ql, qp, table, [300], rows=range(0, 300, 29), row_tile=128)

@@ -272,7 +272,7 @@ def wopts(**kw):
     o = mla.WindowOpts(64, 4, 0, 0)
     for k, v in kw.items():
         if k == "reserved":
-            o.reserved[3] = v
+            o.reserved[2] = v
         else:
             setattr(o, k, v)
     return o
@@ -308,6 +308,8 @@ WINDOW = [
     ("n_sink", dict(opts=wopts(n_sink=-1)), INVALID, "n_sink"),
     ("n_splits", dict(opts=wopts(n_splits=-1)), INVALID, "n_splits"),
     ("out_format", dict(opts=wopts(out_format=2)), INVALID, "out_format"),
+    ("row_tile", dict(opts=wopts(row_tile=96)), INVALID, "row_tile"),
+    ("128 rows of a 4-bit cache", dict(ckv=z(8, 64, 272, dt=U8), opts=wopts(row_tile=128)), UNSUPPORTED, "64-row"),
     ("reserved", dict(opts=wopts(reserved=1)), INVALID, "reserved"),
     ("table too wide", dict(table=z(2, 1, dt=I32).expand(2, 2 ** 25 + 1)), INVALID, "innermost"),
 ]
