@@ -2711,8 +2711,14 @@ void tile64_kernel(const PartialParams p) {
   // swaps between lanes l, l ^ 16 (and l, l ^ 32 for 16-bit rows) give each
   // store instruction 64-byte runs of 16 rows: row 16 j + (lane & 15) of half k.
   const int q = lane >> 4;
-  // 4 bits: the column that slot 8 wave + c / 8 of a converted row holds
-  auto col_of = [&](int c) { return 8 * mx4_chunk(8 * wave + (c >> 3)) + (c & 7); };
+  // 4 bits: the wave's columns c .. c + 7 are 8 neighbours, but its next eight lie 32
+  // columns on (mx4_chunk).  The rows are put together in LDS, where the stages were
+  // (16-byte chunk c of row t in slot c ^ (t & 15)), and stored whole: stored from
+  // here, 16 bytes at a time, 256 tiles of 64 wire rows took 2.7 us longer.
+  auto put_row = [&](int t, int c, int bytes, u32x4_t u) {
+    const int chunk = bytes == 1024 ? mx4_chunk(8 * wave + (c >> 3)) : 2 * mx4_chunk(8 * wave + (c >> 3)) + ((c >> 2) & 1);
+    *(LDS u32x4_t*)(smem + t * bytes + ((chunk ^ (t & 15)) << 4)) = u;
+  };
 #pragma unroll
   for (int k = 0; k < NK; ++k) {
     // the element offsets of this lane's two rows
@@ -2761,11 +2767,10 @@ void tile64_kernel(const PartialParams p) {
           u[1][e] = s[1];
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (ok[j]) {
-            if constexpr (MX4) *(u32x4_t*)(dst + off[j] + col_of(32 * d + 16 * (q & 1) + 8 * (q >> 1))) = u[j];
-            else *(u32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * (q & 1) + 8 * (q >> 1)) = u[j];
-          }
+        for (int j = 0; j < 2; ++j) {
+          if constexpr (MX4) put_row(32 * k + 16 * j + (lane & 15), 32 * d + 16 * (q & 1) + 8 * (q >> 1), 1024, u[j]);
+          else if (ok[j]) *(u32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * (q & 1) + 8 * (q >> 1)) = u[j];
+        }
       }
     } else {
       float* const dst = direct ? p.out : p.ws_o32;
@@ -2783,12 +2788,34 @@ void tile64_kernel(const PartialParams p) {
             u[1][e] = __uint_as_float(s[1]);
           }
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            if (ok[j]) {
-              if constexpr (MX4) *(f32x4_t*)(dst + off[j] + col_of(32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1))) = u[j];
-              else *(f32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1)) = u[j];
-            }
+          for (int j = 0; j < 2; ++j) {
+            if constexpr (MX4) put_row(32 * k + 16 * j + (lane & 15), 32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1), 2048,
+                                       __builtin_bit_cast(u32x4_t, u[j]));
+            else if (ok[j]) *(f32x4_t*)(dst + off[j] + 64 * wave + 32 * d + 16 * b + 8 * (q & 1) + 4 * (q >> 1)) = u[j];
+          }
         }
+      }
+    }
+  }
+  if constexpr (MX4) {
+    static_assert(64 * 2048 <= L::kList, "the output rows fit the stages");
+    lds_barrier();
+    const bool b16 = half || (direct && p.out_wire);
+    uint8_t* const dst = b16 ? (uint8_t*)(half ? p.ws_o16 : p.out16) : (uint8_t*)(direct ? p.out : p.ws_o32);
+    // wave w stores rows 4 NK w .. of the tile, 1 KiB an instruction
+#pragma unroll
+    for (int k = 0; k < 4 * NK; ++k) {
+      const int t = 4 * NK * wave + k, row = row_wg0 + t;
+      if (row >= p.rows) break;
+      const int i = div_by(row, p.by_H), hd = row - i * p.H;
+      const int64_t off = direct ? r * p.out_s0 + i * p.out_s1 + hd * p.out_s2 : (part * p.rows + row) * kDLat;
+      if (b16) {
+        *(u32x4_t*)(dst + 2 * off + 16 * lane) = *(const LDS u32x4_t*)(smem + t * 1024 + ((lane ^ (t & 15)) << 4));
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          *(u32x4_t*)(dst + 4 * off + 1024 * c + 16 * lane) =
+              *(const LDS u32x4_t*)(smem + t * 2048 + (((64 * c + lane) ^ (t & 15)) << 4));
       }
     }
   }
