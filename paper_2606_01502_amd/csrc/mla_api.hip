@@ -475,7 +475,7 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   const int64_t K = (window_halves(Mq, H, NB, opts->window, opts->n_sink) + 1) / 2;
   const bool mx4 = ckv_pool->dtype == MLA_DTYPE_MXFP4;
   const mla::Planner planner({B, Mq, H, NB, K, false, false, fp8, opts->n_splits, mx4 ? 64 : opts->row_tile,
-                              device_cus(), mx4, mla::kWindowList / 2});
+                              device_cus(), mx4, true});
   mla::PartialParams p = common_params(*q_lat, *q_pe, *ckv_pool, *kpe_pool, *block_table, scale, *out_lat, *out_lse, wire);
   p.K = (int32_t)K;
   p.q_jobs = (int32_t)B;

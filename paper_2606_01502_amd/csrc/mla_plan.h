@@ -18,8 +18,8 @@ struct PlanArgs {
   bool tokens, per_row, fp8;
   int32_t n_splits, row_tile;
   int64_t cus;
-  bool mx4 = false;  // a 4-bit cache
-  int64_t list = 0;  // entries one split's list holds (0: by the selection)
+  bool mx4 = false;     // a 4-bit cache
+  bool window = false;  // no selection: K is the blocks that a tile's rows may see
 };
 
 struct Plan {
@@ -113,7 +113,7 @@ struct Planner {
 
   // entries one split's list holds (per-row selections with an fp8 cache: a
   // shorter one, see the kernel's LDS layout)
-  int64_t list_cap() const { return a.list ? a.list : a.per_row && a.fp8 ? kPerRowListShort : kMaxSlotsPerSplit; }
+  int64_t list_cap() const { return a.window ? kWindowList / 2 : a.per_row && a.fp8 ? kPerRowListShort : kMaxSlotsPerSplit; }
   // per-row selections whose tile slots all fit one list split by logical
   // block: every split then scans all slots and the rows that chose a block
   // in different slots still share its load
@@ -133,6 +133,10 @@ struct Planner {
       q.sps = std::max<int64_t>(64, ((a.K + S - 1) / S + 63) / 64 * 64);
       q.sps = std::min<int64_t>(q.sps, kMaxSlotsPerSplit);
       q.S = std::max<int64_t>(1, (a.K + q.sps - 1) / q.sps);
+    } else if (a.window) {
+      // (split on the GPU, evenly: any number of splits goes)
+      q.S = std::max<int64_t>(S, (a.K + cap - 1) / cap);
+      q.sps = std::max<int64_t>(1, (a.K + q.S - 1) / q.S);
     } else if (!q.by_id) {
       S = std::max<int64_t>(S, (a.K * tile_qrows + cap - 1) / cap);
       q.sps = std::max<int64_t>(1, (a.K + S - 1) / S);
@@ -149,7 +153,8 @@ struct Planner {
     // bytes are left out.  Fitted to 140000 timed plans of 28000 calls of 1..700
     // jobs of 8..256 rows x 1..1500 blocks or 16..6000 tokens (9 % rms in 128-row
     // tiles, 9 to 17 % in 64-row ones).
-    const double blocks = q.by_id ? (double)((most_blocks() + q.S - 1) / q.S)
+    const double blocks = a.window ? (double)((2 * a.K + q.S - 1) / q.S) / 2
+                        : q.by_id ? (double)((most_blocks() + q.S - 1) / q.S)
                         : a.tokens ? (double)((q.sps + 63) / 64)
                         : a.per_row ? (double)std::min<int64_t>(std::max<int64_t>(a.NB, 1), q.sps * tile_qrows)
                         : (double)q.sps;
@@ -163,17 +168,47 @@ struct Planner {
          {{6.6, 1.87, 5.5e6}, {9.4, 2.32, 5.5e6}, {9.4, 2.30, 5.5e6}, {14.1, 4.16, 5.5e6}}},
         {{{5.0, 1.99, 6.6e6}, {7.8, 2.19, 6.1e6}, {8.5, 2.17, 8.7e6}, {14.2, 3.78, 5.0e6}},
          {{5.7, 2.38, 5.5e6}, {8.4, 2.64, 5.5e6}, {9.2, 2.49, 5.5e6}, {14.5, 4.89, 5.5e6}}}};
-    const Rate& rate = kRate[a.tokens][a.fp8][rg == 2 ? 3 : rows <= 32 ? 0 : rows <= 64 ? 1 : 2];
+    // 4-bit caches: 64-row tiles only, fitted to 256 work items of 2 .. 64 blocks
+    static constexpr Rate kRateMx4[3] = {{6.6, 2.1, 5.5e6}, {11.0, 2.45, 5.5e6}, {11.0, 2.3, 5.5e6}};
+    const int kind = rg == 2 ? 3 : rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
+    const Rate& rate = a.mx4 && kind < 3 ? kRateMx4[kind] : kRate[a.tokens][a.fp8][kind];
     // (rows with selections of their own share blocks, nobody here knows which)
     const double token_bytes = a.mx4 ? kMx4Row + 2 * kDPe : (kDLat + kDPe) * (a.fp8 ? 1 : 2);
-    const double item_bytes = a.per_row ? 0.0 : blocks * kBlock * token_bytes;
+    // (a window's row tiles see much the same blocks, side by side on one XCD)
+    const double item_bytes = a.per_row ? 0.0 : blocks * kBlock * token_bytes / (a.window && q.row_tiles > 1 ? 2 : 1);
     auto wave_us = [&](int64_t items) {
       return rate.fixed + std::max(blocks * rate.block, (double)items * item_bytes / rate.bytes);
     };
     const int64_t items = a.R * q.row_tiles * q.S, rest = items % a.cus;
     q.us = (double)(items / a.cus) * wave_us(a.cus) + (rest ? wave_us(rest) : 0.0);
     if (q.S > 1) q.us += 1.8 + 0.4e-6 * (double)ws_rows_bytes(q.S);
+    // a row's splits are read one trip after another: 48 rows in 16, 32 and 64
+    // splits 15.1, 20.0 and 26.5 us
+    if (a.window && q.S > 8) q.us += 0.2 * (double)(q.S - 8);
     return q;
+  }
+
+  // Windows are short, and often few: the cheapest of a few split counts up to one
+  // block a split, and of those that fill one, two or three waves.  One 16-row
+  // request with a window of 512 tokens: 14.5 us in the covering three splits, 11.6
+  // in nine; of 2000 tokens 15.1 in twelve, 20.9 in five.
+  Plan choose_window() const {
+    static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
+    const int64_t most = std::max<int64_t>(a.K, 1);
+    Plan plan = cover;
+    for (int rg = 1; rg <= 2; ++rg) {
+      if (row_groups && rg != row_groups) continue;
+      const int64_t units = std::max<int64_t>(a.R * row_tiles_of(rg), 1);
+      auto offer = [&](int64_t S) {
+        const Plan q = plan_of(rg, S);
+        if (fits(plan) && !fits(q)) return;
+        if ((fits(q) && !fits(plan)) || q.us < plan.us) plan = q;
+      };
+      for (int64_t S : kCounts)
+        if (S <= most && S * units <= 3 * a.cus) offer(S);
+      for (int waves = 1; waves <= 3; ++waves) offer(std::max<int64_t>(1, std::min<int64_t>(waves * a.cus / units, most)));
+    }
+    return plan;
   }
 
   Plan choose() const {
@@ -207,6 +242,7 @@ struct Planner {
     // blocks each: 268 us in four ranges, priced cheaper, 241 in the covering
     // five).
     plan = cover;
+    if (a.window) return choose_window();
     if (a.per_row && tile_qrows > 1 && !by_id()) return plan;
     double best = 0.97 * cover.us;
     for (int rg = 1; rg <= 2; ++rg) {
