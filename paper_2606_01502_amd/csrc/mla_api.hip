@@ -251,6 +251,9 @@ mla_status_t enqueue(const mla::Planner& planner, mla::PartialParams& p, int64_t
   p.by_splits = mla::make_div(S);
   p.by_tiles = mla::make_div(row_tiles);
   p.by_rep = mla::make_div(p.q_rep);
+  // windows: a tile's splits, and 16 items' worth of tiles, next to each other
+  p.run = (int32_t)(S * std::max<int64_t>(1, 16 / S));
+  p.by_run = mla::make_div(p.run);
   p.by_K = mla::make_div(std::max<int64_t>(p.K, 1));
   if (S > 1) {
     const size_t n_part_rows = (size_t)R * S * p.rows;

@@ -100,6 +100,10 @@ struct PartialParams {
   const int32_t* win_lens;
   const int32_t* win_qlens;
   int32_t window, n_sink;
+  // windows: work items next to each other that one XCD takes, and the grid's
+  // part that goes in whole rounds of them (see window_item)
+  int32_t run, run_all;
+  Div by_run;
 };
 
 // Combine of the S split partials of every job into the caller's outputs.

@@ -770,6 +770,17 @@ struct Window {
   }
 };
 
+// The work item of workgroup `bid`.  Workgroups go to the 8 XCDs round-robin; of
+// every 8 `run` items each XCD takes `run` neighbours, whose windows are much the
+// same blocks, so that the rows a ragged batch does not have are spread over all
+// XCDs (an eighth of the items to each, as selections go, leaves those of a short
+// request idle).
+__device__ __forceinline__ int window_item(const PartialParams& p, int bid) {
+  if (bid >= p.run_all) return p.first + bid;
+  const int i = bid >> 3, c = div_by(i, p.by_run);
+  return p.first + (8 * c + (bid & 7)) * p.run + (i - c * p.run);
+}
+
 // Of split s, the units of 2^SHIFT tokens (half blocks or blocks) that any of query
 // rows i0 .. i0 + n_i - 1 sees, in order: pool units into list, their first tokens
 // into the place of the row masks.  Those whose table entry names no pool block are
@@ -926,7 +937,8 @@ void partial_kernel(const PartialParams p) {
   // of the same residue class, which then meet in the L2 of one or two XCDs
   // instead of all eight (the query rows, read once per split, are what is
   // fetched more than once instead, the smaller of the two).
-  const int w_id = p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
+  const int w_id = WIN ? window_item(p, blockIdx.x)
+                       : p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
   const bool tiles_fast = PR && p.tiles_fast;
   int s_idx, rt, r_num;
   if (tiles_fast) {
@@ -940,6 +952,8 @@ void partial_kernel(const PartialParams p) {
     r_num = div_by(a, p.by_tiles);
     rt = a - r_num * p.row_tiles;
   }
+  // (without a window the last rows see most: they go first)
+  if constexpr (WIN) rt = p.row_tiles - 1 - rt;
   // jobs that share q rows (r, r + q_jobs, ...) take consecutive numbers
   // (a job's q rows are rq, r mod q_jobs)
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
@@ -1996,7 +2010,8 @@ void tile64_kernel(const PartialParams p) {
   const int n16 = lane & 15, g = lane >> 4;  // S^T: row (or token) and dim group
   const int n32 = lane & 31, g2 = lane >> 5;  // O^T: row (or column) and token group
 
-  const int w_id = p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
+  const int w_id = WIN ? window_item(p, blockIdx.x)
+                       : p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
   const bool tiles_fast = PR && p.tiles_fast;
   int s_idx, rt, r_num;
   if (tiles_fast) {
@@ -2010,6 +2025,8 @@ void tile64_kernel(const PartialParams p) {
     r_num = div_by(a, p.by_tiles);
     rt = a - r_num * p.row_tiles;
   }
+  // (without a window the last rows see most: they go first)
+  if constexpr (WIN) rt = p.row_tiles - 1 - rt;
   // (a job's q rows are qj, r mod q_jobs)
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
   const int r = p.q_rep > 1 ? (r_num - rep * p.q_rep) * p.q_jobs + rep : r_num;
@@ -2833,6 +2850,7 @@ static void launch_items(Kernel kernel, PartialParams p, int items, int threads,
     const int n = std::min(most, items - first);
     p.first = first;
     p.grid8 = n % 8 ? 0 : n / 8;
+    p.run_all = p.run > 0 ? n / (8 * p.run) * (8 * p.run) : 0;
     hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), 0, s, p);
     if (n == items - first) return;
     first += n;
