@@ -102,7 +102,8 @@ typedef struct {
  *                                     scheduled next to each other
  *   ckv_pool          [P, 64, 512]    bf16 or fp8-e4m3fn (+block_scale), contiguous
  *                 or  [P, 64, 272]    MXFP4 (4 bits): one selection per job
- *                                     ([R, K]) and 64-row tiles only
+ *                                     ([R, K]; blocks or, in the token call,
+ *                                     tokens) and 64-row tiles only
  *                                     (MLA_ERR_UNSUPPORTED otherwise)
  *   kpe_pool          [P, 64, 64]     same dtype as ckv_pool (bf16 beside MXFP4),
  *                                     contiguous
@@ -261,8 +262,8 @@ mla_status_t mla_sparse_partial_attn_noalloc(const mla_tensor_t* q_lat,
  * Every other argument, the result (T = the multiset of selected tokens)
  * and the layout rules are those of mla_sparse_partial_attn_ex; opts.n_splits
  * counts splits of the token slots (each split takes whole 64-token groups
- * of slots, at most 1024 slots).  bf16 or fp8 caches (a token takes the
- * scales of its pool block); NB and P must not exceed 2^25 blocks
+ * of slots, at most 1024 slots).  Caches of every type (with fp8, a token takes
+ * the scales of its pool block); NB and P must not exceed 2^25 blocks
  * (MLA_ERR_UNSUPPORTED).  An id
  * outside [0, 64 NB), or a table entry outside [0, P), is a caller error that
  * the call does not detect on the host: such a slot is skipped.

@@ -316,8 +316,8 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     if ((st = check_tensor(out_lat, "out_lat", wire ? MLA_DTYPE_BF16 : MLA_DTYPE_FP32, 4)) != MLA_OK)
       return st;
     if ((st = check_tensor(out_lse, "out_lse", MLA_DTYPE_FP32, wire ? 4 : 3)) != MLA_OK) return st;
-    if (mx4 && (tokens || per_row))
-      return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take one block selection per job");
+    if (mx4 && per_row)
+      return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take one selection per job");
     if (mx4 && opts && opts->row_tile == 128)
       return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take 64-row tiles");
     if (opts) {

@@ -1821,7 +1821,7 @@ struct Issue32 {
   int last;  // WIN: the stage's last row that the sequence holds
   // 4 bits: of the RoPE rows, a stage behind the codes
   const uint8_t* kpe_then;
-  int last_then;
+  int last_then, tok_then;
 
   __device__ __forceinline__ Issue32(const PartialParams& p, int wave, int lane) {
     ckv = p.ckv;
@@ -1829,14 +1829,15 @@ struct Issue32 {
     lds_lat = lds_rope = 0;
     tok = tok_rope = 0;
     last = last_then = 31;
+    tok_then = 0;
     kpe_then = p.kpe;
     const int b3 = (wave >> 1) & 1;           // bit 3 of the wave's rows
     const int kw = (b3 << 1) | (wave >> 2);   // their key32, less the low bits' part
     const int hi = lane >> 5;
-    if constexpr (MX4) {
+    if constexpr (MX4 && !TOK) {
       lat[0] = (uint32_t)((WIN ? 0 : (lane >> 4) * kMx4Row) + ((lane & 15) << 4));
       lat[1] = (uint32_t)(WIN ? 0 : lane * kMx4Row) + kDLat / 2;
-    } else {
+    } else if constexpr (!MX4) {
 #pragma unroll
       for (int k = 0; k < kHeld; ++k)
         lat[k] = FP8 ? (uint32_t)((WIN ? 0 : hi * 512) + (((lane & 31) ^ (hi << 2) ^ kw ^ (k << 3)) << 4))
@@ -1861,6 +1862,7 @@ struct Issue32 {
     if constexpr (MX4) {
       kpe_then = kpe;
       last_then = last;
+      tok_then = tok;
     }
     if constexpr (TOK) {
       tok = e[0];
@@ -1892,6 +1894,10 @@ struct Issue32 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                  :: "v"(a), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
   }
+  __device__ __forceinline__ static void go64_lanes(const uint8_t* a, uint32_t lds, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 exec, %2\n\tglobal_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1"
+                 :: "v"(a), "s"(__builtin_amdgcn_readfirstlane(lds)), "s"(lanes) : "memory", "m0");
+  }
   __device__ __forceinline__ uint32_t lat_of(int j) const {
     return (uint32_t)lds_opaque((int)lat[0]) ^ (uint32_t)(j << (FP8 ? 7 : 6));
   }
@@ -1913,6 +1919,17 @@ struct Issue32 {
       } else {
         const int r = FP8 ? 4 * wave + 2 * j + (l >> 5) : 4 * wave + j;
         go(lat[j] + row_off(r, L::kRow), ckv, lds_lat + (uint32_t)j * 1024u);
+      }
+    } else if constexpr (MX4 && TOK) {
+      const int l = lds_opaque(lane);
+      if (j == 0) {
+        const uint32_t t = (uint32_t)__shfl(tok, l >> 4);
+        go64(p.ckv + (uint64_t)t * kMx4Row + (uint32_t)((l & 15) << 4), lds_lat);
+      } else if (j == 1) {
+        go64_lanes(p.ckv + (uint64_t)(uint32_t)tok * kMx4Row + kDLat / 2, lds_exp(wave), 15);
+      } else {
+        const uint32_t t = (uint32_t)__shfl(tok_then, (l >> 3) & 3);
+        go64_lanes(p.kpe + (uint64_t)t * L::kRopeRow + (rope & 0x70u), lds_rope, 0xffffffffull);
       }
     } else if constexpr (MX4) {
       if (j == 0) go(lat[0], ckv, lds_lat);
@@ -1939,8 +1956,7 @@ struct Issue32 {
         const uint32_t t = (uint32_t)(FP8 ? tok_rope : __shfl(tok, (lane >> 3) & 3));
         const uint32_t o = FP8 ? rope ^ ((uint32_t)(lds_opaque(lane) & 3) << 4) : rope & 0x70u;
         const uint8_t* a = p.kpe + (uint64_t)t * L::kRopeRow + o;
-        asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 exec, %2\n\tglobal_load_lds_dwordx4 %0, off\n\ts_mov_b64 exec, -1"
-                     :: "v"(a), "s"(__builtin_amdgcn_readfirstlane(lds_rope)), "s"(kLanes) : "memory", "m0");
+        go64_lanes(a, lds_rope, kLanes);
       }
     }
   }
@@ -2417,7 +2433,7 @@ void tile64_kernel(const PartialParams p) {
   // key reads in flight ahead of their products (fewer where the tokens' rows
   // take registers: a spilled query fragment would be read back in every stage,
   // with a wait for all loads in flight)
-  constexpr int kAhead = NK == 2 && TOK ? (FP8 ? (kSplitScales ? 2 : 3) : 5)
+  constexpr int kAhead = NK == 2 && TOK ? (MX4 ? 4 : FP8 ? (kSplitScales ? 2 : 3) : 5)
                        : NK == 2 && WIN ? (MX4 ? 4 : FP8 ? (kSplitScales ? 2 : 3) : 5)
                        : NK == 2 && MX4 ? 5 : FP8 ? 3 : 6;
   auto scores = [&](int i, auto mid) -> u32x2_t {
@@ -2898,7 +2914,8 @@ hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups,
     else
       launch_window<kKvBf16>(p, grid, row_groups, s);
   } else if (kv == kKvMx4) {
-    launch_tile64<kKvMx4, kSelShared>(p, grid, s);
+    if (sel_kind == kSelTokens) launch_tile64<kKvMx4, kSelTokens>(p, grid, s);
+    else launch_tile64<kKvMx4, kSelShared>(p, grid, s);
   } else if (sel_kind == kSelPerRow) {
     if (kv == kKvFp8Shared)
       launch_kv<kKvFp8Shared, kSelPerRow>(p, grid, row_groups, s);

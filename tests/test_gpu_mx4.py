@@ -92,10 +92,40 @@ def test_entry_points(no_alloc):
     check(*inputs(13, 2, 1, 128, 30, 25), no_alloc=no_alloc)
 
 
+@pytest.mark.parametrize("wire", [False, True])
+@pytest.mark.parametrize("R,Mq,H,NB,K", [(1, 1, 16, 4, 1), (2, 1, 128, 9, 200), (3, 2, 16, 9, 33), (2, 3, 40, 30, 97),
+                                         (1, 1, 1, 3, 64), (2, 1, 33, 60, 1500), (9, 1, 8, 5, 31), (1, 2, 32, 40, 2048)])
+def test_token_selections(R, Mq, H, NB, K, wire):
+    print(f"case: mx4 tokens {R} {Mq} {H} {NB} {K} {wire}", flush=True)
+    c = T.Cache(R + H, R * NB + 2, "mx4")
+    rs = np.random.default_rng(K)
+    table = rs.permutation(R * NB + 2)[:R * NB].reshape(R, NB)
+    sel = rs.integers(0, NB * 64, (R, K))  # (repeats among them)
+    sel[rs.random(sel.shape) < 0.1] = -1
+    if K > 3:
+        sel[0, :2] = NB * 64, -9
+        table = table.copy()
+        table[-1, 0] = c.lat.shape[0] + 5
+    ql, qp = T.randn(K, R, Mq, H, 512), T.randn(K + 1, R, Mq, H, 64)
+    for kw in (dict(), dict(n_splits=3)):
+        out, stat = mla.sparse_partial_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(sel), SCALE, wire=wire,
+                                            tokens=True, **kw)
+        torch.cuda.synchronize()
+        q = np.concatenate([T.host(ql), T.host(qp)], -1)
+        for r in range(R):
+            ids = sel[r][(sel[r] >= 0) & (sel[r] < NB * 64)]
+            ids = ids[table[r][ids // 64] < c.lat.shape[0]]
+            b, t = table[r][ids // 64], ids % 64
+            keys = np.concatenate([c.lat[b, t], c.pe[b, t]], -1)
+            for i in range(Mq):
+                ref = S.attend(q[r, i], keys, c.lat[b, t], np.ones(len(ids), bool), float(np.float32(SCALE)))
+                T.check_row(ref, T.host(out)[r, i], T.host(stat)[r, i], wire, f"job {r} row {i}")
+
+
 def test_refused_forms():
     c, ql, qp, table, sel = inputs(15, 2, 2, 16, 6, 4)
     args = (ql, qp, c.ckv, c.kpe, T.i32(table))
-    for kw, s in ((dict(tokens=True), sel), (dict(row_tile=128), sel), (dict(), np.stack([sel, sel], 1))):
+    for kw, s in ((dict(row_tile=128), sel), (dict(row_tile=128, tokens=True), sel), (dict(), np.stack([sel, sel], 1))):
         with pytest.raises(mla.MlaError) as e:
             mla.sparse_partial_attn(*args, T.i32(s), SCALE, **kw)
         assert e.value.status == mla.MLA_ERR_UNSUPPORTED

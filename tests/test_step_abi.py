@@ -341,8 +341,8 @@ def test_window_overlaps_refused():
 def test_partial_of_a_4bit_cache_refuses_what_it_does_not_do():
     from tests import abi_cases as C
     lib = mla.load()
-    for tokens, sel, tile, text in ((True, (2, 3), 0, "one block selection"), (False, (2, 3, 3), 0, "one block selection"),
-                                    (False, (2, 3), 128, "64-row")):
+    for tokens, sel, tile, text in ((False, (2, 3, 3), 0, "one selection"), (False, (2, 3), 128, "64-row"),
+                                    (True, (2, 3), 128, "64-row")):
         a = C.partial_args(torch.device("cpu"))
         a["ckv"], a["sel"] = z(8, 64, 272, dt=U8), z(*sel, dt=I32)
         a["opts"].row_tile = tile
