@@ -310,7 +310,8 @@ typedef struct {
  * and those at negative positions, is empty: out_lat 0, out_lse -inf (wire: (-inf,
  * 0)).  Scores, weights and splits are those of mla_sparse_partial_attn, as are
  * the layout rules, the limits of scale, the workspace and graph capture.  What the
- * cache holds behind a sequence's last token is not used, whatever it is; blocks
+ * cache holds behind a sequence's last token is not used, whatever it is (within
+ * it, an infinity or a NaN may reach rows that do not see its token); blocks
  * past NB, and those whose table entry is outside [0, P) (a window may let go of
  * the blocks behind it), are left out.  A request's work is that of the blocks its
  * rows see; plans are made for the NB blocks that the table is wide, so a table
@@ -454,7 +455,8 @@ typedef struct {
   int32_t inverse;    /* 1: turn back, which is also the gradient's way: the
                          transpose of the map, mscale included                     */
   int32_t reserved;   /* must be zero                                              */
-  double base;        /* > 0 (YARN: > 1)                                           */
+  double base;        /* > 0 (YARN: > 1); no pair may turn more than 2^20 times a
+                         position                                                  */
   double factor;      /* LINEAR, YARN: s > 0                                       */
   double beta_fast;   /* YARN: turns in orig_len from which a pair keeps its angle */
   double beta_slow;   /* YARN: turns up to which a pair is slowed s times, > 0     */

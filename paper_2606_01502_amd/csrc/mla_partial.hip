@@ -1997,7 +1997,7 @@ struct Convert {
     LDS uint8_t* const a = (LDS uint8_t*)(uintptr_t)(put + out);
 #pragma unroll
     for (int j = j0; j < j1; ++j)
-      *(LDS u32x4_t*)(a + j * 256) = mx4x8_bf16(codes[j], __uint_as_float(exp << 23));
+      *(LDS u32x4_t*)(a + j * 256) = mx4x8_bf16(codes[j], mx4_scale(exp));
   }
 };
 

@@ -70,7 +70,7 @@ mla_status_t check_rope_opts(const mla_rope_opts_t* o, int64_t D) {
   if (o->scaling != MLA_ROPE_PLAIN && o->scaling != MLA_ROPE_LINEAR && o->scaling != MLA_ROPE_YARN)
     return bad("opts.scaling must be MLA_ROPE_PLAIN, MLA_ROPE_LINEAR or MLA_ROPE_YARN");
   if (!(o->base > 0.0) || !std::isfinite(o->base)) return bad("opts.base must be finite and > 0");
-  if (!std::isfinite(o->mscale)) return bad("opts.mscale must be finite");
+  if (!std::isfinite((float)o->mscale)) return bad("opts.mscale must be finite in fp32");
   if (o->scaling != MLA_ROPE_PLAIN && (!(o->factor > 0.0) || !std::isfinite(o->factor)))
     return bad("opts.factor must be finite and > 0");
   if (o->scaling == MLA_ROPE_YARN &&
@@ -195,6 +195,9 @@ mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, cons
     p.mscale = (float)opts->mscale;
     p.sin_scale = opts->inverse ? -p.mscale : p.mscale;
     rope_turns(*opts, p.turns);
+    // (a position is at most 2^31, and doubles hold the products' whole turns up to 2^53)
+    for (int i = 0; i < half; ++i)
+      if (!(p.turns[i] <= 1048576.0)) return fail(MLA_ERR_INVALID_ARGUMENT, "opts: a pair turns more than 2^20 times a position");
     return launched(mla::launch_rope(p, reinterpret_cast<hipStream_t>(stream)), "rope");
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");

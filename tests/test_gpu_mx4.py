@@ -86,6 +86,21 @@ def test_every_exponent_the_writer_uses():
     check(c, ql, qp, table, sel)
 
 
+def test_a_group_that_is_nan():
+    """Exponent byte 255: every row that attends the token is NaN, whatever the
+    codes and the scores; jobs without it are not touched."""
+    print("case: mx4 nan", flush=True)
+    for H in (16, 64):
+        c, ql, qp, table, sel = inputs(17, 2, 1, H, 6, 4)
+        sel[:] = [[0, 1, 2, 3], [2, 3, 4, 5]]
+        want, _ = mla.sparse_partial_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(sel), SCALE)
+        c.ckv[table[0, 2], 40, 256 + 7] = 255
+        c.ckv[table[0, 2], 40, :256] = 0
+        out, _ = mla.sparse_partial_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(sel), SCALE)
+        torch.cuda.synchronize()
+        assert torch.isnan(out[0, ..., 224:256]).all() and torch.equal(out[1], want[1])
+
+
 @pytest.mark.parametrize("no_alloc", [False, True])
 def test_entry_points(no_alloc):
     print(f"case: mx4 entry {no_alloc}", flush=True)

@@ -92,6 +92,16 @@ def test_slots_edges(what):
     _check_slots(c, n, f, t, T, strided=what == "strided")
 
 
+def test_slots_most_requests():
+    print("case: slots 8192", flush=True)
+    rs = np.random.default_rng(3)
+    c, n = rs.integers(0, 70, 8192), rs.integers(0, 3, 8192)
+    t = np.full((8192, 3), -1)
+    t[:, 0], t[:, 1] = np.arange(8192), np.where(c > 64, 8192 + np.arange(8192), -1)
+    t[c == 0, 0] = -1
+    _check_slots(c, n, np.arange(20000, 30000), t, int(n.sum()))
+
+
 def test_slots_no_requests():
     _check_slots(np.zeros(0, int), np.zeros(0, int), np.arange(3), np.zeros((0, 4), int), 10)
 
@@ -342,6 +352,37 @@ def test_gather_of_4bit_rows_is_exact():
     got = oc.float().cpu().numpy().astype(np.float64)
     assert np.array_equal(got, want, equal_nan=True)
     assert np.array_equal(_bits(ok), np.where(live[None, :, None], _bits(kpe)[:, at[0], at[1]], 0))
+
+
+def test_pools_past_4_gib():
+    """The last blocks of pools of more than 4 GiB, written, read back and attended."""
+    print("case: large pools", flush=True)
+    P, n = 262000, 150
+    far = np.array([P - 1, P - 70000, P - 2])
+    slots = (far[:, None] * 64 + np.arange(64)).reshape(-1)[:n]
+    ckv, kpe = randn(1, n, 512, sigma=0.5), randn(2, n, 64)
+    q = randn(3, 1, 2, 24, 576)
+    for kv in ("mx4", "bf16"):
+        row, dt = (272, torch.uint8) if kv == "mx4" else (512, torch.bfloat16)
+        got = []
+        for blocks, at in ((P, slots), (3, np.arange(n))):
+            pool = torch.empty((blocks, 64, row), dtype=dt, device="cuda")
+            kpool = torch.empty((blocks, 64, 64), dtype=torch.bfloat16, device="cuda")
+            mla.cache_append(ckv, kpe, i32(at), pool, kpool)
+            table = far if blocks == P else np.arange(3)
+            back = mla.fetch_gather(pool[None], kpool[None], i32(table), i32(np.arange(n)))
+            args = (q[..., :512], q[..., 512:], pool, kpool, i32(table[None]))
+            outs = [mla.window_attn(*args, i32([n]), 0.07, window=100, n_sink=2)]
+            outs += [mla.sparse_partial_attn(*args, i32([[0, 1]]), 0.07, row_tile=64)]
+            outs += [mla.sparse_partial_attn(*args, i32(np.arange(n)[None]), 0.07, tokens=True, row_tile=64)]
+            if kv == "bf16":
+                outs += [mla.window_attn(*args, i32([n]), 0.07, window=100, n_sink=2, row_tile=128)]
+            got.append([x.clone() for o in [back, *outs] for x in o])
+            del pool, kpool
+            torch.cuda.empty_cache()
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
+        assert torch.isfinite(got[0][2]).all()
 
 
 # ---------------------------------------------------------------- streams, graphs

@@ -125,7 +125,8 @@ ROPE += [(f"opts {k}={v}", dict(opts=rope_args(**{k: v, **more})["opts"]), text)
     ("rot_offset", 33, {}, "within the head"), ("rot_offset", -1, {}, "within the head"),
     ("pairing", 2, {}, "pairing"), ("inverse", 2, {}, "inverse"), ("scaling", 3, {}, "scaling"),
     ("reserved", 1, {}, "reserved"), ("base", 0.0, {}, "base"), ("base", float("inf"), {}, "base"),
-    ("mscale", float("nan"), {}, "mscale"), ("factor", 0.0, {"scaling": 1}, "factor"),
+    ("mscale", float("nan"), {}, "mscale"), ("mscale", 1e300, {}, "mscale"), ("base", 1e-9, {}, "2^20"),
+    ("factor", 1e-12, {"scaling": 1}, "2^20"), ("factor", 0.0, {"scaling": 1}, "factor"),
     ("factor", float("nan"), {"scaling": 2}, "factor"), ("base", 1.0, {"scaling": 2}, "YARN"),
     ("orig_len", 0, {"scaling": 2}, "YARN"), ("beta_slow", 0.0, {"scaling": 2}, "YARN"),
     ("beta_slow", 33.0, {"scaling": 2}, "YARN"), ("beta_fast", float("inf"), {"scaling": 2}, "YARN")]]
