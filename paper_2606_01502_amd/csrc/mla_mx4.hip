@@ -32,20 +32,20 @@ __device__ __forceinline__ int quad_max(int v) {
   return max(v, __shfl_xor(v, 2));
 }
 
-// Eight bf16 values (two to a word) -> eight E2M1 codes of v / 2^(byte - 127).
-__device__ __forceinline__ uint32_t to_codes(u32x4_t v, int byte) {
-  // v / 2^e as fp32, exact: e is within -125 .. 125, and what underflows rounds to 0 either way
-  const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
-  uint32_t codes = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t w = (i & 1) ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16;
-    const float a = fabsf(__uint_as_float(w)) * inv;
-    const uint32_t q = (uint32_t)(a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) +
-                       (a >= 3.5f) + (a > 5.0f);
-    codes |= (q | (w >> 28 & 8u)) << (4 * i);
-  }
-  return codes;
+// Eight bf16 values (two to a word) -> eight E2M1 codes of v / s, s a power of two:
+// to nearest, halfway to the even code, at most 6 (compared for every bf16 value).
+// The conversion instruction does two at once: 30,001 tokens are written in 9.2 us
+// (46 MB, 5 TB/s), 16.5 with comparisons against the seven borders, which are about
+// 130 instructions for these eight values.
+__device__ __forceinline__ uint32_t to_codes(u32x4_t v, float s) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  // (a bit cast of a vector's element would take the first one)
+  const uint32_t w0 = v[0], w1 = v[1], w2 = v[2], w3 = v[3];
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w0), s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w1), s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w2), s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w3), s, 3);
 }
 
 template <bool MX4>
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendParams p) 
         const bool bad = mag >= 0x7F80;
         const int byte = min(max((mag >> 7) - 2, 2), 252);
         uint32_t* const dst = (uint32_t*)(p.ckv + row[j] * kMx4Row);
-        dst[lane] = to_codes(v[j], byte);
+        dst[lane] = to_codes(v[j], __uint_as_float((uint32_t)byte << 23));
         // four groups' bytes to a word: lanes 0, 16, 32, 48 store them
         uint32_t b = (uint32_t)(bad ? 255 : byte) << (lane >> 2 & 3) * 8;
         b |= __shfl_xor(b, 4);

@@ -199,22 +199,26 @@ def _describe_latent(t, block_scale=None):
 def _on_one_gpu(*tensors):
     """Raise ValueError unless every given tensor lives on one CUDA (HIP)
     device: the library reads and writes device memory only, and a host
-    tensor's address handed to a kernel would fault."""
-    devs = {t.device for t in tensors if t is not None}
-    bad = [d for d in devs if d.type != "cuda"]
-    if bad:
-        raise ValueError(f"tensors must be on the GPU, got {bad[0]}")
-    if len(devs) > 1:
-        raise ValueError(f"tensors must be on one device, got {sorted(map(str, devs))}")
+    tensor's address handed to a kernel would fault.  Returns its index."""
+    first = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"tensors must be on the GPU, got {t.device}")
+        if first is None:
+            first = t.get_device()
+        elif t.get_device() != first:
+            raise ValueError(f"tensors must be on one device, got {['cuda:%d' % first, str(t.device)]}")
+    return first
 
 
 def _on_current_gpu(*tensors):
     """_on_one_gpu, and that device is the current one, whose stream the call
     goes to."""
-    _on_one_gpu(*tensors)
-    dev = next(t.device for t in tensors if t is not None)
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {dev}, which is not the current device")
+    dev = _on_one_gpu(*tensors)
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{dev}, which is not the current device")
 
 
 def _stream(stream):
