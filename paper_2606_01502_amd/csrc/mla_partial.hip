@@ -46,8 +46,14 @@
 // rows' blocks once and masks every row to its own multiset; or single
 // tokens (an indexer's top-k, Section 6.3's selection budgets), gathered 64
 // at a time into the same stage layout, each with its own block's fp8
-// scales.  Splits of a workspace of a megabyte or more store their rows as
+// scales; or no list but positions (kSelWindow): the rows are the last tokens
+// of sequences, each sees the tokens of its window and the first few, and a
+// tile reads the blocks that any of its rows sees.  Splits of a workspace of a megabyte or more store their rows as
 // fp16 scaled by the row's largest magnitude.
+//
+// 4-bit caches (64-row tiles only): 272 bytes of E2M1 codes and exponents a
+// token, converted to bf16 on the way from one LDS ring to another, exactly,
+// once a workgroup; scores and values are then as over a bf16 cache.
 //
 // LDS swizzles (token t of the block, 16-byte chunk c of its row) are
 // described with bf16_key, fp8_key and key32 below.
