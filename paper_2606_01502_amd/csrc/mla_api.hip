@@ -264,6 +264,7 @@ mla_status_t enqueue(const mla::Planner& planner, mla::PartialParams& p, int64_t
     p.ws_scale = (float*)((char*)ws + o_bytes);
     p.ws_lse = p.ws_scale + n_part_rows;
     p.ws_max = p.ws_lse + n_part_rows;
+    if (planner.shares(S)) p.ws_share = (int32_t*)(p.ws_max + n_part_rows);
   }
   hipError_t e = mla::launch_partial(p, (int)R, kv, row_groups, sel_kind, hs);
   if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("partial kernel launch: ") + hipGetErrorString(e));
@@ -275,6 +276,7 @@ mla_status_t enqueue(const mla::Planner& planner, mla::PartialParams& p, int64_t
     c.ws_scale = p.ws_scale;
     c.ws_lse = p.ws_lse;
     c.ws_max = p.ws_max;
+    c.ws_share = p.ws_share;
     c.R = (int32_t)R; c.S = (int32_t)S; c.Mq = p.Mq; c.H = p.H; c.rows = p.rows;
     c.by_H = p.by_H;
     c.by_rows = mla::make_div(p.rows);

@@ -104,6 +104,9 @@ struct PartialParams {
   // part that goes in whole rounds of them (see window_item)
   int32_t run, run_all;
   Div by_run;
+  // windows: splits shared out by what each request's rows see (see
+  // window_shares), two ints a request: its first split and their number; else null
+  int32_t* ws_share;
 };
 
 // Combine of the S split partials of every job into the caller's outputs.
@@ -122,6 +125,7 @@ struct CombineParams {
   int64_t out_s0, out_s1, out_s2;
   float* lse;
   int64_t lse_s0, lse_s1, lse_s2;
+  const int32_t* ws_share;  // of PartialParams; null: S splits each
 };
 
 // Merge of n parts given by pointers with shared strides.  wire: the parts
@@ -249,6 +253,10 @@ constexpr int kSelTokens = 2;
 constexpr int kSelWindow = 3;
 // half blocks that one split of a window lists
 constexpr int kWindowList = kPerRowListShort;
+// Requests that splits are shared out between by length: one to a lane.
+constexpr int kShareRequests = 64;
+// Most splits of a request then: its rows' splits are read one trip after another.
+constexpr int kShareMost = 64;
 
 // Launchers; return hipSuccess or the launch error.
 // row_groups: 2 (row tiles of 128 rows) or 1 (row tiles of 64 rows)

@@ -58,7 +58,13 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const CombineParams p
   const int lane = threadIdx.x & 63;
   const int r = div_by(grow, p.by_rows);
   const int row = grow - r * p.rows;
-  combine_row(p, p.S, r, row, lane);
+  int S = p.S;
+  int64_t part0 = (int64_t)r * S;
+  if (p.ws_share) {
+    part0 = p.ws_share[2 * r];
+    S = __builtin_amdgcn_readfirstlane(p.ws_share[2 * r + 1]);
+  }
+  combine_row(p, S, part0, r, row, lane);
 }
 
 }  // namespace

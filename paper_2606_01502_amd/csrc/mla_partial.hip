@@ -787,13 +787,91 @@ __device__ __forceinline__ int window_item(const PartialParams& p, int bid) {
   return p.first + (8 * c + (bid & 7)) * p.run + (i - c * p.run);
 }
 
-// Of split s, the units of 2^SHIFT tokens (half blocks or blocks) that any of query
+// What the rows of a request see: len and q_len of win_lens and win_qlens.
+__device__ __forceinline__ Window window_of(const PartialParams& p, int len, int q_len) {
+  Window w{};
+  len = max(len, 0);
+  w.qn = min(max(q_len, 0), p.Mq);
+  w.pos0 = len - w.qn;
+  w.window = p.window;
+  w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
+  w.n_sink = p.window ? p.n_sink : 0;
+  return w;
+}
+
+// The units of 2^SHIFT tokens that any of query rows i0 .. i1 sees: units 0 ..
+// sinks - 1, then lo .. sinks - 1 + all.
+struct Units {
+  int sinks, lo, all;
+};
+template <int SHIFT>
+__device__ __forceinline__ Units units_of(const Window& w, int i0, int i1) {
+  const int live = min(i1, w.qn - 1);  // the last row with a query
+  const int hi = live >= i0 ? w.hi_of(live) : -1, lo = w.lo_of(i0);
+  if (hi < 0) return {0, 0, 0};
+  const int u_lo = min(lo, hi) >> SHIFT, u_hi = hi >> SHIFT;
+  const int sinks = (int)min(((int64_t)w.n_sink + (1 << SHIFT) - 1) >> SHIFT, (int64_t)u_lo);
+  return {sinks, u_lo, sinks + u_hi - u_lo + 1};
+}
+
+// Sum of v over lanes 0 .. the own one.
+__device__ __forceinline__ int lanes_up(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // within rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 to row 1, 47 to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+  return v;
+}
+
+// Splits shared out by what the requests' rows see.  The grid holds S splits a
+// request; with u units to a split, request r takes max(1, ceil(n_r / u)) of them.
+// The smallest u that B S splits suffice for (within 1/16) lies between the mean
+// and the largest share of S splits, which always suffices.  One request to a
+// lane; every wave finds the same.  Work item w_id -> request, tile and split;
+// false: the item is not needed.
+struct Share {
+  int r, rt, s, n, first;  // s: of n splits, which are splits first .. first + n - 1 of the call
+};
+template <int SHIFT>
+__device__ __forceinline__ bool window_shares(const PartialParams& p, int w_id, int lane, Share& sh) {
+  const int B = p.q_jobs, S = p.n_splits;
+  int n = 0;
+  // (no more than a tile's rows may see, K blocks or 2 K half blocks, or the ends of
+  // two more: what a split of u units takes off a tile then fits its list)
+  if (lane < B) n = min(units_of<SHIFT>(window_of(p, p.win_lens[lane], p.win_qlens ? p.win_qlens[lane] : p.Mq), 0, p.Mq - 1).all, SHIFT == 5 ? 2 * p.K : p.K + 1);
+  const int total = __builtin_amdgcn_readlane(lanes_up(n), 63);
+  int most = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
+  most = __builtin_amdgcn_readfirstlane(most);
+  auto up = [](int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); };
+  auto splits = [&](int u) { return lane < B ? max(1, up(n, u)) : 0; };
+  int hi = max(1, up(most, S)), lo = max(1, max(up(total, B * S), up(most, kShareMost)));
+  while (lo < hi - hi / 16) {
+    const int u = (lo + hi) >> 1;
+    if (__builtin_amdgcn_readlane(lanes_up(splits(u)), 63) <= B * S) hi = u;
+    else lo = u + 1;
+  }
+  const int own = splits(hi), first = lanes_up(own) - own;
+  const uint64_t at = __ballot(lane < B && first * p.row_tiles <= w_id);
+  sh.r = 63 - __builtin_clzll(at);
+  sh.n = __builtin_amdgcn_readlane(own, sh.r);
+  sh.first = __builtin_amdgcn_readlane(first, sh.r);
+  const int i = w_id - sh.first * p.row_tiles;
+  sh.rt = __builtin_amdgcn_readfirstlane(i / sh.n);
+  sh.s = i - sh.rt * sh.n;
+  return sh.rt < p.row_tiles;
+}
+
+// Of split s of n_splits, the units of 2^SHIFT tokens (half blocks or blocks) that any of query
 // rows i0 .. i0 + n_i - 1 sees, in order: pool units into list, their first tokens
 // into the place of the row masks.  Those whose table entry names no pool block are
 // left out.  Returns their number.
 template <class L, int SHIFT>
-__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int i0, int n_i, int cap, Window& w,
-                                              LDS uint8_t* smem, int tid) {
+__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int n_splits, int i0, int n_i, int cap,
+                                              Window& w,                                              LDS uint8_t* smem, int tid) {
   constexpr bool FP8 = L::kFp8;
   constexpr int kHalves = SHIFT == 5 ? 1 : 0;
   const int lane = tid & 63;
@@ -802,28 +880,20 @@ __device__ __forceinline__ int compact_window(const PartialParams& p, int r, int
   LDS int* first = (LDS int*)(smem + L::kMasks);
   LDS float* scales = (LDS float*)(smem + L::kScales);
   LDS int* wave_cnt = (LDS int*)(smem + L::kWaveCnt);
-  const int len = max(p.win_lens[r], 0);
-  w.qn = p.win_qlens ? min(max(p.win_qlens[r], 0), p.Mq) : p.Mq;
-  w.pos0 = len - w.qn;
-  w.window = p.window;
-  w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
-  w.n_sink = p.window ? p.n_sink : 0;
-  const int i1 = i0 + n_i - 1, live = min(i1, w.qn - 1);  // the tile's last row, the last with a query
+  w = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
+  const int i1 = i0 + n_i - 1;  // the tile's last row
   w.hi_all = i1 < w.qn ? w.hi_of(i0) : -1;
   w.lo_all = w.lo_of(i1);
-  const int hi = live >= i0 ? w.hi_of(live) : -1, lo = w.lo_of(i0);
-  if (hi < 0) return 0;
-  const int u_lo = min(lo, hi) >> SHIFT, u_hi = hi >> SHIFT;
-  const int sinks = (int)min(((int64_t)w.n_sink + (1 << SHIFT) - 1) >> SHIFT, (int64_t)u_lo);
-  const int n_all = sinks + u_hi - u_lo + 1;
-  const int e0 = (int)((int64_t)n_all * s / p.n_splits), e1 = (int)((int64_t)n_all * (s + 1) / p.n_splits);
+  const Units un = units_of<SHIFT>(w, i0, i1);
+  if (un.all == 0) return 0;
+  const int e0 = (int)((int64_t)un.all * s / n_splits), e1 = (int)((int64_t)un.all * (s + 1) / n_splits);
   const int n_e = min(e1 - e0, cap);
   int n_valid = 0;
   for (int base = 0; base < n_e; base += L::kThreads) {
     const int e = e0 + base + tid;
     int b = -1, u = 0;
     if (base + tid < n_e) {
-      u = e < sinks ? e : u_lo + (e - sinks);
+      u = e < un.sinks ? e : un.lo + (e - un.sinks);
       const int bb = p.table[r * p.table_s0 + (u >> kHalves)];
       if (bb >= 0 && bb < p.P) b = bb;
     }
@@ -958,8 +1028,21 @@ void partial_kernel(const PartialParams p) {
     r_num = div_by(a, p.by_tiles);
     rt = a - r_num * p.row_tiles;
   }
-  // (without a window the last rows see most: they go first)
-  if constexpr (WIN) rt = p.row_tiles - 1 - rt;
+  int n_of = p.n_splits, part0 = 0;  // windows: the splits of the request, and its first one
+  if constexpr (WIN) {
+    part0 = r_num * n_of;
+    if (p.ws_share) {
+      Share sh;
+      if (!window_shares<6>(p, w_id, lane, sh)) return;
+      s_idx = sh.s;
+      rt = sh.rt;
+      r_num = sh.r;
+      n_of = sh.n;
+      part0 = sh.first;
+    }
+    // (without a window the last rows see most: they go first)
+    rt = p.row_tiles - 1 - rt;
+  }
   // jobs that share q rows (r, r + q_jobs, ...) take consecutive numbers
   // (a job's q rows are rq, r mod q_jobs)
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
@@ -1022,7 +1105,7 @@ void partial_kernel(const PartialParams p) {
   int n_tok = 0;  // token selections: the listed tokens (n_valid counts virtual blocks)
   Window win{};
   if constexpr (WIN) {
-    n_valid = compact_window<L, 6>(p, r, s_idx, i0, n_i, L::kPerRowCap, win, smem, tid);
+    n_valid = compact_window<L, 6>(p, r, s_idx, n_of, i0, n_i, L::kPerRowCap, win, smem, tid);
   } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                    p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
@@ -1498,7 +1581,13 @@ void partial_kernel(const PartialParams p) {
   // of row rr in slot c ^ rr) and stored as contiguous 1 KiB rows.
   const bool direct = p.n_splits == 1;
   const bool half = !direct && p.ws_f16;
-  const int64_t part = (int64_t)r * p.n_splits + s_idx;
+  const int64_t part = (WIN ? part0 : (int64_t)r * p.n_splits) + s_idx;
+  if constexpr (WIN) {
+    if (p.ws_share && rt == 0 && s_idx == 0 && tid == 0) {
+      p.ws_share[2 * r] = part0;
+      p.ws_share[2 * r + 1] = n_of;
+    }
+  }
   lds_barrier();  // every wave is done with the last block's LDS
   LDS uint8_t* const stage = smem + wave * 32768;
   const int ln = lds_opaque(lane);
@@ -2047,8 +2136,21 @@ void tile64_kernel(const PartialParams p) {
     r_num = div_by(a, p.by_tiles);
     rt = a - r_num * p.row_tiles;
   }
-  // (without a window the last rows see most: they go first)
-  if constexpr (WIN) rt = p.row_tiles - 1 - rt;
+  int n_of = p.n_splits, part0 = 0;  // windows: the splits of the request, and its first one
+  if constexpr (WIN) {
+    part0 = r_num * n_of;
+    if (p.ws_share) {
+      Share sh;
+      if (!window_shares<5>(p, w_id, lane, sh)) return;
+      s_idx = sh.s;
+      rt = sh.rt;
+      r_num = sh.r;
+      n_of = sh.n;
+      part0 = sh.first;
+    }
+    // (without a window the last rows see most: they go first)
+    rt = p.row_tiles - 1 - rt;
+  }
   // (a job's q rows are qj, r mod q_jobs)
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
   const int r = p.q_rep > 1 ? (r_num - rep * p.q_rep) * p.q_jobs + rep : r_num;
@@ -2120,7 +2222,7 @@ void tile64_kernel(const PartialParams p) {
   Window win{};
   int hi_row = -1, lo_row = 0;  // of the lane's score row
   if constexpr (WIN) {
-    n_valid = compact_window<L, 5>(p, r, s_idx, i0, n_i, L::kCap, win, smem, tid);
+    n_valid = compact_window<L, 5>(p, r, s_idx, n_of, i0, n_i, L::kCap, win, smem, tid);
     const int i_row = div_by(row_wg0 + 16 * rq + n16, p.by_H);
     hi_row = win.hi_of(i_row);
     lo_row = win.lo_of(i_row);
@@ -2668,7 +2770,13 @@ void tile64_kernel(const PartialParams p) {
   // groups) through the weights' place, then each writes its 64 columns.
   const bool direct = p.n_splits == 1;
   const bool half = !direct && p.ws_f16;
-  const int64_t part = (int64_t)r * p.n_splits + s_idx;
+  const int64_t part = (WIN ? part0 : (int64_t)r * p.n_splits) + s_idx;
+  if constexpr (WIN) {
+    if (p.ws_share && rt == 0 && s_idx == 0 && tid == 0) {
+      p.ws_share[2 * r] = part0;
+      p.ws_share[2 * r + 1] = n_of;
+    }
+  }
   lds_barrier();  // every wave is done with the last block's weights
   LDS float* const xsum = (LDS float*)pbuf;       // [64][2]
   LDS float* const xtrue = xsum + 128;            // [64][2]

@@ -314,3 +314,59 @@ def test_long_and_many_tiles_of_128_rows(kv):
     c, ql, qp, table = inputs(142, 1, 300, 16, 10, kv)
     check(c, ql, qp, table, [600], window=129, n_sink=4, rows=range(0, 300, 17), row_tile=128)
     check(c, ql, qp, table, [300], rows=range(0, 300, 29), row_tile=128)
+
+
+def pooled(seed, B, Mq, H, NB, P, kv):
+    """Requests whose tables draw on one small pool."""
+    c = T.Cache(seed, P, kv)
+    table = np.random.default_rng(seed).integers(0, P, (B, NB))
+    return c, T.randn(seed, B, Mq, H, 512), T.randn(seed + 1, B, Mq, H, 64), table
+
+
+@pytest.mark.parametrize("kv", T.KVS)
+@pytest.mark.parametrize("B,Mq,H,NB,longest", [(40, 1, 16, 48, 48 * 64), (64, 1, 128, 16, 1024), (2, 1, 16, 600, 600 * 64),
+                                               (64, 2, 64, 300, 300 * 64), (63, 3, 24, 64, 64 * 64), (17, 1, 130, 90, 90 * 64)])
+@pytest.mark.parametrize("spread", ["one long", "any", "alike"])
+def test_splits_shared_by_length(kv, B, Mq, H, NB, longest, spread):
+    """Automatic plans over requests of unlike lengths: none, one token, the whole table."""
+    print(f"case: shares {kv} {B} {Mq} {H} {NB} {spread}", flush=True)
+    rs = np.random.default_rng([B, NB])
+    lens = {"one long": rs.integers(0, 200, B), "any": rs.integers(0, min(longest, 3000), B),
+            "alike": np.full(B, min(longest, 1000))}[spread]
+    if spread != "alike":
+        lens[B // 2] = longest
+        lens[0], lens[-1] = (0, 1) if B > 2 else (70, longest)
+    q_lens = rs.integers(0, Mq + 1, B) if Mq > 1 else None
+    if q_lens is not None:
+        q_lens[B // 2] = Mq
+    c, ql, qp, table = pooled(B, B, Mq, H, NB, 37, kv)
+    table[1, :2] = -1
+    check(c, ql, qp, table, lens, q_lens, rows=[0, Mq - 1], wire=spread == "any")
+    if spread == "one long":  # (a window of more than half the table, with sinks)
+        check(c, ql, qp, table, lens, q_lens, rows=[0, Mq - 1], window=40 * NB + 7, n_sink=33)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "mx4"])
+def test_shared_splits_follow_the_lengths_of_a_replay(kv):
+    print(f"case: shares replayed {kv}", flush=True)
+    B, H, NB = 40, 16, 48
+    c, ql, qp, table = pooled(4, B, 1, H, NB, 37, kv)
+    tab, lens = T.i32(table), T.i32(np.full(B, 900))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        f = mla.prepare_window(ql, qp, c.ckv, c.kpe, tab, lens, SCALE, **c.scales)
+        f()  # (the workspace grows outside of the capture)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        out, lse = f()
+    for seed in range(4):
+        new = np.random.default_rng(seed).integers(0, NB * 64 + 1, B) // (1 if seed & 1 else np.arange(1, B + 1))
+        lens.copy_(T.i32(new))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        side.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        eager, eager_lse = check(c, ql, qp, table, new)
+        assert torch.equal(got, eager) and torch.equal(got_lse, eager_lse)
