@@ -315,7 +315,7 @@ typedef struct {
  * past NB, and those whose table entry is outside [0, P) (a window may let go of
  * the blocks behind it), are left out.  A request's work is that of the blocks its
  * rows see; plans are made for the NB blocks that the table is wide, so a table
- * view as wide as the longest sequence serves best.  Automatic splits of up to 64
+ * view as wide as the longest sequence serves best.  Automatic splits of up to 256
  * requests follow what each one's rows see, on the GPU, where windows reach over
  * more than half the table: a result then depends, within its rounding, on the
  * lengths of its neighbours too.  NB at most 2^25 blocks

@@ -253,8 +253,8 @@ constexpr int kSelTokens = 2;
 constexpr int kSelWindow = 3;
 // half blocks that one split of a window lists
 constexpr int kWindowList = kPerRowListShort;
-// Requests that splits are shared out between by length: one to a lane.
-constexpr int kShareRequests = 64;
+// Requests that splits are shared out between by length: four to a lane.
+constexpr int kShareRequests = 256;
 // Most splits of a request then: its rows' splits are read one trip after another.
 constexpr int kShareMost = 64;
 

@@ -828,26 +828,42 @@ __device__ __forceinline__ int lanes_up(int v) {
 // Splits shared out by what the requests' rows see.  The grid holds S splits a
 // request; with u units to a split, request r takes max(1, ceil(n_r / u)) of them.
 // The smallest u that B S splits suffice for (within 1/16) lies between the mean
-// and the largest share of S splits, which always suffices.  One request to a
-// lane; every wave finds the same.  Work item w_id -> request, tile and split;
+// and the largest share of S splits, which always suffices.  A lane takes up to four
+// requests; every wave finds the same.  Work item w_id -> request, tile and split;
 // false: the item is not needed.
 struct Share {
   int r, rt, s, n, first;  // s: of n splits, which are splits first .. first + n - 1 of the call
 };
 template <int SHIFT>
 __device__ __forceinline__ bool window_shares(const PartialParams& p, int w_id, int lane, Share& sh) {
+  constexpr int kPer = kShareRequests / 64;
   const int B = p.q_jobs, S = p.n_splits;
-  int n = 0;
-  // (no more than a tile's rows may see, K blocks or 2 K half blocks, or the ends of
-  // two more: what a split of u units takes off a tile then fits its list)
-  if (lane < B) n = min(units_of<SHIFT>(window_of(p, p.win_lens[lane], p.win_qlens ? p.win_qlens[lane] : p.Mq), 0, p.Mq - 1).all, SHIFT == 5 ? 2 * p.K : p.K + 1);
-  const int total = __builtin_amdgcn_readlane(lanes_up(n), 63);
-  int most = n;
+  const int c = (B + 63) >> 6, r0 = c * lane;  // the lane's requests: r0 .. r0 + c - 1
+  int n[kPer] = {};
+  int total = 0, most = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int r = r0 + k;
+    // (no more than a tile's rows may see, K blocks or 2 K half blocks, or the ends of
+    // two more: what a split of u units takes off a tile then fits its list)
+    if (k < c && r < B)
+      n[k] = min(units_of<SHIFT>(window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq), 0, p.Mq - 1).all,
+                 SHIFT == 5 ? 2 * p.K : p.K + 1);
+    total += n[k];
+    most = max(most, n[k]);
+  }
+  total = __builtin_amdgcn_readlane(lanes_up(total), 63);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
   most = __builtin_amdgcn_readfirstlane(most);
   auto up = [](int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); };
-  auto splits = [&](int u) { return lane < B ? max(1, up(n, u)) : 0; };
+  auto splits = [&](int u) {
+    int v = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (k < c && r0 + k < B) v += max(1, up(n[k], u));
+    return v;
+  };
   int hi = max(1, up(most, S)), lo = max(1, max(up(total, B * S), up(most, kShareMost)));
   while (lo < hi - hi / 16) {
     const int u = (lo + hi) >> 1;
@@ -855,10 +871,19 @@ __device__ __forceinline__ bool window_shares(const PartialParams& p, int w_id, 
     else lo = u + 1;
   }
   const int own = splits(hi), first = lanes_up(own) - own;
-  const uint64_t at = __ballot(lane < B && first * p.row_tiles <= w_id);
-  sh.r = 63 - __builtin_clzll(at);
-  sh.n = __builtin_amdgcn_readlane(own, sh.r);
-  sh.first = __builtin_amdgcn_readlane(first, sh.r);
+  // the last lane whose first item is not past w_id, and its last such request
+  const int l = 63 - __builtin_clzll(__ballot(r0 < B && first * p.row_tiles <= w_id));
+  sh.r = c * l;
+  sh.first = __builtin_amdgcn_readlane(first, l);
+  sh.n = __builtin_amdgcn_readlane(max(1, up(n[0], hi)), l);
+#pragma unroll
+  for (int k = 1; k < kPer; ++k) {
+    if (k < c && c * l + k < B && (sh.first + sh.n) * p.row_tiles <= w_id) {
+      sh.r = c * l + k;
+      sh.first += sh.n;
+      sh.n = __builtin_amdgcn_readlane(max(1, up(n[k], hi)), l);
+    }
+  }
   const int i = w_id - sh.first * p.row_tiles;
   sh.rt = __builtin_amdgcn_readfirstlane(i / sh.n);
   sh.s = i - sh.rt * sh.n;

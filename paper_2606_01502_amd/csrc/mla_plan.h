@@ -114,9 +114,9 @@ struct Planner {
   // tokens and one of 32,768 140 -> 45.  Finding the shares takes 0.7 to 2 us, which
   // splits of few blocks do not gain: 4 requests of 16 rows with 1054 to 3916
   // tokens, two blocks a split, 16.2 -> 18.6.
-  bool shares(int64_t S) const {
-    return a.window && S > 1 && a.n_splits == 0 && a.R > 1 && a.R <= kShareRequests && a.NB <= (1 << 24) &&
-           2 * a.K > a.NB && a.K >= 8 * S;
+  bool shares(int64_t S) const { return S > 1 && may_share() && a.K >= 8 * S; }
+  bool may_share() const {
+    return a.window && a.n_splits == 0 && a.R > 1 && a.R <= kShareRequests && a.NB <= (1 << 20) && 2 * a.K > a.NB;
   }
   uint64_t ws_size(int64_t S) const {
     return ws_rows_bytes(S) + 3 * split_rows(S) * 4 + (shares(S) ? 8 * kShareRequests : 0);
@@ -208,11 +208,22 @@ struct Planner {
     static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64};
     const int64_t most = std::max<int64_t>(a.K, 1);
     Plan plan = cover;
+    // Long sequences of so many requests that the chip is full without splits: two at
+    // least, so that there is something to share out.  128 requests of 128 4-bit rows:
+    // 281 to 16,379 tokens 620 -> 457 us, 127 of 300 tokens and one of 16,384 614 -> 82,
+    // all of 16,384 649 -> 687; from 128 blocks on, for all of 4096 take 169 -> 209.
+    const bool two = may_share() && a.K >= 128 && a.R * row_tiles_of(2) <= 2 * a.cus;
+    if (two && plan.S == 1) plan.us = INFINITY;
     for (int rg = 1; rg <= 2; ++rg) {
       if (row_groups && rg != row_groups) continue;
       const int64_t units = std::max<int64_t>(a.R * row_tiles_of(rg), 1);
       auto offer = [&](int64_t S) {
+        if (two) S = std::max<int64_t>(S, 2);
         const Plan q = plan_of(rg, S);
+        if (two) {
+          if (q.us < plan.us) plan = q;
+          return;
+        }
         if (fits(plan) && !fits(q)) return;
         if ((fits(q) && !fits(plan)) || q.us < plan.us) plan = q;
       };

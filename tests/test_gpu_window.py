@@ -370,3 +370,17 @@ def test_shared_splits_follow_the_lengths_of_a_replay(kv):
         got, got_lse = out.clone(), lse.clone()
         eager, eager_lse = check(c, ql, qp, table, new)
         assert torch.equal(got, eager) and torch.equal(got_lse, eager_lse)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "mx4"])
+@pytest.mark.parametrize("B,H,NB", [(65, 16, 130), (128, 128, 130), (129, 24, 140), (193, 8, 128), (256, 5, 256), (257, 8, 130)])
+def test_splits_shared_in_large_batches(kv, B, H, NB):
+    """Several requests a lane, the last lanes without any; more than are shared between."""
+    print(f"case: shares, large batch {kv} {B} {H} {NB}", flush=True)
+    rs = np.random.default_rng([B, NB])
+    lens = rs.integers(0, 150, B)
+    lens[rs.integers(0, B, 3)] = NB * 64 - 5
+    lens[rs.integers(0, B, 9)] = rs.integers(0, 3000, 9)
+    lens[-1] = 777
+    c, ql, qp, table = pooled(B, B, 1, H, NB, 37, kv)
+    check(c, ql, qp, table, lens, wire=B % 2 == 0)
