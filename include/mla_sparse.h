@@ -156,6 +156,8 @@ typedef struct {
  *   s_t = scale * (q_lat . ckv_t + q_pe . kpe_t),
  *   out_lse = ln sum_T exp(s_t),   out_lat = sum_T exp(s_t - out_lse) * ckv_t,
  * and for an empty T: out_lat = 0, out_lse = -inf.  No mask, no positions.
+ * Where a score is NaN (a NaN in the row or in a token it attends), out_lat and
+ * out_lse are NaN (wire: both m and l), in any number of splits.
  *
  * Layout: q and out rows may be strided on the R, Mq and H dims (16-byte
  * aligned rows); pools must be contiguous and 16-byte aligned.  Slot order
@@ -340,12 +342,13 @@ mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe
  * Per row, over the live parts (lse != -inf): L = max lse_j,
  * lse = L + ln sum exp(lse_j - L), out = sum exp(lse_j - lse) * out_lat[j].
  * A part whose lse is -inf is skipped whatever its out_lat holds (even NaN);
- * if no part is live the row is 0.  The parts may live anywhere but must
+ * if no part is live the row is 0.  A part whose lse is NaN is live, and the
+ * row NaN.  The parts may live anywhere but must
  * share one set of strides; out may not overlap any input.
  * Parts in the bf16 wire form (Section 3.2; see mla_partial_opts_t
  * out_format) are accepted too: out_lat[j] [B, Mq, H, 512] bf16 with
  * out_lse[j] [B, Mq, H, 2] fp32 pairs (m, l), whose lse is m + ln l (-inf
- * when l = 0); every part must then be in that form.  out stays fp32.
+ * when l = 0, NaN when l is); every part must then be in that form.  out stays fp32.
  */
 mla_status_t mla_merge_partials(const mla_tensor_t* const* out_lat,
                                 const mla_tensor_t* const* out_lse, int32_t n_parts,

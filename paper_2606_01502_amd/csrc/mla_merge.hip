@@ -28,12 +28,13 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(const MergeParams p) {
   f32x4_t acc0, acc1;
   float lse;
   if (p.wire) {
-    // wire-form parts: lse = m + ln l from the (m, l) pair (-inf when l = 0)
+    // wire-form parts: lse = m + ln l from the (m, l) pair (-inf when l = 0; NaN
+    // when l is)
     lse = merge_parts<true, Bf16Rows>(
         p.n_parts,
         [&](int j) {
           const float m = p.lse[j][lo], l = p.lse[j][lo + 1];
-          return l > 0.f ? m + __logf(l) : -INFINITY;
+          return l <= 0.f ? -INFINITY : m + __logf(l);
         },
         [&](int j) { return (const uint16_t*)p.o[j] + oo; }, [](int) { return 1.f; }, acc0, acc1,
         lane);

@@ -1621,8 +1621,10 @@ void partial_kernel(const PartialParams p) {
     const float l_tot = xor_sum(l_run[rg]);
     const int row0 = row_wg0 + wave * 16 * RG + rg * 16;
     const int row = row0 + n16;
-    const float lse = l_tot > 0.f ? (m_run[rg] + __log2f(l_tot)) * kLn2 : -INFINITY;
-    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    // (a sum that is NaN, of a row that attends one, is no empty row's)
+    const bool some = l_tot != 0.f;
+    const float lse = some ? (m_run[rg] + __log2f(l_tot)) * kLn2 : -INFINITY;
+    const float inv = some ? 1.f / l_tot : 0.f;
     if (!half) {
       if (g == 0 && row < p.rows) {
         if (direct) {
@@ -1630,9 +1632,11 @@ void partial_kernel(const PartialParams p) {
           const int64_t lo = r * p.lse_s0 + i * p.lse_s1 + hd * p.lse_s2;
           if (p.out_wire) {
             // (m, l): the largest score, and the denominator relative to it
-            // (l_tot is relative to the running maximum, which is at most m)
-            p.lse[lo] = l_tot > 0.f ? m_true[rg] * kLn2 : -INFINITY;
-            p.lse[lo + 1] = l_tot > 0.f ? l_tot * __builtin_amdgcn_exp2f(m_run[rg] - m_true[rg]) : 0.f;
+            // (l_tot is relative to the running maximum, which is at most m;
+            // maxima pass over a NaN, which m has to be where l is)
+            const float m = l_tot == l_tot ? m_true[rg] * kLn2 : l_tot;
+            p.lse[lo] = some ? m : -INFINITY;
+            p.lse[lo + 1] = some ? l_tot * __builtin_amdgcn_exp2f(m_run[rg] - m_true[rg]) : 0.f;
           } else {
             p.lse[lo] = lse;
           }
@@ -2849,7 +2853,9 @@ void tile64_kernel(const PartialParams p) {
     for (int k = 0; k < NK; ++k) {
       const int rl = 32 * k + n32, row = row_wg0 + rl;
       const float l_tot = ls[k][0] + ls[k][1];
-      mult[k] = l_tot > 0.f ? recip(lw[k][0] + lw[k][1]) : 0.f;
+      // (a sum that is NaN, of a row that attends one, is no empty row's)
+      const bool some = l_tot != 0.f;
+      mult[k] = some ? recip(lw[k][0] + lw[k][1]) : 0.f;
       float row_scale = 1.f;
       if (half) {
         const float amax = fmaxf(fmaxf(fmaxf(am[k][0], am[k][1]), fmaxf(am[k][2], am[k][3])),
@@ -2858,7 +2864,7 @@ void tile64_kernel(const PartialParams p) {
         mult[k] *= 1.f / row_scale;
       }
       if (wave == k && g2 == 0 && row < p.rows) {
-        const float lse = l_tot > 0.f ? (m_all[k] + __log2f(l_tot)) * kLn2 : -INFINITY;
+        const float lse = some ? (m_all[k] + __log2f(l_tot)) * kLn2 : -INFINITY;
         const f32x2_t mt2 = *(LDS const f32x2_t*)(xtrue + 2 * rl);
         const float mt = fmaxf(mt2[0], mt2[1]);
         if (direct) {
@@ -2866,8 +2872,10 @@ void tile64_kernel(const PartialParams p) {
           const int64_t lo = r * p.lse_s0 + i * p.lse_s1 + hd * p.lse_s2;
           if (p.out_wire) {
             // (m, l): the largest score, and the denominator relative to it
-            p.lse[lo] = l_tot > 0.f ? mt * kLn2 : -INFINITY;
-            p.lse[lo + 1] = l_tot > 0.f ? l_tot * __builtin_amdgcn_exp2f(m_all[k] - mt) : 0.f;
+            // (maxima pass over a NaN, which m has to be where l is)
+            const float m = l_tot == l_tot ? mt * kLn2 : l_tot;
+            p.lse[lo] = some ? m : -INFINITY;
+            p.lse[lo + 1] = some ? l_tot * __builtin_amdgcn_exp2f(m_all[k] - mt) : 0.f;
           } else {
             p.lse[lo] = lse;
           }

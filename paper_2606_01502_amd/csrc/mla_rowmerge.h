@@ -4,7 +4,8 @@
 // Per row, over the live parts (lse != -inf):
 //   L = max lse_j,  lse = L + ln sum exp(lse_j - L),  out = sum exp(lse_j - lse) o_j.
 // A part with lse = -inf is skipped (its o is never read, so a NaN there
-// cannot leak); no live part gives out = 0, lse = -inf.  The wave reads the
+// cannot leak); no live part gives out = 0, lse = -inf.  A part whose lse is NaN is
+// live: the maximum passes over it, the sum does not, and the row is NaN.  The wave reads the
 // row's part lse values lane-parallel (lane j holds part j), reduces max and
 // sum across the wave, and then visits only the live parts, eight at a time,
 // with each lane moving two 16-byte vectors per part (columns 4*lane and
@@ -122,45 +123,45 @@ __device__ __forceinline__ float merge_row(int n, LseAt lse_at, RowAt row_at, Sc
     if (j < n) m = fmaxf(m, lse_at(j));
   }
   m = wave_max(m);
+  // (no live part but such as are NaN: the sum below says which; of none it is 0,
+  // whose logarithm is the -inf of an empty row)
+  m = m == -INFINITY ? 0.f : m;
   acc0 = f32x4_t{0.f, 0.f, 0.f, 0.f};
   acc1 = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float lse = -INFINITY;
-  if (m != -INFINITY) {
-    float s = 0.f;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-      const int j = j0 + lane;
-      const float l = j < n ? lse_at(j) : -INFINITY;
-      if (l != -INFINITY) s += __expf(l - m);
-    }
-    lse = m + __logf(wave_sum(s));
-    for (int j0 = 0; j0 < n; j0 += 64) {
-      const int j = j0 + lane;
-      const float l = j < n ? lse_at(j) : -INFINITY;
-      const float w = l != -INFINITY ? __expf(l - lse) * scale_at(j) : 0.f;
-      uint64_t live = __ballot(l != -INFINITY);
-      while (live) {
-        int idx[kBatch];
-        int cnt = 0;
+  float s = 0.f;
+  for (int j0 = 0; j0 < n; j0 += 64) {
+    const int j = j0 + lane;
+    const float l = j < n ? lse_at(j) : -INFINITY;
+    if (l != -INFINITY) s += __expf(l - m);
+  }
+  const float lse = m + __logf(wave_sum(s));
+  for (int j0 = 0; j0 < n; j0 += 64) {
+    const int j = j0 + lane;
+    const float l = j < n ? lse_at(j) : -INFINITY;
+    const float w = l != -INFINITY ? __expf(l - lse) * scale_at(j) : 0.f;
+    uint64_t live = __ballot(l != -INFINITY);
+    while (live) {
+      int idx[kBatch];
+      int cnt = 0;
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-          idx[k] = live ? __builtin_ctzll(live) : idx[0];
-          if (live) {
-            live &= live - 1;
-            ++cnt;
-          }
+      for (int k = 0; k < kBatch; ++k) {
+        idx[k] = live ? __builtin_ctzll(live) : idx[0];
+        if (live) {
+          live &= live - 1;
+          ++cnt;
         }
-        // raw values first (converted at use), so that no load waits for another
-        typename Rows::Raw v0[kBatch], v1[kBatch];
+      }
+      // raw values first (converted at use), so that no load waits for another
+      typename Rows::Raw v0[kBatch], v1[kBatch];
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-          if (k < cnt) Rows::load_raw(row_at, j0 + idx[k], lane, v0[k], v1[k]);
+      for (int k = 0; k < kBatch; ++k)
+        if (k < cnt) Rows::load_raw(row_at, j0 + idx[k], lane, v0[k], v1[k]);
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-          if (k < cnt) {
-            const float wk = lane_value(w, idx[k]);
-            acc0 += wk * Rows::cvt(v0[k]);
-            acc1 += wk * Rows::cvt(v1[k]);
-          }
+      for (int k = 0; k < kBatch; ++k) {
+        if (k < cnt) {
+          const float wk = lane_value(w, idx[k]);
+          acc0 += wk * Rows::cvt(v0[k]);
+          acc1 += wk * Rows::cvt(v1[k]);
         }
       }
     }
@@ -273,7 +274,7 @@ __device__ __forceinline__ void combine_row(const P& p, int S, int64_t part0, in
   m2 = wave_max(m2);
   if (lane == 0) {
     const float m = m2 * 0.69314718055994530942f;
-    p.lse[lo] = lse == -INFINITY ? -INFINITY : m;
+    p.lse[lo] = lse == -INFINITY || lse != lse ? lse : m;
     p.lse[lo + 1] = lse == -INFINITY ? 0.f : __expf(lse - m);
   }
 }
