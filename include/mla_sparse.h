@@ -157,7 +157,9 @@ typedef struct {
  *   out_lse = ln sum_T exp(s_t),   out_lat = sum_T exp(s_t - out_lse) * ckv_t,
  * and for an empty T: out_lat = 0, out_lse = -inf.  No mask, no positions.
  * Where a score is NaN (a NaN in the row or in a token it attends), out_lat and
- * out_lse are NaN (wire: both m and l), in any number of splits.
+ * out_lse are NaN (wire: both m and l), in any number of splits.  (Selections per
+ * query row: an infinity or a NaN in a block may reach out_lat of rows of the job
+ * that select other blocks, not of rows that select none.)
  *
  * Layout: q and out rows may be strided on the R, Mq and H dims (16-byte
  * aligned rows); pools must be contiguous and 16-byte aligned.  Slot order
@@ -313,7 +315,8 @@ typedef struct {
  * 0)).  Scores, weights and splits are those of mla_sparse_partial_attn, as are
  * the layout rules, the limits of scale, the workspace and graph capture.  What the
  * cache holds behind a sequence's last token is not used, whatever it is (within
- * it, an infinity or a NaN may reach rows that do not see its token); blocks
+ * it, an infinity or a NaN may reach out_lat of rows that do not see its token
+ * but others, not of empty rows); blocks
  * past NB, and those whose table entry is outside [0, P) (a window may let go of
  * the blocks behind it), are left out.  A request's work is that of the blocks its
  * rows see; plans are made for the NB blocks that the table is wide, so a table

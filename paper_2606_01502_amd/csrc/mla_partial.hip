@@ -1625,6 +1625,10 @@ void partial_kernel(const PartialParams p) {
     const bool some = l_tot != 0.f;
     const float lse = some ? (m_run[rg] + __log2f(l_tot)) * kLn2 : -INFINITY;
     const float inv = some ? 1.f / l_tot : 0.f;
+    // A row without a token: the weights it had in other rows' blocks are 0, its sums
+    // NaN where such a block holds one.  It is put right behind the stores (selecting
+    // ahead of them would spill).
+    const bool blank = (PR || WIN) && __ballot(!some && row < p.rows) != 0;
     if (!half) {
       if (g == 0 && row < p.rows) {
         if (direct) {
@@ -1655,6 +1659,10 @@ void partial_kernel(const PartialParams p) {
           asm volatile("" : "+a"(v));  // read in place, no copy back
           *(u16x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_bf16(v * inv);
         }
+        if (blank && !some) {
+#pragma unroll 1
+          for (int dt = 0; dt < 32; ++dt) *(u16x4_t*)(dst + 4 * (4 * dt + g)) = u16x4_t{};
+        }
       } else if (row < p.rows) {
         float* dst;
         if (direct) {
@@ -1669,6 +1677,10 @@ void partial_kernel(const PartialParams p) {
           asm volatile("" : "+a"(v));  // read in place, no copy back
           *(f32x4_t*)(dst + 4 * (4 * dt + g)) = v * inv;
         }
+        if (blank && !some) {
+#pragma unroll 1
+          for (int dt = 0; dt < 32; ++dt) *(f32x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_t{};
+        }
       }
       continue;
     }
@@ -1681,6 +1693,10 @@ void partial_kernel(const PartialParams p) {
       v *= inv;
       amax = fmaxf(amax, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
       *(LDS f32x4_t*)(stage + n16 * 2048 + (((4 * dt + g) ^ n16) << 4)) = v;
+    }
+    if (blank && !some) {
+#pragma unroll 1
+      for (int dt = 0; dt < 32; ++dt) *(LDS f32x4_t*)(stage + n16 * 2048 + (((4 * dt + g) ^ n16) << 4)) = f32x4_t{};
     }
     amax = xor_max(amax);
     const float row_scale = amax > 0.f ? amax : 1.f;
@@ -2838,6 +2854,7 @@ void tile64_kernel(const PartialParams p) {
   lds_barrier();
   // the rows' statistics, both halves before the first store (their LDS trips overlap)
   float mult[NK];
+  bool none[NK];  // the row has no token
   {
     f32x2_t ls[NK], lw[NK];
     f32x4_t am[NK], an[NK];
@@ -2855,6 +2872,7 @@ void tile64_kernel(const PartialParams p) {
       const float l_tot = ls[k][0] + ls[k][1];
       // (a sum that is NaN, of a row that attends one, is no empty row's)
       const bool some = l_tot != 0.f;
+      none[k] = !some && row < p.rows;
       mult[k] = some ? recip(lw[k][0] + lw[k][1]) : 0.f;
       float row_scale = 1.f;
       if (half) {
@@ -2885,6 +2903,20 @@ void tile64_kernel(const PartialParams p) {
           if (p.out_wire) p.ws_max[part * p.rows + row] = mt;
         }
       }
+    }
+  }
+  if constexpr (PR || WIN) {
+    // (the weights it had in other rows' stages are 0, its sums NaN where such a stage
+    // holds one)
+    bool any = none[0];
+    if constexpr (NK == 2) any = any || none[1];
+    if (__ballot(any) != 0) {
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[d][k][i] = none[k] ? 0.f : O[d][k][i];
     }
   }
   // A lane holds 4 neighbouring columns of row 32 k + n32 at a time, 8 apart;

@@ -192,7 +192,7 @@ __device__ __forceinline__ void store_row(uint16_t* out, f32x4_t acc0, f32x4_t a
 // re-read part n - 1, which the cache serves).  Rows of dead parts are read
 // but never enter the sum: with kGuard (callers' parts, which may hold NaN
 // there) a part is added only when live; without it (the split-K workspace,
-// whose rows are always finite) a dead part is added with weight 0.  Same
+// whose dead parts' rows are 0) a dead part is added with weight 0.  Same
 // arithmetic and order as merge_row.  n >= 1 (the merge takes 1..64 parts,
 // the combine two splits or more).
 template <int N, bool kGuard, typename Rows, typename LseAt, typename RowAt, typename ScaleAt>

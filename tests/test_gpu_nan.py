@@ -147,3 +147,84 @@ def test_a_partial_and_its_merge():
             torch.cuda.synchronize()
             assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
             assert torch.isfinite(out[1]).all() and torch.isfinite(lse[1]).all()
+
+
+# ---------------------------------------------------------------- rows without a token
+@pytest.mark.parametrize("wire", [False, True])
+@pytest.mark.parametrize("n_splits", [0, 1, 2, 20])
+@pytest.mark.parametrize("H,row_tile", [(5, 64), (12, 64), (12, 128)])
+@pytest.mark.parametrize("kv", T.KVS)
+def test_rows_without_a_token_are_empty(kv, H, row_tile, n_splits, wire):
+    """Padding rows and rows at negative positions, in one tile with rows that
+    attend a NaN: 0, and the statistics of an empty row."""
+    print(f"case: nan beside empty rows {kv} {H} {row_tile} {n_splits} {wire}", flush=True)
+    if kv == "mx4" and row_tile == 128:
+        return  # refused
+    c, ql, qp, table = inputs(13, 2, 6, H, 24, kv)
+    lens, q_lens = [24 * 64 - 3, 2], [4, 6]  # of the second: rows 0 to 3 lie ahead of its start
+    poison(c, table[0, 2], 5)
+    poison(c, table[1, 0], 0)
+    for window, sinks in ((0, 0), (3, 200)):
+        out, stat = mla.window_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(lens), SCALE, window=window,
+                                    n_sink=sinks, q_lens=T.i32(q_lens), n_splits=n_splits, row_tile=row_tile,
+                                    wire=wire, **c.scales)
+        torch.cuda.synchronize()
+        empty = np.zeros((2, 6), bool)
+        empty[0, 4:] = empty[1, :4] = True
+        o, st = T.host(out), T.host(stat)
+        assert (o[empty] == 0).all() and np.isnan(o[~empty]).all() and np.isnan(st[~empty]).all()
+        assert np.isneginf(st[empty][..., 0] if wire else st[empty]).all() and (not wire or (st[empty][..., 1] == 0).all())
+
+
+@pytest.mark.parametrize("wire", [False, True])
+@pytest.mark.parametrize("n_splits", [30, 60])
+@pytest.mark.parametrize("sinks", [2, 1900])  # (few splits a row; more than a wave reads in one trip)
+@pytest.mark.parametrize("kv,H,row_tile", [("bf16", 1, 64), ("bf16", 2, 64), ("bf16", 1, 128), ("fp8", 1, 64), ("fp8", 1, 128),
+                                           ("fp8split", 1, 64), ("mx4", 1, 64), ("mx4", 2, 64)])
+def test_splits_without_a_token(kv, H, row_tile, sinks, n_splits, wire):
+    """Splits of a stage or two: rows that see none of the tokens of a NaN's split
+    are what they were, however many splits they have; rows that see it are NaN."""
+    print(f"case: nan in other rows' split {kv} {H} {row_tile} {sinks} {n_splits} {wire}", flush=True)
+    Mq, n, window = 128 // H, 2570, 8
+    c, ql, qp, table = inputs(15, 1, Mq, H, 41, kv)
+    n_splits += 24 if sinks > 1000 else 0
+
+    def call():
+        return mla.window_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32([n]), SCALE, window=window, n_sink=sinks,
+                               n_splits=n_splits, row_tile=row_tile, wire=wire, **c.scales)
+    want = [t.clone() for t in call()]
+    t = n - 2
+    poison(c, table[0, t // 64], t % 64)
+    got = call()
+    torch.cuda.synchronize()
+    pos = n - Mq + np.arange(Mq)
+    sees = pos >= t
+    # The NaN is in the last split.  A call takes at most K splits, K the blocks that a
+    # tile may see: with 2 sinks 3 or 4 for as many stages, one a split; with 1900
+    # sinks 32 or 33, for 33 stages of 64 tokens, or 62 or 63 of 32, two in the last.
+    first = t // 64 * 64 if row_tile == 128 else t // 32 * 32 - (32 if sinks > 1000 else 0)
+    apart = pos < first
+    assert sees.sum() == 2 and apart.sum() > 20
+    for a, b in zip(got, want):
+        assert torch.isnan(a[0][T.host(torch.from_numpy(sees)).astype(bool)]).all()
+        keep = torch.from_numpy(apart).cuda()
+        assert torch.equal(a[0][keep], b[0][keep])
+
+
+def test_rows_with_an_empty_selection_of_their_own():
+    """Rows that select nothing beside rows that attend a NaN."""
+    for kv in ("bf16", "fp8", "fp8split"):
+        for H, row_tile in ((5, 64), (12, 64), (12, 128)):
+            for n_splits in (0, 1, 3):
+                for wire in (False, True):
+                    print(f"case: nan beside empty selections {kv} {H} {row_tile} {n_splits} {wire}", flush=True)
+                    c, ql, qp, table = inputs(17, 2, 3, H, 12, kv)
+                    sel = np.tile(np.arange(9), (2, 3, 1))
+                    sel[:, 1] = -1
+                    poison(c, table[0, 4], 9)
+                    out, stat = mla.sparse_partial_attn(ql, qp, c.ckv, c.kpe, T.i32(table), T.i32(sel), SCALE,
+                                                        wire=wire, n_splits=n_splits, row_tile=row_tile, **c.scales)
+                    torch.cuda.synchronize()
+                    assert (out[:, 1] == 0).all() and torch.isneginf(stat[:, 1, :, 0] if wire else stat[:, 1]).all()
+                    assert torch.isnan(out[0, 0]).all() and torch.isnan(stat[0, 2]).all()
+                    assert torch.isfinite(out[1]).all()
