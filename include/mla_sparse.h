@@ -464,8 +464,9 @@ typedef struct {
   int32_t inverse;    /* 1: turn back, which is also the gradient's way: the
                          transpose of the map, mscale included                     */
   int32_t reserved;   /* must be zero                                              */
-  double base;        /* > 0 (YARN: > 1); no pair may turn more than 2^20 times a
-                         position                                                  */
+  double base;        /* > 0 (YARN: > 1); no pair may turn more than once a position
+                         (those of a base >= 1 and a factor >= 1 turn at most a
+                         sixth)                                                    */
   double factor;      /* LINEAR, YARN: s > 0                                       */
   double beta_fast;   /* YARN: turns in orig_len from which a pair keeps its angle */
   double beta_slow;   /* YARN: turns up to which a pair is slowed s times, > 0     */
@@ -488,8 +489,8 @@ enum { MLA_ROPE_PLAIN = 0, MLA_ROPE_LINEAR = 1, MLA_ROPE_YARN = 2 };
  *   positions [T] int32, any value
  *   out       [T, H, D] of x's type, written; may be x itself (same data and
  *             strides), must not overlap it otherwise
- * Angles are reduced in fp64, products are formed in fp32, each value is rounded
- * once.  Rows need no alignment; 16-byte aligned ones with D, the offset and
+ * Angles are reduced in fp64 (positions of 2^31: within 2^-20 of a turn), products
+ * are formed in fp32, each value is rounded once.  Rows need no alignment; 16-byte aligned ones with D, the offset and
  * (half) the rotated part multiples of 16 bytes go in 16-byte accesses. */
 mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, const mla_tensor_t* out,
                       const mla_rope_opts_t* opts, void* stream);

@@ -3,9 +3,10 @@
 //
 // Pair i of a row at position p becomes m (x cos a - y sin a, x sin a + y cos a),
 // a = p w_i; the angular frequencies w_i (long-context scaling included) come
-// from the host in turns a position, in double.  p w_i is formed and reduced to
-// one turn in double (a position of 2^31 leaves 2^-22 of a turn), cos and sin of
-// the rest in fp32, the products in fp32, one rounding to the output's type.
+// from the host in turns a position, in double, at most one.  p w_i is formed and
+// reduced to one turn in double (a position of 2^31 leaves 2^-22 of a turn, and the
+// host's roundings of w_i as much three times), cos and sin of the rest in fp32, the
+// products in fp32, one rounding to the output's type.
 //
 // A stream through HBM: each value read once, written once.  What bounds small
 // calls is the launch and the trip; large ones the copy rate.  A workgroup takes

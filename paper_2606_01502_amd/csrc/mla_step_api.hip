@@ -195,9 +195,13 @@ mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, cons
     p.mscale = (float)opts->mscale;
     p.sin_scale = opts->inverse ? -p.mscale : p.mscale;
     rope_turns(*opts, p.turns);
-    // (a position is at most 2^31, and doubles hold the products' whole turns up to 2^53)
+    // What a position of 2^31 leaves of a turn: a double holds 2^31 turns to 2^-22 of one,
+    // more of them to less, 2^51 (a pair of 2^20 turns) to half a turn.
     for (int i = 0; i < half; ++i)
-      if (!(p.turns[i] <= 1048576.0)) return fail(MLA_ERR_INVALID_ARGUMENT, "opts: a pair turns more than 2^20 times a position");
+      if (!(p.turns[i] <= 1.0))
+        return fail(MLA_ERR_INVALID_ARGUMENT,
+                    "opts: a pair turns more than once a position, where far positions lose their angle (at 2^20 turns "
+                    "a position of 2^31 all of it)");
     return launched(mla::launch_rope(p, reinterpret_cast<hipStream_t>(stream)), "rope");
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");
