@@ -426,9 +426,12 @@ def batch_slots(cached_lens, new_lens, free_blocks, block_table, n_tokens=None, 
 def prepare_rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=10000.0,
                  scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0, mscale=1.0,
                  inverse=False, stream=None):
-    """rope with every argument fixed (see prepare_partial)."""
+    """rope with every argument fixed (see prepare_partial).  No gradients go
+    through the call: x must not require them where they are recorded."""
     if x.dim() != 3:
         raise ValueError("x must be [T, H, D]")
+    if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+        raise ValueError("gradients go through rope(x, ...) without out only: detach x, or call under no_grad")
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     _on_current_gpu(x, positions, out)
@@ -440,6 +443,23 @@ def prepare_rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, 
                      (d, o, x, positions), out)
 
 
+class _Rope(torch.autograd.Function):
+    """rope with its gradient, the transposed map: a rope that turns back."""
+
+    @staticmethod
+    def forward(ctx, x, positions, opts, inverse, stream):
+        ctx.save_for_backward(positions)
+        ctx.opts, ctx.inverse = opts, inverse
+        return prepare_rope(x, positions, None, *opts, inverse, stream)()
+
+    @staticmethod
+    def backward(ctx, g):
+        positions, = ctx.saved_tensors
+        # (the gradient of a sum is one number under strides of 0)
+        g = g if g.stride(2) == 1 else g.contiguous()
+        return rope(g, positions, None, *ctx.opts, not ctx.inverse), None, None, None, None
+
+
 def rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=10000.0,
          scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0, mscale=1.0,
          inverse=False, stream=None):
@@ -448,9 +468,13 @@ def rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=100
     positions[t], the others are copied.  pairing 0: dims (2i, 2i+1), 1: (i,
     i + rot_dim/2); scaling "none", "linear" (factor) or "yarn" (factor,
     orig_len, beta_fast, beta_slow); out may be x.  inverse=True is the
-    transpose of the map, which takes gradients of out to gradients of x."""
-    return prepare_rope(x, positions, out, rot_offset, rot_dim, pairing, base, scaling, factor,
-                        orig_len, beta_fast, beta_slow, mscale, inverse, stream)()
+    transpose of the map, which takes gradients of out to gradients of x: an x
+    that requires them gets them (the one call here that records any), without
+    out."""
+    opts = (rot_offset, rot_dim, pairing, base, scaling, factor, orig_len, beta_fast, beta_slow, mscale)
+    if out is None and torch.is_grad_enabled() and x.requires_grad:
+        return _Rope.apply(x, positions, opts, inverse, stream)
+    return prepare_rope(x, positions, out, *opts, inverse, stream)()
 
 
 def prepare_cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):

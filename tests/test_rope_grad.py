@@ -1,0 +1,161 @@
+"""Gradients through rope: against autograd over the formula in 64 bits and
+against differences, in every layout that a gradient arrives in; the calls that
+cannot carry any refuse an input that requires them."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_01502_amd import mla
+
+SCALINGS = [dict(), dict(scaling="linear", factor=8.0), dict(scaling="yarn", factor=40.0, orig_len=4096, mscale=1.25)]
+
+
+def angles(pos, d, base, scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0):
+    i = torch.arange(d // 2, dtype=torch.float64)
+    w = base ** (-2.0 * i / d)
+    if scaling == "linear":
+        w = w / factor
+    if scaling == "yarn":
+        lo = max(math.floor(d / 2 * math.log(orig_len / (2 * math.pi * beta_fast), base)), 0)
+        hi = min(math.ceil(d / 2 * math.log(orig_len / (2 * math.pi * beta_slow), base)), d - 1)
+        r = ((i - lo) / max(hi - lo, 0.001)).clamp(0, 1)
+        w = w * (1 - r) + w / factor * r
+    return pos.double()[:, None] * w
+
+
+def formula(x, pos, at, d, pairing, inverse, mscale=1.0, base=1e4, **kw):
+    """x [T, H, D] float64, differentiable."""
+    a = angles(pos, d, base, **kw)[:, None] * (-1 if inverse else 1)
+    c, s = a.cos() * mscale, a.sin() * mscale
+    v = x[..., at:at + d]
+    u, w = (v[..., 0::2], v[..., 1::2]) if pairing == 0 else (v[..., :d // 2], v[..., d // 2:])
+    y = u * c - w * s, u * s + w * c
+    y = torch.stack(y, -1).flatten(-2) if pairing == 0 else torch.cat(y, -1)
+    return torch.cat([x[..., :at], y, x[..., at + d:]], -1)
+
+
+def close(got, ref, mag, steps):
+    """Off by the roundings of the type, half a step each, and fp32 arithmetic
+    (2^-20 of the magnitudes of the pair, which mag bounds)."""
+    half = torch.finfo(got.dtype).eps / 2
+    err = (got.double().cpu() - ref).abs()
+    assert (err <= (steps * half * 1.01 + 2.0 ** -20) * mag + 1e-30).all(), float((err / mag).max())
+
+
+def test_calls_that_carry_no_gradient_refuse():
+    x, pos = torch.zeros(2, 1, 64, requires_grad=True), torch.zeros(2, dtype=torch.int32)
+    out = torch.zeros(2, 1, 64)
+    for f in (lambda: mla.prepare_rope(x, pos), lambda: mla.rope(x, pos, out=out), lambda: mla.rope(x, pos, out=x),
+              lambda: mla.rope(out, pos, out=x), lambda: mla.prepare_rope(out, pos, out=x)):
+        with pytest.raises(ValueError, match="gradients go through"):
+            f()
+    with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):  # (past that check)
+        mla.rope(x, pos, out=out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("scaling", range(3))
+@pytest.mark.parametrize("pairing", [0, 1])
+@pytest.mark.parametrize("T,H,D,at,d", [(1, 1, 64, 0, 64), (5, 8, 192, 128, 64), (33, 3, 37, 3, 22), (0, 2, 64, 0, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradient_of_the_formula(T, H, D, at, d, pairing, scaling, inverse, dtype):
+    print(f"case: rope gradient {T} {H} {D} {at} {d} {pairing} {scaling} {inverse} {dtype}", flush=True)
+    g = torch.Generator().manual_seed(T + D)
+    x = torch.randn((T, H, D), generator=g).to(dtype).cuda().requires_grad_()
+    w = torch.randn((T, H, D), generator=g).to(dtype)
+    pos = torch.randint(0, 100000, (T,), generator=g)
+    kw = dict(pairing=pairing, inverse=inverse, **SCALINGS[scaling])
+    y = mla.rope(x, pos.int().cuda(), rot_offset=at, rot_dim=d, **kw)
+    assert y.requires_grad and y.dtype == dtype
+    y.backward(w.cuda())
+    xd = x.detach().double().cpu().requires_grad_()
+    ref = formula(xd, pos, at, d, **kw)
+    ref.backward(w.double())
+    m = kw.get("mscale", 1.0)
+    close(x.grad, xd.grad, 2 * m * w.double().abs().amax(-1, keepdim=True) if T else xd.grad, 1)
+    close(y.detach(), ref.detach(), 2 * m * xd.detach().abs().amax(-1, keepdim=True) if T else ref.detach(), 1)
+
+
+@pytest.mark.gpu
+def test_gradient_of_differences():
+    """The map is linear: a difference over a step of 1 is its derivative."""
+    print("case: rope differences", flush=True)
+    x = torch.randn((3, 2, 16), generator=torch.Generator().manual_seed(1)).cuda()
+    w = torch.randn((3, 2, 16), generator=torch.Generator().manual_seed(2)).cuda()
+    pos = torch.tensor([0, 17, 4001], dtype=torch.int32).cuda()
+    kw = dict(rot_offset=4, rot_dim=10, pairing=1, mscale=1.25)
+    leaf = x.clone().requires_grad_()
+    (mla.rope(leaf, pos, **kw) * w).sum().backward()
+    for t, h, c in [(0, 0, 0), (1, 1, 4), (1, 0, 9), (2, 1, 13), (2, 0, 15)]:
+        up = x.clone()
+        up[t, h, c] += 1
+        slope = ((mla.rope(up, pos, **kw).double() - mla.rope(x, pos, **kw).double()) * w.double()).sum()
+        # (two values of a pair, each a rounding of |x| + 1 <= 6 off on both sides)
+        assert abs(float(slope - leaf.grad[t, h, c])) <= 4 * 2.0 ** -22 * 6 * 1.25 * float(w.abs().max())
+
+
+@pytest.mark.gpu
+def test_layouts_sums_and_second_derivatives():
+    """Gradients that are one number, strided or of a part; inputs that are views,
+    broadcast or used twice; the gradient's own gradient; no history where none is asked for."""
+    print("case: rope gradient layouts", flush=True)
+    gen = torch.Generator().manual_seed(5)
+    pos = torch.arange(6, dtype=torch.int32)
+    dpos = pos.cuda()
+
+    def both(fn, *leaves):
+        mine = [t.cuda().requires_grad_() for t in leaves]
+        ref = [t.double().requires_grad_() for t in leaves]
+        got = fn(lambda x, **kw: mla.rope(x, dpos, **kw), mine)
+        want = fn(lambda x, **kw: formula(x, pos, kw.get("rot_offset", 0), kw.get("rot_dim", x.shape[2]),
+                                          kw.get("pairing", 0), kw.get("inverse", False)), ref)
+        for a, b in zip(got, want):
+            # (sums of up to 24 products of numbers below 6, four roundings each)
+            assert (a.detach().double().cpu() - b.detach()).abs().max() <= 24 * 36 * 4 * 2.0 ** -23
+
+    x, y = torch.randn((6, 4, 32), generator=gen), torch.randn((4, 6, 40), generator=gen)
+    row = torch.randn((1, 1, 32), generator=gen)
+
+    def total(f, t):
+        return torch.autograd.grad(f(t[0]).sum(), t)
+
+    def transposed(f, t):
+        out = f(t[0].transpose(0, 1)[..., 8:], pairing=1)
+        return torch.autograd.grad((out.transpose(0, 1)[1:] ** 2).sum(), t)
+
+    def broadcast(f, t):
+        return torch.autograd.grad(f(t[0].expand(6, 4, 32))[:, ::3].sum(), t)
+
+    def twice(f, t):
+        return torch.autograd.grad((f(t[0]) * f(t[0], pairing=1, rot_offset=8, rot_dim=16)).sum(), t)
+
+    def second(f, t):
+        first, = torch.autograd.grad((f(t[0]) ** 3).sum(), t[:1], create_graph=True)
+        return torch.autograd.grad((first * t[1]).sum(), t)
+
+    both(total, x)
+    both(transposed, y)
+    both(broadcast, row)
+    both(twice, x)
+    both(second, x * 0.5, torch.randn((6, 4, 32), generator=gen) * 0.5)
+    leaf = x.cuda().requires_grad_()
+    with torch.no_grad():
+        assert not mla.rope(leaf, dpos).requires_grad
+        assert mla.prepare_rope(leaf, dpos)().grad_fn is None
+    assert mla.rope(leaf.detach(), dpos).grad_fn is None
+
+
+@pytest.mark.gpu
+def test_on_a_stream_of_its_own():
+    print("case: rope gradient on a stream", flush=True)
+    s = torch.cuda.Stream()
+    x = torch.randn((2000, 16, 64), generator=torch.Generator().manual_seed(7)).cuda().requires_grad_()
+    pos = torch.arange(2000, dtype=torch.int32).cuda()
+    want, = torch.autograd.grad((mla.rope(x, pos) ** 2).sum(), x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        got, = torch.autograd.grad((mla.rope(x, pos) ** 2).sum(), x)
+    s.synchronize()
+    assert torch.equal(got, want)
