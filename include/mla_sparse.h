@@ -67,10 +67,12 @@ typedef enum {
 
 /* A 4-bit latent row (OCP MX with E2M1 elements): the 512 codes of a token, two
  * to a byte, the even column in the low half, then 16 exponent bytes, one for
- * each 32 columns: value = E2M1 code * 2^(byte - 127); byte 255 is NaN.  The last
- * dim of a descriptor of this type counts bytes.  Values of less than 2^-126
- * (bytes 0 and 1) may read as 0.  The RoPE pool beside it holds bf16: 400 bytes
- * a token. */
+ * each 32 columns: value = E2M1 code * 2^(byte - 127); byte 255 is NaN.  Every
+ * value is a bf16 number but those past its largest (bytes 253 and 254), which read
+ * as infinities; mla_cache_append writes bytes 2 .. 252 and 255.  In attention
+ * values of less than 2^-126 (bytes 0 and 1) may count as 0.  The last dim of a
+ * descriptor of this type counts bytes.  The RoPE pool beside it holds bf16: 400
+ * bytes a token. */
 #define MLA_MX4_ROW 272
 
 /* A strided view of device memory.  shape/stride beyond ndim are ignored;

@@ -6,12 +6,13 @@
 
 namespace mla {
 
-// The scale of exponent byte b: 2^(b - 127); 255 is NaN.
+// The scale of exponent byte b: 2^(b - 127); 255 is NaN.  (The conversions take the
+// exponent field alone, whose 0 is 2^-127: byte 0 is no zero.)
 __device__ __forceinline__ float mx4_scale(uint32_t b) {
   return __uint_as_float(b == 255u ? 0x7FC00000u : b << 23);
 }
 
-// Two codes (byte N of w) times s -> two bf16, exact for a normal result.
+// Two codes (byte N of w) times s -> two bf16, exact unless past bf16's largest.
 template <int N>
 __device__ __forceinline__ uint32_t mx4x2_bf16(uint32_t w, float s) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, N));
