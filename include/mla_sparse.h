@@ -42,6 +42,9 @@
 extern "C" {
 #endif
 
+/* Raised when a call that was there changes.  Entries and types that have come to
+ * version 4 since (mla_window_attn, mla_batch_slots, mla_rope, mla_cache_append,
+ * MXFP4 pools) are told by their symbols. */
 #define MLA_SPARSE_VERSION 4
 
 #define MLA_DLAT 512  /* latent width = d_v (Section 3.2)                    */
@@ -269,7 +272,7 @@ mla_status_t mla_sparse_partial_attn_noalloc(const mla_tensor_t* q_lat,
  * and the layout rules are those of mla_sparse_partial_attn_ex; opts.n_splits
  * counts splits of the token slots (each split takes whole 64-token groups
  * of slots, at most 1024 slots).  Caches of every type (with fp8, a token takes
- * the scales of its pool block); NB and P must not exceed 2^25 blocks
+ * the scales of its pool block); NB and P must be less than 2^25 blocks
  * (MLA_ERR_UNSUPPORTED).  An id
  * outside [0, 64 NB), or a table entry outside [0, P), is a caller error that
  * the call does not detect on the host: such a slot is skipped.
@@ -325,7 +328,7 @@ typedef struct {
  * view as wide as the longest sequence serves best.  Automatic splits of up to 256
  * requests follow what each one's rows see, on the GPU, where windows reach over
  * more than half the table: a result then depends, within its rounding, on the
- * lengths of its neighbours too.  NB at most 2^25 blocks
+ * lengths of its neighbours too.  NB less than 2^25 blocks
  * (MLA_ERR_UNSUPPORTED).
  */
 mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,

@@ -366,7 +366,7 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
     if (R > INT32_MAX || Mq * H > (1 << 24) || K > INT32_MAX || NB > INT32_MAX || P > INT32_MAX)
       return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the int32 index range");
     if (tokens && (NB > (INT32_MAX >> 6) || P > (INT32_MAX >> 6)))
-      return fail(MLA_ERR_UNSUPPORTED, "token selections: NB or P beyond 2^25 blocks");
+      return fail(MLA_ERR_UNSUPPORTED, "token selections: NB or P of 2^25 blocks or more");
 
     const Extent outs[2] = {extent(*out_lat), extent(*out_lse)};
     auto scale_extent = [&](const float* sc) -> Extent {

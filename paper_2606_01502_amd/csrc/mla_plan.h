@@ -180,7 +180,8 @@ struct Planner {
          {{6.6, 1.87, 5.5e6}, {9.4, 2.32, 5.5e6}, {9.4, 2.30, 5.5e6}, {14.1, 4.16, 5.5e6}}},
         {{{5.0, 1.99, 6.6e6}, {7.8, 2.19, 6.1e6}, {8.5, 2.17, 8.7e6}, {14.2, 3.78, 5.0e6}},
          {{5.7, 2.38, 5.5e6}, {8.4, 2.64, 5.5e6}, {9.2, 2.49, 5.5e6}, {14.5, 4.89, 5.5e6}}}};
-    // 4-bit caches: 64-row tiles only, fitted to 256 work items of 2 .. 64 blocks
+    // 4-bit caches: 64-row tiles only, fitted to 256 work items of 2 .. 64 blocks, and
+    // taken for token selections too, which were not timed apart
     static constexpr Rate kRateMx4[3] = {{6.6, 2.1, 5.5e6}, {11.0, 2.45, 5.5e6}, {11.0, 2.3, 5.5e6}};
     const int kind = rg == 2 ? 3 : rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
     const Rate& rate = a.mx4 && kind < 3 ? kRateMx4[kind] : kRate[a.tokens][a.fp8][kind];
@@ -212,6 +213,9 @@ struct Planner {
     // least, so that there is something to share out.  128 requests of 128 4-bit rows:
     // 281 to 16,379 tokens 620 -> 457 us, 127 of 300 tokens and one of 16,384 614 -> 82,
     // all of 16,384 649 -> 687; from 128 blocks on, for all of 4096 take 169 -> 209.
+    // The split rows' 64 MiB do not bind here: those of 512 tiles in two splits are up
+    // to 256 MiB (held in fp32, as one split would have), and no window has to fit
+    // the allocation-free entry's array.
     const bool two = may_share() && a.K >= 128 && a.R * row_tiles_of(2) <= 2 * a.cus;
     if (two && plan.S == 1) plan.us = INFINITY;
     for (int rg = 1; rg <= 2; ++rg) {
