@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import functools
 import os
 import struct
 
@@ -213,12 +214,22 @@ def _on_one_gpu(*tensors):
     return first
 
 
-def _on_current_gpu(*tensors):
-    """_on_one_gpu, and that device is the current one, whose stream the call
-    goes to."""
+def _on_current_gpu(*tensors, stream=None):
+    """_on_one_gpu, and that device is the current one, on whose stream (or the
+    given one, of the same device) the call goes, and in whose memory its
+    workspace lies.  Returns its index."""
     dev = _on_one_gpu(*tensors)
     if dev != torch.cuda.current_device():
         raise ValueError(f"tensors are on cuda:{dev}, which is not the current device")
+    at = getattr(stream, "device_index", dev)
+    if at != dev:
+        raise ValueError(f"tensors are on cuda:{dev}, the stream is on cuda:{at}")
+    return dev
+
+
+@functools.cache
+def _several_gpus():
+    return torch.cuda.device_count() > 1
 
 
 def _stream(stream):
@@ -241,10 +252,14 @@ class _Prepared:
     once and the tensors they point to are kept alive, so each call costs
     one foreign call (for serving loops that reuse static buffers)."""
 
-    def __init__(self, fn, args, keep, result):
+    def __init__(self, fn, args, keep, result, device):
         self._fn, self._args, self._keep, self.result = fn, args, keep, result
+        # (nothing to look at in each call where there is one device)
+        self._device = device if _several_gpus() else None
 
     def __call__(self):
+        if self._device is not None and torch.cuda.current_device() != self._device:
+            raise ValueError(f"the call was prepared on cuda:{self._device}, which is not the current device")
         st = self._fn(*self._args)
         if st != MLA_OK:
             raise MlaError(st, load().mla_last_error().decode())
@@ -266,8 +281,8 @@ def _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_
                   out_lat, out_lse, ckv_scale, kpe_scale, n_splits, row_tile, stream, wire=False):
     R = chunk_block_table.shape[0]  # jobs; q may hold fewer rows (R_q dividing R)
     out_lat, out_lse = _attn_outputs(R, q_lat, out_lat, out_lse, wire)
-    _on_one_gpu(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids, out_lat,
-                out_lse, ckv_scale, kpe_scale)
+    dev = _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids, out_lat,
+                          out_lse, ckv_scale, kpe_scale, stream=stream)
     opts = PartialOpts()
     opts.n_splits = int(n_splits)
     opts.row_tile = int(row_tile)
@@ -279,7 +294,7 @@ def _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_
         tuple(_ref(d) for d in outs) + (ctypes.byref(opts), _stream(stream))
     keep = (descs, outs, opts, q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table,
             sel_block_ids, ckv_scale, kpe_scale)
-    return args, keep, (out_lat, out_lse)
+    return args, keep, (out_lat, out_lse), dev
 
 
 def _partial_fn(lib, tokens, no_alloc):
@@ -296,11 +311,11 @@ def prepare_partial(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_bloc
     """sparse_partial_attn with every argument fixed, the stream included
     (the current one when None); calling the result launches the work and
     returns (out_lat, out_lse)."""
-    args, keep, result = _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table,
-                                       sel_block_ids, scale, out_lat, out_lse, ckv_scale,
-                                       kpe_scale, n_splits, row_tile, stream, wire)
+    args, keep, result, dev = _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table,
+                                            sel_block_ids, scale, out_lat, out_lse, ckv_scale,
+                                            kpe_scale, n_splits, row_tile, stream, wire)
     lib = load()
-    return _Prepared(_partial_fn(lib, tokens, no_alloc), args, keep, result)
+    return _Prepared(_partial_fn(lib, tokens, no_alloc), args, keep, result, dev)
 
 
 def sparse_partial_attn(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_block_ids,
@@ -318,9 +333,9 @@ def sparse_partial_attn(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_
     wire=True (out_lat bf16 [R, Mq, H, 512], (m, l) pairs fp32 [R, Mq, H, 2]).
     """
     lib = load()
-    args, _keep, result = _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table,
-                                        sel_block_ids, scale, out_lat, out_lse, ckv_scale,
-                                        kpe_scale, n_splits, row_tile, stream, wire)
+    args, _keep, result, _ = _partial_args(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table,
+                                           sel_block_ids, scale, out_lat, out_lse, ckv_scale,
+                                           kpe_scale, n_splits, row_tile, stream, wire)
     _check(lib, _partial_fn(lib, tokens, no_alloc)(*args))
     return result
 
@@ -330,8 +345,8 @@ def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale
                    n_splits=0, stream=None, wire=False, row_tile=0):
     """window_attn with every argument fixed (see prepare_partial)."""
     out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
-    _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, *out, ckv_scale,
-                    kpe_scale)
+    dev = _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, *out, ckv_scale,
+                          kpe_scale, stream=stream)
     o = WindowOpts(int(window), int(n_sink), int(n_splits), OUT_BF16_WIRE if wire else OUT_FP32,
                    int(row_tile))
     d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale),
@@ -341,7 +356,7 @@ def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale
             _stream(stream))
     keep = (d, do, o, q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, ckv_scale,
             kpe_scale)
-    return _Prepared(load().mla_window_attn, args, keep, out)
+    return _Prepared(load().mla_window_attn, args, keep, out, dev)
 
 
 def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
@@ -370,7 +385,7 @@ def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=N
         out_ckv = torch.empty((L, K, DLAT), dtype=torch.bfloat16, device=ckv_pool.device)
     if out_kpe is None:
         out_kpe = torch.empty((L, K, DPE), dtype=torch.bfloat16, device=ckv_pool.device)
-    _on_one_gpu(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv, out_kpe)
+    _on_current_gpu(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv, out_kpe, stream=stream)
     lib = load()
     d = [_describe_latent(ckv_pool)]
     d += [describe(t) for t in (kpe_pool, chunk_block_table, sel_token_ids, out_ckv, out_kpe)]
@@ -384,7 +399,7 @@ def fetch_splice(chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table, dst_star
     paged pools at positions dst_start .. dst_start + n - 1 of the sequence
     that block_table maps, its RoPE pairs turned by delta positions
     (pairing 0: dims (2i, 2i+1), 1: dims (i, i+32))."""
-    _on_one_gpu(chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table)
+    _on_current_gpu(chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table, stream=stream)
     lib = load()
     d = [describe(t) for t in (chunk_ckv, chunk_kpe, ckv_pool, kpe_pool, block_table)]
     _check(lib, lib.mla_fetch_splice(*[_ref(x) for x in d], int(dst_start), int(delta),
@@ -406,10 +421,10 @@ def prepare_batch_slots(cached_lens, new_lens, free_blocks, block_table, n_token
     def out(t, n):
         return torch.empty(n, dtype=torch.int32, device=dev) if t is None else t
     plan = SlotPlan(slots, out(positions, slots.shape[0]), out(seq_lens, B), out(starts, B + 1), out(info, 4))
-    _on_current_gpu(cached_lens, new_lens, free_blocks, block_table, *plan)
+    gpu = _on_current_gpu(cached_lens, new_lens, free_blocks, block_table, *plan, stream=stream)
     keep = (cached_lens, new_lens, free_blocks, block_table)
     d = [describe(t) for t in (*keep, *plan)]
-    return _Prepared(load().mla_batch_slots, (*[_ref(x) for x in d], _stream(stream)), (d, keep), plan)
+    return _Prepared(load().mla_batch_slots, (*[_ref(x) for x in d], _stream(stream)), (d, keep), plan, gpu)
 
 
 def batch_slots(cached_lens, new_lens, free_blocks, block_table, n_tokens=None, slots=None,
@@ -434,13 +449,13 @@ def prepare_rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, 
         raise ValueError("gradients go through rope(x, ...) without out only: detach x, or call under no_grad")
     if out is None:
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _on_current_gpu(x, positions, out)
+    dev = _on_current_gpu(x, positions, out, stream=stream)
     o = RopeOpts(int(rot_offset), int(x.shape[2] - rot_offset if rot_dim is None else rot_dim),
                  int(pairing), ROPE_SCALINGS.index(scaling), int(bool(inverse)), 0, float(base),
                  float(factor), float(beta_fast), float(beta_slow), float(mscale), int(orig_len))
     d = [describe(t) for t in (x, positions, out)]
     return _Prepared(load().mla_rope, (*[_ref(t) for t in d], ctypes.byref(o), _stream(stream)),
-                     (d, o, x, positions), out)
+                     (d, o, x, positions), out, dev)
 
 
 class _Rope(torch.autograd.Function):
@@ -479,10 +494,10 @@ def rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=100
 
 def prepare_cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):
     """cache_append with every argument fixed (see prepare_partial)."""
-    _on_current_gpu(ckv, kpe, slots, ckv_pool, kpe_pool)
+    dev = _on_current_gpu(ckv, kpe, slots, ckv_pool, kpe_pool, stream=stream)
     d = [describe(ckv), describe(kpe), describe(slots), _describe_latent(ckv_pool), describe(kpe_pool)]
     return _Prepared(load().mla_cache_append, (*[_ref(t) for t in d], _stream(stream)),
-                     (d, ckv, kpe, slots), (ckv_pool, kpe_pool))
+                     (d, ckv, kpe, slots), (ckv_pool, kpe_pool), dev)
 
 
 def cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):
@@ -518,7 +533,7 @@ def _merge_args(parts_lat, parts_lse, out, out_lse, stream):
     if out_lse is True:
         out_lse = torch.empty(parts_lse[0].shape[:3], dtype=torch.float32,
                               device=parts_lse[0].device)
-    _on_one_gpu(*parts_lat, *parts_lse, out, out_lse if want_lse else None)
+    dev = _on_current_gpu(*parts_lat, *parts_lse, out, out_lse if want_lse else None, stream=stream)
     d_lat = [describe(t) for t in parts_lat]
     d_lse = [describe(t) for t in parts_lse]
     arr_lat = (ctypes.POINTER(Tensor) * max(n, 1))(*[ctypes.pointer(d) for d in d_lat])
@@ -527,13 +542,13 @@ def _merge_args(parts_lat, parts_lse, out, out_lse, stream):
     d_out_lse = describe(out_lse) if want_lse else None
     args = (arr_lat, arr_lse, n, _ref(d_out), _ref(d_out_lse), _stream(stream))
     keep = (d_lat, d_lse, d_out, d_out_lse, list(parts_lat), list(parts_lse))
-    return args, keep, ((out, out_lse) if want_lse else out)
+    return args, keep, ((out, out_lse) if want_lse else out), dev
 
 
 def prepare_merge(parts_lat, parts_lse, out=None, out_lse=None, stream=None):
     """merge_partials with every argument fixed (see prepare_partial)."""
-    args, keep, result = _merge_args(parts_lat, parts_lse, out, out_lse, stream)
-    return _Prepared(load().mla_merge_partials_ex, args, keep, result)
+    args, keep, result, dev = _merge_args(parts_lat, parts_lse, out, out_lse, stream)
+    return _Prepared(load().mla_merge_partials_ex, args, keep, result, dev)
 
 
 def merge_partials(parts_lat, parts_lse, out=None, out_lse=None, stream=None):
@@ -543,6 +558,6 @@ def merge_partials(parts_lat, parts_lse, out=None, out_lse=None, stream=None):
     Returns out (and the merged lse when out_lse is given or requested by
     passing out_lse=True)."""
     lib = load()
-    args, _keep, result = _merge_args(parts_lat, parts_lse, out, out_lse, stream)
+    args, _keep, result, _ = _merge_args(parts_lat, parts_lse, out, out_lse, stream)
     _check(lib, lib.mla_merge_partials_ex(*args))
     return result
