@@ -1625,10 +1625,6 @@ void partial_kernel(const PartialParams p) {
     const bool some = l_tot != 0.f;
     const float lse = some ? (m_run[rg] + __log2f(l_tot)) * kLn2 : -INFINITY;
     const float inv = some ? 1.f / l_tot : 0.f;
-    // A row without a token: the weights it had in other rows' blocks are 0, its sums
-    // NaN where such a block holds one.  It is put right behind the stores (selecting
-    // ahead of them would spill).
-    const bool blank = (PR || WIN) && __ballot(!some && row < p.rows) != 0;
     if (!half) {
       if (g == 0 && row < p.rows) {
         if (direct) {
@@ -1659,10 +1655,6 @@ void partial_kernel(const PartialParams p) {
           asm volatile("" : "+a"(v));  // read in place, no copy back
           *(u16x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_bf16(v * inv);
         }
-        if (blank && !some) {
-#pragma unroll 1
-          for (int dt = 0; dt < 32; ++dt) *(u16x4_t*)(dst + 4 * (4 * dt + g)) = u16x4_t{};
-        }
       } else if (row < p.rows) {
         float* dst;
         if (direct) {
@@ -1677,10 +1669,6 @@ void partial_kernel(const PartialParams p) {
           asm volatile("" : "+a"(v));  // read in place, no copy back
           *(f32x4_t*)(dst + 4 * (4 * dt + g)) = v * inv;
         }
-        if (blank && !some) {
-#pragma unroll 1
-          for (int dt = 0; dt < 32; ++dt) *(f32x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_t{};
-        }
       }
       continue;
     }
@@ -1693,10 +1681,6 @@ void partial_kernel(const PartialParams p) {
       v *= inv;
       amax = fmaxf(amax, fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
       *(LDS f32x4_t*)(stage + n16 * 2048 + (((4 * dt + g) ^ n16) << 4)) = v;
-    }
-    if (blank && !some) {
-#pragma unroll 1
-      for (int dt = 0; dt < 32; ++dt) *(LDS f32x4_t*)(stage + n16 * 2048 + (((4 * dt + g) ^ n16) << 4)) = f32x4_t{};
     }
     amax = xor_max(amax);
     const float row_scale = amax > 0.f ? amax : 1.f;
@@ -1727,6 +1711,38 @@ void partial_kernel(const PartialParams p) {
       *(u32x4_t*)(p.ws_o16 + (part * p.rows + rw) * kDLat + 8 * ln) = h;
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // reads of this row group done before it is overwritten
+  }
+
+  // Rows without a token: the weights they had in other rows' blocks are 0, their sums
+  // NaN where such a block holds one.  They are 0, written over what the same lanes
+  // stored above: choosing there cost every tile of per-row selections 1 to 2 us, here
+  // 8 x 16 rows of 20 blocks each, in splits that leave many rows without one, take
+  // 28.1 us for 27.2.
+  if constexpr (PR || WIN) {
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+      const int row0 = row_wg0 + wave * 16 * RG + rg * 16;
+      const int row = row0 + n16;
+      const bool none = xor_sum(l_run[rg]) == 0.f && row < p.rows;
+      const uint32_t rows_none = (uint32_t)__ballot(none) & 0xffffu;
+      if (rows_none == 0) continue;
+      if (half) {
+#pragma unroll 1
+        for (int rr = 0; rr < 16; ++rr)
+          if (rows_none >> rr & 1) *(u32x4_t*)(p.ws_o16 + (part * p.rows + row0 + rr) * kDLat + 8 * ln) = u32x4_t{};
+      } else if (none) {
+        const int i = div_by(row, p.by_H), hd = row - i * p.H;
+        const int64_t oo = r * p.out_s0 + i * p.out_s1 + hd * p.out_s2;
+        if (direct && p.out_wire) {
+#pragma unroll 1
+          for (int dt = 0; dt < 32; ++dt) *(u16x4_t*)(p.out16 + oo + 4 * (4 * dt + g)) = u16x4_t{};
+        } else {
+          float* const dst = direct ? p.out + oo : p.ws_o32 + (part * p.rows + row) * kDLat;
+#pragma unroll 1
+          for (int dt = 0; dt < 32; ++dt) *(f32x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_t{};
+        }
+      }
+    }
   }
 }
 
