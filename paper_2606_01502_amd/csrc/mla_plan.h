@@ -181,7 +181,7 @@ struct Planner {
         {{{5.0, 1.99, 6.6e6}, {7.8, 2.19, 6.1e6}, {8.5, 2.17, 8.7e6}, {14.2, 3.78, 5.0e6}},
          {{5.7, 2.38, 5.5e6}, {8.4, 2.64, 5.5e6}, {9.2, 2.49, 5.5e6}, {14.5, 4.89, 5.5e6}}}};
     // 4-bit caches: 64-row tiles only, fitted to 256 work items of 2 .. 64 blocks, and
-    // taken for token selections too, which were not timed apart
+    // taken for token selections too, which were not fitted apart
     static constexpr Rate kRateMx4[3] = {{6.6, 2.1, 5.5e6}, {11.0, 2.45, 5.5e6}, {11.0, 2.3, 5.5e6}};
     const int kind = rg == 2 ? 3 : rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
     const Rate& rate = a.mx4 && kind < 3 ? kRateMx4[kind] : kRate[a.tokens][a.fp8][kind];
