@@ -485,7 +485,8 @@ def rope(x, positions, out=None, rot_offset=0, rot_dim=None, pairing=0, base=100
     orig_len, beta_fast, beta_slow); out may be x.  inverse=True is the
     transpose of the map, which takes gradients of out to gradients of x: an x
     that requires them gets them (the one call here that records any), without
-    out."""
+    out.  A graph that captures the backward captures its forward too, and takes
+    the gradients by torch.autograd.grad."""
     opts = (rot_offset, rot_dim, pairing, base, scaling, factor, orig_len, beta_fast, beta_slow, mscale)
     if out is None and torch.is_grad_enabled() and x.requires_grad:
         return _Rope.apply(x, positions, opts, inverse, stream)

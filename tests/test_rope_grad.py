@@ -159,3 +159,35 @@ def test_on_a_stream_of_its_own():
         got, = torch.autograd.grad((mla.rope(x, pos) ** 2).sum(), x)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_forward_and_backward_in_a_graph():
+    print("case: rope gradient captured", flush=True)
+    gen = torch.Generator().manual_seed(11)
+    x, w = (torch.randn((300, 5, 64), generator=gen).bfloat16().cuda() for _ in range(2))
+    x.requires_grad_()
+    pos = torch.arange(300, dtype=torch.int32).cuda()
+    side = torch.cuda.Stream()
+
+    def step():
+        y = mla.rope(x, pos, pairing=1, rot_offset=8, rot_dim=48)
+        return y.detach(), torch.autograd.grad(y, x, w)[0]
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        y, gx = step()
+    for k in range(4):
+        with torch.no_grad():
+            x.copy_(torch.randn(x.shape, generator=gen))
+            w.copy_(torch.randn(x.shape, generator=gen))
+            pos.copy_(torch.randint(0, 9000, (300,), generator=gen))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        side.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(gx, want[1])
