@@ -44,7 +44,8 @@ extern "C" {
 
 /* Raised when a call that was there changes.  Entries and types that have come to
  * version 4 since (mla_window_attn, mla_batch_slots, mla_rope, mla_cache_append,
- * MXFP4 pools) are told by their symbols. */
+ * MXFP4 pools, mla_rope_append, mla_block_means, mla_block_scores, mla_select_topk,
+ * mla_prefix_attn) are told by their symbols. */
 #define MLA_SPARSE_VERSION 4
 
 #define MLA_DLAT 512  /* latent width = d_v (Section 3.2)                    */
@@ -294,7 +295,9 @@ typedef struct {
   int32_t out_format;  /* MLA_OUT_FP32 or MLA_OUT_BF16_WIRE                        */
   int32_t row_tile;    /* rows per work item: 64 or 128 (0 = automatic; 4-bit
                           caches: 64)                                              */
-  int32_t reserved[3]; /* must be zero                                             */
+  int32_t whole_blocks; /* 1: a window begins with the block that its first token
+                          lies in (what mla_block_scores leaves to it)             */
+  int32_t reserved[2]; /* must be zero                                             */
 } mla_window_opts_t;
 
 /*
@@ -315,7 +318,8 @@ typedef struct {
  *
  * Row i < q_lens[b] sits at position p = seq_lens[b] - q_lens[b] + i and sees the
  * tokens t <= p with t > p - window, or t < n_sink (window 0: all t <= p; n_sink
- * then says nothing).  A row that sees no token, as the rows from q_lens[b] on
+ * then says nothing; whole_blocks: t > p - window is t >= 64 floor((p - window + 1) /
+ * 64)).  A row that sees no token, as the rows from q_lens[b] on
  * and those at negative positions, is empty: out_lat 0, out_lse -inf (wire: (-inf,
  * 0)).  Scores, weights and splits are those of mla_sparse_partial_attn, as are
  * the layout rules, the limits of scale, the workspace and graph capture.  What the
@@ -337,6 +341,58 @@ mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe
                              const mla_tensor_t* q_lens, float scale, const mla_tensor_t* out_lat,
                              const mla_tensor_t* out_lse, const mla_window_opts_t* opts,
                              void* stream);
+
+/* Options of mla_prefix_attn. */
+typedef struct {
+  int32_t n_splits;    /* split-K: splits of a prefix (0 = automatic)              */
+  int32_t own_splits;  /* and of a request's own tokens (0 = automatic)            */
+  int32_t out_format;  /* MLA_OUT_FP32 or MLA_OUT_BF16_WIRE                        */
+  int32_t reserved[5]; /* must be zero                                             */
+} mla_prefix_opts_t;
+
+/*
+ * Attention for a batch that shares long prefixes (a document, an instruction): the
+ * requests of a group attend its prefix, which is cached once and read once for all
+ * of their rows, and each its own tokens behind it.
+ *
+ *   q_lat [B, Mq, H, 512], q_pe [B, Mq, H, 64] bf16   a q per request; requests and
+ *                                     query rows must be one dim (stride of B = Mq x
+ *                                     stride of Mq, where both are more than 1)
+ *   ckv_pool, kpe_pool                as mla_sparse_partial_attn takes them: bf16,
+ *                                     fp8-e4m3fn or MXFP4
+ *   prefix_table [G, NBP] int32       logical block of group g's prefix -> pool block
+ *   prefix_lens  [G] int32            tokens of the prefix
+ *   group_starts [G + 1] int32        group g is the requests group_starts[g] ..
+ *                                     group_starts[g + 1] - 1 (none: an empty group).
+ *                                     They must not fall; the first group begins with
+ *                                     request 0 and the last ends with B - 1, whatever
+ *                                     its first and last entry say
+ *   block_table  [B, NB] int32        as mla_window_attn's, of the tokens behind the
+ *                                     prefix
+ *   seq_lens     [B] int32            of those tokens, the query rows' own among them
+ *   q_lens       [B] int32 or NULL    as there
+ *   out_lat, out_lse                  as mla_sparse_partial_attn's, in either form;
+ *                                     requests and query rows one dim, as in q
+ *
+ * Row i < q_lens[b] of request b in group g sees all of the first prefix_lens[g]
+ * tokens of prefix_table[g], and of its own those up to position seq_lens[b] -
+ * q_lens[b] + i (none where that is negative); the rows from q_lens[b] on are empty:
+ * out_lat 0, out_lse -inf (wire: (-inf, 0)).  Positions are the caller's: nothing is
+ * rotated.  Blocks past a table's width and those whose entry is outside [0, P) are
+ * left out, what the cache holds behind a sequence's last token is not used, NaN and
+ * infinities are as in mla_window_attn.  Starts that fall are a caller error that is
+ * not detected: rows of the batch may then come out undefined.  One launch for
+ * prefixes and own tokens, one that joins them; the workspace, its limits and graph
+ * capture as in mla_sparse_partial_attn (nothing to fall back on where it cannot
+ * grow).  G at most 4096, B Mq H less than 2^30, tables less than 2^25 blocks wide
+ * (MLA_ERR_UNSUPPORTED). */
+mla_status_t mla_prefix_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
+                             const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
+                             const mla_tensor_t* prefix_table, const mla_tensor_t* prefix_lens,
+                             const mla_tensor_t* group_starts, const mla_tensor_t* block_table,
+                             const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,
+                             const mla_tensor_t* out_lat, const mla_tensor_t* out_lse,
+                             const mla_prefix_opts_t* opts, void* stream);
 
 /*
  * Log-sum-exp merge of n_parts partials of the same rows (the requester's
@@ -518,6 +574,92 @@ mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, cons
 mla_status_t mla_cache_append(const mla_tensor_t* ckv, const mla_tensor_t* kpe,
                               const mla_tensor_t* slots, const mla_tensor_t* ckv_pool,
                               const mla_tensor_t* kpe_pool, void* stream);
+
+/* mla_rope_append: mla_rope of the RoPE parts and mla_cache_append in one call: new
+ * tokens into the paged cache, the position rotation applied on the way.
+ *   ckv, kpe, slots, ckv_pool, kpe_pool   as mla_cache_append takes them, kpe as
+ *                                     projected, not rotated
+ *   positions [T] int32               of each token, any value
+ *   opts                              as mla_rope takes them, of heads of 64 dims
+ * The cache receives what mla_rope would write of kpe (fp32 products and sum, rounded
+ * once to bf16; fused in another order, so that now and then a last bit differs). */
+mla_status_t mla_rope_append(const mla_tensor_t* ckv, const mla_tensor_t* kpe,
+                             const mla_tensor_t* positions, const mla_tensor_t* slots,
+                             const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
+                             const mla_rope_opts_t* opts, void* stream);
+
+/*
+ * ---- The choice of the blocks that a query row attends: the mean keys of whole
+ * blocks, a cheap score of each block by them, the best ones.
+ *
+ *     mla_rope_append -> mla_block_means -> mla_block_scores -> mla_select_topk ->
+ *     mla_sparse_partial_attn + mla_window_attn (whole_blocks) -> mla_merge_partials
+ *
+ * mla_block_means: the mean keys of blocks that have become whole.
+ *   ckv_pool, kpe_pool                as mla_sparse_partial_attn takes them: bf16,
+ *                                     fp8-e4m3fn with scales or MXFP4
+ *   slots [T] int32                   pool tokens (block * 64 + row), as
+ *                                     mla_batch_slots writes them: for each that is
+ *                                     its block's last row (row 63, which is
+ *                                     written last) that block's mean is formed;
+ *                                     others, and those outside [0, 64 P), are
+ *                                     passed over.  A block may be named twice
+ *   means [P, 576] bf16               contiguous, 16-byte aligned: row b is written
+ *                                     with the mean of block b's 64 entries, latent
+ *                                     then RoPE part, summed in fp32 and rounded
+ *                                     once; no other row is */
+mla_status_t mla_block_means(const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
+                             const mla_tensor_t* slots, const mla_tensor_t* means, void* stream);
+
+/* Options of mla_block_scores. */
+typedef struct {
+  int32_t window;   /* the last tokens up to a row's own, which it attends anyway:
+                       as mla_window_attn's with whole_blocks (0: none but those
+                       of a block that is not whole yet)                         */
+  int32_t n_sink;   /* first tokens of the sequence that every row attends anyway */
+  int32_t n_splits; /* splits of a request's blocks (0 = automatic)               */
+  int32_t reserved[5]; /* must be zero                                            */
+} mla_scores_opts_t;
+
+/*
+ * mla_block_scores: how much of its attention each query row's heads would give the
+ * blocks of its sequence, if a block's keys were their mean.
+ *   q_lat [B, Mq, H, 512], q_pe [B, Mq, H, 64] bf16   as mla_window_attn takes them
+ *   means [P, 576] bf16               mla_block_means'
+ *   block_table [B, NB], seq_lens [B], q_lens [B] or NULL int32   as there
+ *   scale                             as there
+ *   scores [B, Mq, NB] fp32           written (rows may be strided)
+ *
+ * Row i < q_lens[b], at position p = seq_lens[b] - q_lens[b] + i, may choose from
+ * the blocks j with 64 j >= n_sink and 64 (j + 1) <= p - window + 1, whose table entry
+ * lies in [0, P): with s_hj = scale (q_lat,h . k_lat,j + q_pe,h . k_pe,j) and k_j the
+ * block's mean key,
+ *   scores[b, i, j] = sum over h of exp(s_hj) / sum over those j' of exp(s_hj'),
+ * and -inf for every other block.  So with n_sink a multiple of 64 a row's choice
+ * and what mla_window_attn with whole_blocks = 1 attends share no token, and cover
+ * all if all are chosen.  Logits are bf16 products summed in fp32, weights and
+ * sums fp32; a logit of a row and block it may choose that is NaN or +inf makes all
+ * its scores NaN.  Splits leave two floats a row and split in the workspace of
+ * mla_sparse_partial_attn; where that cannot grow (graph capture) the call takes
+ * one split.  NB less than 2^25 blocks, Mq x H at most 2^24 (MLA_ERR_UNSUPPORTED). */
+mla_status_t mla_block_scores(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
+                              const mla_tensor_t* means, const mla_tensor_t* block_table,
+                              const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,
+                              const mla_tensor_t* scores, const mla_scores_opts_t* opts,
+                              void* stream);
+
+/*
+ * mla_select_topk: the K best scores of each row, as a selection that
+ * mla_sparse_partial_attn (block scores) or mla_sparse_partial_attn_tokens (token
+ * scores) takes.
+ *   scores [B, Mq, N] or [R, N] fp32  rows may be strided
+ *   ids    [B, Mq, K] or [R, K] int32 written: the places of the K largest scores in
+ *                                     rising order; of equal ones the first are
+ *                                     taken; -inf is never taken: -1 follows the
+ *                                     last place of a row that has fewer than K
+ * NaN ranks above all other values, -0 equals 0.  N and K may be any size (K more
+ * than N too); at most 2^29 rows (MLA_ERR_UNSUPPORTED). */
+mla_status_t mla_select_topk(const mla_tensor_t* scores, const mla_tensor_t* ids, void* stream);
 
 /*
  * The closed-form cost model of the three redistribution primitives and the

@@ -43,6 +43,11 @@ std::mutex g_ws_mutex;
 std::map<std::pair<int, hipStream_t>, Workspace> g_ws;
 std::vector<void*> g_ws_retired;
 
+}  // namespace
+
+namespace mla {
+namespace host {
+
 mla_status_t get_workspace(hipStream_t stream, size_t bytes, void** out,
                            std::unique_lock<std::mutex>& lock) {
   int dev = 0;
@@ -75,6 +80,24 @@ mla_status_t get_workspace(hipStream_t stream, size_t bytes, void** out,
   return MLA_OK;
 }
 
+int device_cus() {
+  static int cus = 0;
+  if (cus == 0) {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) == hipSuccess &&
+        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
+      cus = n;
+    else
+      cus = 256;
+  }
+  return cus;
+}
+
+}  // namespace host
+}  // namespace mla
+
+namespace {
+
 // The split-K workspace of mla_sparse_partial_attn_noalloc: a static device
 // array that the runtime places on every GPU the library runs on, held until
 // the process ends.  Host code never uses its name as an address (on the host
@@ -102,63 +125,6 @@ mla_status_t scratch_address(void** out) {
     g_scratch_ptr[dev] = ptr;
   }
   *out = g_scratch_ptr[dev];
-  return MLA_OK;
-}
-
-int device_cus() {
-  static int cus = 0;
-  if (cus == 0) {
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-      cus = n;
-    else
-      cus = 256;
-  }
-  return cus;
-}
-
-bool shape_is(const mla_tensor_t* t, std::initializer_list<int64_t> s) {
-  int d = 0;
-  for (int64_t v : s)
-    if (t->shape[d++] != v) return false;
-  return true;
-}
-
-// The pools of an attention call: types, shapes, then layout.  The latent pool is
-// bf16, e4m3 (the RoPE pool alike, both with scales) or 4 bits (the RoPE pool bf16).
-mla_status_t check_pool_types(const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool) {
-  const int32_t kv_dtype = ckv_pool->dtype;
-  if (kv_dtype != MLA_DTYPE_BF16 && kv_dtype != MLA_DTYPE_FP8_E4M3FN && kv_dtype != MLA_DTYPE_MXFP4)
-    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: dtype must be bf16 or fp8-e4m3fn or mxfp4");
-  const bool fp8 = kv_dtype == MLA_DTYPE_FP8_E4M3FN;
-  mla_status_t st;
-  if ((st = check_tensor(ckv_pool, "ckv_pool", kv_dtype, 3, fp8)) != MLA_OK) return st;
-  const int32_t pe_dtype = kv_dtype == MLA_DTYPE_MXFP4 ? (int32_t)MLA_DTYPE_BF16 : kv_dtype;
-  if ((st = check_tensor(kpe_pool, "kpe_pool", pe_dtype, 3, fp8)) != MLA_OK) return st;
-  if (fp8 && (!ckv_pool->block_scale || !kpe_pool->block_scale))
-    return fail(MLA_ERR_INVALID_ARGUMENT, "fp8 pools need block_scale");
-  return MLA_OK;
-}
-
-int64_t latent_row(const mla_tensor_t& ckv_pool) { return ckv_pool.dtype == MLA_DTYPE_MXFP4 ? MLA_MX4_ROW : MLA_DLAT; }
-
-mla_status_t check_pool_shapes(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
-  const int64_t P = ckv_pool.shape[0];
-  if (!shape_is(&ckv_pool, {P, MLA_BLOCK, latent_row(ckv_pool)}))
-    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: shape must be [P, 64, 512] (MXFP4: [P, 64, 272])");
-  if (!shape_is(&kpe_pool, {P, MLA_BLOCK, MLA_DPE}))
-    return fail(MLA_ERR_INVALID_ARGUMENT, "kpe_pool: shape must be [P, 64, 64] with the P of ckv_pool");
-  return MLA_OK;
-}
-
-mla_status_t check_pool_layout(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
-  const int64_t row = latent_row(ckv_pool);
-  if (ckv_pool.stride[0] != MLA_BLOCK * row || ckv_pool.stride[1] != row ||
-      kpe_pool.stride[0] != MLA_BLOCK * MLA_DPE || kpe_pool.stride[1] != MLA_DPE)
-    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be contiguous");
-  if (!aligned16(ckv_pool.data) || !aligned16(kpe_pool.data))
-    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
   return MLA_OK;
 }
 
@@ -405,9 +371,10 @@ mla_status_t partial_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
 
 // The most half blocks that the rows of a tile (of 128 rows, or 64) of a window see:
 // the window of its first row and of those after it, and the sinks.
-int64_t window_halves(int64_t Mq, int64_t H, int64_t NB, int64_t window, int64_t n_sink) {
+int64_t window_halves(int64_t Mq, int64_t H, int64_t NB, int64_t window, int64_t n_sink, bool whole_blocks) {
   if (window == 0) return 2 * NB;
   const int64_t n_i = std::min<int64_t>(Mq, (128 - 1) / H + 2);  // query rows that 128 rows meet
+  if (whole_blocks) window += MLA_BLOCK - 1;
   return std::min<int64_t>(2 * NB, (n_sink + 31) / 32 + (window + n_i - 2) / 32 + 2);
 }
 
@@ -426,8 +393,9 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   if ((st = check_tensor(seq_lens, "seq_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (q_lens && (st = check_tensor(q_lens, "q_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (!opts) return bad("opts: null pointer");
-  for (int i = 0; i < 3; ++i)
+  for (int i = 0; i < 2; ++i)
     if (opts->reserved[i]) return bad("opts.reserved must be zero");
+  if (opts->whole_blocks != 0 && opts->whole_blocks != 1) return bad("opts.whole_blocks must be 0 or 1");
   if (opts->row_tile != 0 && opts->row_tile != 64 && opts->row_tile != 128)
     return bad("opts.row_tile must be 0, 64 or 128");
   if (opts->row_tile == 128 && ckv_pool->dtype == MLA_DTYPE_MXFP4)
@@ -477,7 +445,7 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
 
   // splits are cut on the GPU, out of what each tile's rows see; the plan goes by
   // the most that can be
-  const int64_t K = (window_halves(Mq, H, NB, opts->window, opts->n_sink) + 1) / 2;
+  const int64_t K = (window_halves(Mq, H, NB, opts->window, opts->n_sink, opts->whole_blocks != 0) + 1) / 2;
   const bool mx4 = ckv_pool->dtype == MLA_DTYPE_MXFP4;
   const mla::Planner planner({B, Mq, H, NB, K, false, false, fp8, opts->n_splits, mx4 ? 64 : opts->row_tile,
                               device_cus(), mx4, true});
@@ -489,8 +457,148 @@ mla_status_t window_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   p.win_qlens = q_lens ? (const int32_t*)q_lens->data : nullptr;
   p.window = opts->window;
   p.n_sink = opts->n_sink;
+  p.win_lo_mask = opts->whole_blocks ? -MLA_BLOCK : -1;
   return enqueue(planner, p, B, cache_kind(*ckv_pool, *kpe_pool), mla::kSelWindow, false,
                  reinterpret_cast<hipStream_t>(stream));
+}
+
+// Requests and query rows of a [B, Mq, ..] tensor are one dim; its stride.
+bool one_dim(const mla_tensor_t& t, int64_t* stride) {
+  const int64_t B = t.shape[0], Mq = t.shape[1];
+  if (B > 1 && Mq > 1 && t.stride[0] != Mq * t.stride[1]) return false;
+  *stride = Mq > 1 ? t.stride[1] : t.stride[0];
+  return true;
+}
+
+mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, const mla_tensor_t* ckv_pool,
+                         const mla_tensor_t* kpe_pool, const mla_tensor_t* prefix_table,
+                         const mla_tensor_t* prefix_lens, const mla_tensor_t* group_starts,
+                         const mla_tensor_t* block_table, const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens,
+                         float scale, const mla_tensor_t* out_lat, const mla_tensor_t* out_lse,
+                         const mla_prefix_opts_t* opts, void* stream) {
+  auto bad = [](const std::string& m) { return fail(MLA_ERR_INVALID_ARGUMENT, m); };
+  mla_status_t st;
+  if ((st = check_tensor(q_lat, "q_lat", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
+  if ((st = check_tensor(q_pe, "q_pe", MLA_DTYPE_BF16, 4)) != MLA_OK) return st;
+  if (!ckv_pool || !kpe_pool) return bad("ckv_pool/kpe_pool: null descriptor");
+  if ((st = check_pool_types(ckv_pool, kpe_pool)) != MLA_OK) return st;
+  if ((st = check_tensor(prefix_table, "prefix_table", MLA_DTYPE_INT32, 2)) != MLA_OK) return st;
+  if ((st = check_tensor(prefix_lens, "prefix_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if ((st = check_tensor(group_starts, "group_starts", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if ((st = check_tensor(block_table, "block_table", MLA_DTYPE_INT32, 2)) != MLA_OK) return st;
+  if ((st = check_tensor(seq_lens, "seq_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if (q_lens && (st = check_tensor(q_lens, "q_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if (!opts) return bad("opts: null pointer");
+  for (int i = 0; i < 5; ++i)
+    if (opts->reserved[i]) return bad("opts.reserved must be zero");
+  if (opts->n_splits < 0) return bad("opts.n_splits must be >= 0");
+  if (opts->own_splits < 0) return bad("opts.own_splits must be >= 0");
+  if (opts->out_format != MLA_OUT_FP32 && opts->out_format != MLA_OUT_BF16_WIRE)
+    return bad("opts.out_format must be MLA_OUT_FP32 or MLA_OUT_BF16_WIRE");
+  const bool wire = opts->out_format == MLA_OUT_BF16_WIRE;
+  if ((st = check_tensor(out_lat, "out_lat", wire ? MLA_DTYPE_BF16 : MLA_DTYPE_FP32, 4)) != MLA_OK) return st;
+  if ((st = check_tensor(out_lse, "out_lse", MLA_DTYPE_FP32, wire ? 4 : 3)) != MLA_OK) return st;
+
+  const int64_t B = block_table->shape[0], NB = block_table->shape[1], P = ckv_pool->shape[0];
+  const int64_t G = prefix_table->shape[0], NBP = prefix_table->shape[1];
+  const int64_t Mq = q_lat->shape[1], H = q_lat->shape[2];
+  if (!shape_is(q_lat, {B, Mq, H, MLA_DLAT})) return bad("q_lat: shape must be [B, Mq, H, 512] with the B of block_table");
+  if (!shape_is(q_pe, {B, Mq, H, MLA_DPE})) return bad("q_pe: shape must be [B, Mq, H, 64]");
+  if ((st = check_pool_shapes(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
+  if (G < 1) return bad("prefix_table: at least one group");
+  if (!contiguous(*prefix_lens, {G})) return bad("prefix_lens: must be contiguous [G]");
+  if (!contiguous(*group_starts, {G + 1})) return bad("group_starts: must be contiguous [G + 1]");
+  if (!contiguous(*seq_lens, {B})) return bad("seq_lens: must be contiguous [B]");
+  if (q_lens && !contiguous(*q_lens, {B})) return bad("q_lens: must be contiguous [B]");
+  if (!shape_is(out_lat, {B, Mq, H, MLA_DLAT})) return bad("out_lat: shape must be [B, Mq, H, 512]");
+  if (!wire && !shape_is(out_lse, {B, Mq, H})) return bad("out_lse: shape must be [B, Mq, H]");
+  if (wire && (!shape_is(out_lse, {B, Mq, H, 2}) || out_lse->stride[3] != 1))
+    return bad("out_lse: the wire form takes [B, Mq, H, 2] (m, l) pairs");
+  if ((st = check_pool_layout(*ckv_pool, *kpe_pool)) != MLA_OK) return st;
+  if (!rows_aligned(*q_lat, 2) || !rows_aligned(*q_pe, 2)) return bad("q_lat/q_pe rows must be 16-byte aligned");
+  if (!rows_aligned(*out_lat, wire ? 2 : 4)) return bad("out_lat rows must be 16-byte aligned");
+  if (wire && !pairs_aligned(*out_lse)) return bad("out_lse (m, l) pairs must be 8-byte aligned");
+  if (!rows_apart(*out_lat) || !rows_apart(*out_lse)) return bad("out_lat / out_lse: rows overlap");
+  if (!(std::fabs(scale) <= 18446744073709551616.0f)) return bad("scale must be finite with |scale| <= 2^64");
+  if (G > 4096) return fail(MLA_ERR_UNSUPPORTED, "more than 4096 groups");
+  if (B > INT32_MAX || Mq * H > (1 << 24) || NB > (INT32_MAX >> 6) || NBP > (INT32_MAX >> 6) || P > (INT32_MAX >> 1) ||
+      B * Mq * H >= (1 << 30))
+    return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the int32 index range");
+  const Extent outs[2] = {extent(*out_lat), extent(*out_lse)};
+  const bool fp8 = ckv_pool->dtype == MLA_DTYPE_FP8_E4M3FN, mx4 = ckv_pool->dtype == MLA_DTYPE_MXFP4;
+  auto scales = [&](const float* sc) -> Extent {
+    if (!fp8 || P == 0) return {0, 0};
+    return {(uintptr_t)sc, (uintptr_t)(sc + P)};
+  };
+  const Extent ins[12] = {extent(*q_lat), extent(*q_pe), extent(*ckv_pool), extent(*kpe_pool), extent(*prefix_table),
+                          extent(*prefix_lens), extent(*group_starts), extent(*block_table), extent(*seq_lens),
+                          q_lens ? extent(*q_lens) : Extent{0, 0}, scales(ckv_pool->block_scale),
+                          scales(kpe_pool->block_scale)};
+  if (overlaps(outs[0], outs[1])) return bad("out_lat and out_lse overlap");
+  for (const Extent& o : outs)
+    for (const Extent& i : ins)
+      if (overlaps(o, i)) return bad("an output overlaps an input");
+  if (B == 0 || Mq * H == 0) return MLA_OK;
+
+  mla::PartialParams p = common_params(*q_lat, *q_pe, *ckv_pool, *kpe_pool, *block_table, scale, *out_lat, *out_lse, wire);
+  if (!one_dim(*q_lat, &p.ql_s1) || !one_dim(*q_pe, &p.qp_s1) || !one_dim(*out_lat, &p.out_s1) ||
+      !one_dim(*out_lse, &p.lse_s1))
+    return fail(MLA_ERR_UNSUPPORTED, "q and out: requests and query rows must be one dim");
+  const mla::PrefixPlan plan = mla::plan_prefix({B, G, NBP, NB, p.rows, device_cus(), opts->n_splits, opts->own_splits, fp8, mx4});
+  if (plan.grid > (1 << 22)) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
+  p.q_jobs = (int32_t)B;
+  p.q_rep = 1;
+  p.win_lens = (const int32_t*)seq_lens->data;
+  p.win_qlens = q_lens ? (const int32_t*)q_lens->data : nullptr;
+  p.win_lo_mask = -1;
+  p.grp_starts = (const int32_t*)group_starts->data;
+  p.grp_lens = (const int32_t*)prefix_lens->data;
+  p.grp_table = (const int32_t*)prefix_table->data;
+  p.grp_table_s0 = prefix_table->stride[0];
+  p.G = (int32_t)G;
+  p.grp_NB = (int32_t)NBP;
+  p.grp_splits = (int32_t)plan.S;
+  p.grp_tiles = (int32_t)plan.tiles;
+  p.grp_grid = (int32_t)plan.prefix_grid;
+  p.own_items = (int32_t)plan.own_items;
+  p.all_rows = (int32_t)(B * p.rows);
+  p.by_grp_tiles = mla::make_div(plan.tiles);
+  p.by_Mq = mla::make_div(Mq);
+  p.n_splits = (int32_t)plan.own_S;
+  p.row_tiles = (int32_t)plan.own_tiles;
+  p.by_splits = mla::make_div(plan.own_S);
+  p.by_tiles = mla::make_div(plan.own_tiles);
+  const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  std::unique_lock<std::mutex> lock;  // held until the combine is queued
+  void* ws = nullptr;
+  if ((st = get_workspace(hs, plan.ws_bytes, &ws, lock)) != MLA_OK) return st;
+  const int64_t S = plan.S + plan.own_S, n_part_rows = S * p.all_rows;
+  p.ws_f16 = plan.ws_f16;
+  p.ws_o32 = (float*)ws;
+  p.ws_o16 = (uint16_t*)ws;
+  p.ws_scale = (float*)((char*)ws + (uint64_t)n_part_rows * mla::kDLat * (plan.ws_f16 ? 2 : 4));
+  p.ws_lse = p.ws_scale + n_part_rows;
+  p.ws_max = p.ws_lse + n_part_rows;
+  hipError_t e = mla::launch_prefix(p, cache_kind(*ckv_pool, *kpe_pool), hs);
+  if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("prefix kernel launch: ") + hipGetErrorString(e));
+  // all rows as one job's, whose splits lie one after another
+  mla::CombineParams c{};
+  c.ws_f16 = p.ws_f16;
+  c.ws_o32 = p.ws_o32;
+  c.ws_o16 = p.ws_o16;
+  c.ws_scale = p.ws_scale;
+  c.ws_lse = p.ws_lse;
+  c.ws_max = p.ws_max;
+  c.R = 1; c.S = (int32_t)S; c.Mq = (int32_t)(B * Mq); c.H = p.H; c.rows = p.all_rows;
+  c.by_H = p.by_H;
+  c.by_rows = mla::make_div(p.all_rows);
+  c.out_wire = p.out_wire;
+  c.out16 = p.out16;
+  c.out = p.out; c.out_s1 = p.out_s1; c.out_s2 = p.out_s2;
+  c.lse = p.lse; c.lse_s1 = p.lse_s1; c.lse_s2 = p.lse_s2;
+  e = mla::launch_combine(c, hs);
+  if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("combine kernel launch: ") + hipGetErrorString(e));
+  return MLA_OK;
 }
 
 }  // namespace
@@ -506,6 +614,21 @@ mla_status_t mla_window_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe
     g_last_error.clear();
     return window_call(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, scale, out_lat, out_lse, opts,
                        stream);
+  } catch (...) {
+    return fail(MLA_ERR_HIP, "internal error");
+  }
+}
+
+mla_status_t mla_prefix_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, const mla_tensor_t* ckv_pool,
+                             const mla_tensor_t* kpe_pool, const mla_tensor_t* prefix_table,
+                             const mla_tensor_t* prefix_lens, const mla_tensor_t* group_starts,
+                             const mla_tensor_t* block_table, const mla_tensor_t* seq_lens,
+                             const mla_tensor_t* q_lens, float scale, const mla_tensor_t* out_lat,
+                             const mla_tensor_t* out_lse, const mla_prefix_opts_t* opts, void* stream) {
+  try {
+    g_last_error.clear();
+    return prefix_call(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table, seq_lens,
+                       q_lens, scale, out_lat, out_lse, opts, stream);
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");
   }

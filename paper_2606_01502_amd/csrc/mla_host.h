@@ -2,8 +2,11 @@
 // of tensor descriptors.
 #pragma once
 
+#include <hip/hip_runtime.h>
+
 #include <cstdint>
 #include <initializer_list>
+#include <mutex>
 #include <string>
 
 #include "../../include/mla_sparse.h"
@@ -115,6 +118,55 @@ inline bool rows_apart(const mla_tensor_t& t) {
     hi += (t.shape[d] - 1) * t.stride[d];
   }
   return true;
+}
+
+// The split-K workspace of a stream, at least `bytes` of it (mla_api.hip); the caller
+// keeps `lock` until the kernels that use it are queued.
+mla_status_t get_workspace(hipStream_t stream, size_t bytes, void** out, std::unique_lock<std::mutex>& lock);
+int device_cus();
+
+inline bool shape_is(const mla_tensor_t* t, std::initializer_list<int64_t> s) {
+  int d = 0;
+  for (int64_t v : s)
+    if (t->shape[d++] != v) return false;
+  return true;
+}
+
+// The pools of an attention call: types, shapes, then layout.  The latent pool is
+// bf16, e4m3 (the RoPE pool alike, both with scales) or 4 bits (the RoPE pool bf16).
+inline mla_status_t check_pool_types(const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool) {
+  const int32_t kv_dtype = ckv_pool->dtype;
+  if (kv_dtype != MLA_DTYPE_BF16 && kv_dtype != MLA_DTYPE_FP8_E4M3FN && kv_dtype != MLA_DTYPE_MXFP4)
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: dtype must be bf16 or fp8-e4m3fn or mxfp4");
+  const bool fp8 = kv_dtype == MLA_DTYPE_FP8_E4M3FN;
+  mla_status_t st;
+  if ((st = check_tensor(ckv_pool, "ckv_pool", kv_dtype, 3, fp8)) != MLA_OK) return st;
+  const int32_t pe_dtype = kv_dtype == MLA_DTYPE_MXFP4 ? (int32_t)MLA_DTYPE_BF16 : kv_dtype;
+  if ((st = check_tensor(kpe_pool, "kpe_pool", pe_dtype, 3, fp8)) != MLA_OK) return st;
+  if (fp8 && (!ckv_pool->block_scale || !kpe_pool->block_scale))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "fp8 pools need block_scale");
+  return MLA_OK;
+}
+
+inline int64_t latent_row(const mla_tensor_t& ckv_pool) { return ckv_pool.dtype == MLA_DTYPE_MXFP4 ? MLA_MX4_ROW : MLA_DLAT; }
+
+inline mla_status_t check_pool_shapes(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
+  const int64_t P = ckv_pool.shape[0];
+  if (!shape_is(&ckv_pool, {P, MLA_BLOCK, latent_row(ckv_pool)}))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv_pool: shape must be [P, 64, 512] (MXFP4: [P, 64, 272])");
+  if (!shape_is(&kpe_pool, {P, MLA_BLOCK, MLA_DPE}))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "kpe_pool: shape must be [P, 64, 64] with the P of ckv_pool");
+  return MLA_OK;
+}
+
+inline mla_status_t check_pool_layout(const mla_tensor_t& ckv_pool, const mla_tensor_t& kpe_pool) {
+  const int64_t row = latent_row(ckv_pool);
+  if (ckv_pool.stride[0] != MLA_BLOCK * row || ckv_pool.stride[1] != row ||
+      kpe_pool.stride[0] != MLA_BLOCK * MLA_DPE || kpe_pool.stride[1] != MLA_DPE)
+    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be contiguous");
+  if (!aligned16(ckv_pool.data) || !aligned16(kpe_pool.data))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
+  return MLA_OK;
 }
 
 }  // namespace host

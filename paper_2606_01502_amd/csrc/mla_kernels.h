@@ -100,6 +100,16 @@ struct PartialParams {
   const int32_t* win_lens;
   const int32_t* win_qlens;
   int32_t window, n_sink;
+  int32_t win_lo_mask;  // -64: windows begin with whole blocks; else -1
+  // shared prefixes: groups of requests (first requests [G + 1], tokens, block tables),
+  // splits of a prefix and tiles of all prefixes' rows, workgroups of those (a multiple
+  // of 8), work items of the requests' own tokens, rows of the batch
+  const int32_t* grp_starts;
+  const int32_t* grp_lens;
+  const int32_t* grp_table;
+  int64_t grp_table_s0;
+  int32_t G, grp_NB, grp_splits, grp_tiles, grp_grid, own_items, all_rows;
+  Div by_grp_tiles, by_Mq;
   // windows: work items next to each other that one XCD takes, and the grid's
   // part that goes in whole rounds of them (see window_item)
   int32_t run, run_all;
@@ -218,6 +228,65 @@ struct AppendParams {
 };
 hipError_t launch_append(const AppendParams& p, hipStream_t s);
 
+// The same with the RoPE part turned by the token's position on the way.
+struct RopeAppendParams {
+  AppendParams a;
+  const int32_t* pos;               // [T]
+  int32_t at, rot, pairing;         // rotated dims at .. at + rot - 1
+  float mscale, sin_scale;          // factors of the cosine and the sine
+  double turns[kDPe / 2];           // turns a position
+};
+hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t s);
+
+// Mean keys of whole blocks.
+struct MeansParams {
+  const uint8_t* ckv;
+  const uint8_t* kpe;
+  const float* ckv_scale;  // [P] (fp8 only)
+  const float* kpe_scale;
+  const int32_t* slots;    // [T]; of those of n_slots that are a block's last row, that block's mean
+  uint16_t* means;         // [P][576] bf16
+  int64_t T, n_slots;
+};
+hipError_t launch_means(const MeansParams& p, int kv, hipStream_t s);
+
+// Scores of blocks by their mean keys: one workgroup a request, group of query rows
+// and split of its blocks.
+constexpr int kScoreChunks = 2;  // 16-row chunks a wave holds
+struct ScoresParams {
+  const uint16_t* q_lat;
+  const uint16_t* q_pe;
+  int64_t ql_s0, ql_s1, ql_s2, qp_s0, qp_s1, qp_s2;  // element strides over (request, Mq, H)
+  const uint8_t* means;    // [P][576] bf16
+  const int32_t* table;
+  int64_t table_s0, P;
+  const int32_t* lens;
+  const int32_t* q_lens;   // null: Mq
+  float* out;              // [B][Mq][NB]
+  int64_t out_s0, out_s1;
+  float* stats;            // two floats of [B][groups][chunks of a group][16 rows][splits], the largest logit and sum
+  int32_t Mq, H, NB;
+  int32_t window, first_block;
+  int32_t row_chunks;      // chunks of a query row
+  int32_t group_rows, group_chunks, n_groups;  // query rows and chunks of a group
+  int32_t n_splits, wave_rows;
+  float scale_log2;        // softmax scale * log2(e)
+  Div by_splits, by_groups, by_chunks;
+};
+hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s);
+
+// The K best of each row of N scores.
+struct TopkParams {
+  const float* x;
+  int32_t* ids;
+  int64_t x_s0, x_s1, ids_s0, ids_s1;  // element strides over (request, Mq)
+  int64_t rows;
+  int32_t N, K;
+  Div by_Mq;
+  int32_t Mq;
+};
+hipError_t launch_topk(const TopkParams& p, hipStream_t s);
+
 // Cache kinds of the partial kernel.
 constexpr int kKvBf16 = 0;
 constexpr int kKvFp8Shared = 1;  // e4m3, one scale per block for ckv and kpe
@@ -251,6 +320,9 @@ constexpr int kSelTokens = 2;
 // No selection: each query row sees the last tokens of its request's sequence,
 // and its first ones.
 constexpr int kSelWindow = 3;
+// A group's shared prefix, which all of its requests' rows see, and each request's own
+// tokens.
+constexpr int kSelPrefix = 4;
 // half blocks that one split of a window lists
 constexpr int kWindowList = kPerRowListShort;
 // Requests that splits are shared out between by length: four to a lane.
@@ -262,6 +334,7 @@ constexpr int kShareMost = 64;
 // row_groups: 2 (row tiles of 128 rows) or 1 (row tiles of 64 rows)
 hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups, int sel_kind,
                           hipStream_t s);
+hipError_t launch_prefix(const PartialParams& p, int kv, hipStream_t s);
 hipError_t launch_combine(const CombineParams& p, hipStream_t s);
 hipError_t launch_merge(const MergeParams& p, hipStream_t s);
 

@@ -17,6 +17,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mla_kernels.h"
 #include "mla_mx4.h"
 
@@ -49,8 +51,66 @@ __device__ __forceinline__ uint32_t to_codes(u32x4_t v, float s) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w3), s, 3);
 }
 
-template <bool MX4>
-__global__ __launch_bounds__(kThreads) void append_kernel(const AppendParams p) {
+// ROPE: the RoPE part of a token, two tokens to a wave, a pair of its dims to a lane:
+// lane l < rot / 2 of a half turns its pair (see mla_rope.hip: the same products and
+// one rounding), the others copy what is not turned.
+struct RopeLane {
+  int c0, c1;      // the lane's columns
+  double turns;    // of its pair a position (0: copied)
+  __device__ __forceinline__ RopeLane(const RopeAppendParams& p, int lane) {
+    const int i = lane & 31, half = p.rot >> 1;
+    if (i < half) {
+      c0 = p.at + (p.pairing == 0 ? 2 * i : i);
+      c1 = c0 + (p.pairing == 0 ? 1 : half);
+      turns = p.turns[i];
+    } else {
+      c0 = 2 * (i - half);
+      c1 = c0 + 1;
+      if (c0 >= p.at) c0 += p.rot;
+      if (c1 >= p.at) c1 += p.rot;
+      turns = 0.0;
+    }
+  }
+};
+
+// Turns the RoPE parts of tokens t0 .. t0 + n - 1 into the cache.
+__device__ __forceinline__ void rope_tokens(const RopeAppendParams& pp, int64_t t0, int n, int lane) {
+  const AppendParams& p = pp.a;
+  const RopeLane at(pp, lane);
+  for (int j = 0; j < n; j += 2) {
+    const int k = j + (lane >> 5);
+    if (k >= n) break;
+    const int64_t t = t0 + k;
+    const int32_t s = p.slots[t];
+    const uint16_t* const src = p.src_kpe + t * p.kpe_s0;
+    const uint32_t x = src[at.c0], y = src[at.c1];
+    const int32_t pos = pp.pos[t];
+    if (s < 0 || s >= p.n_slots) continue;
+    uint16_t* const dst = (uint16_t*)(p.kpe + (int64_t)s * (2 * kDPe));
+    uint16_t a = (uint16_t)x, b = (uint16_t)y;
+    if ((lane & 31) < pp.rot >> 1) {
+      double turns = (double)pos * at.turns;
+      turns -= rint(turns);
+      float sn, cs;
+      sincospif(2.0f * (float)turns, &sn, &cs);
+      cs *= pp.mscale;
+      sn *= pp.sin_scale;
+      const float xf = __uint_as_float(x << 16), yf = __uint_as_float(y << 16);
+      a = __builtin_bit_cast(uint16_t, (__bf16)(xf * cs - yf * sn));
+      b = __builtin_bit_cast(uint16_t, (__bf16)(xf * sn + yf * cs));
+    }
+    dst[at.c0] = a;
+    dst[at.c1] = b;
+  }
+}
+
+__device__ __forceinline__ const AppendParams& append_of(const AppendParams& p) { return p; }
+__device__ __forceinline__ const AppendParams& append_of(const RopeAppendParams& p) { return p.a; }
+
+template <bool MX4, class Params>
+__global__ __launch_bounds__(kThreads) void append_kernel(const Params pp) {
+  constexpr bool ROPE = std::is_same<Params, RopeAppendParams>::value;
+  const AppendParams& p = append_of(pp);
   const int lane = threadIdx.x & 63;
   const int64_t wave = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 6;
   const int64_t t0 = wave * p.wave_toks;
@@ -59,18 +119,19 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendParams p) 
   for (int k0 = 0; k0 < n; k0 += kAhead) {
     u32x4_t v[kAhead], w[kAhead];
     int64_t row[kAhead];
+    if constexpr (ROPE) rope_tokens(pp, t0 + k0, min(n - k0, kAhead), lane);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int64_t t = t0 + min(k0 + j, n - 1);  // past the end: loaded, not stored
       const int32_t s = p.slots[t];
       row[j] = k0 + j < n && s >= 0 && s < p.n_slots ? s : -1;
       v[j] = *(const u32x4_t*)(p.src_ckv + t * p.ckv_s0 + 8 * lane);
-      if (lane < 8) w[j] = *(const u32x4_t*)(p.src_kpe + t * p.kpe_s0 + 8 * lane);
+      if (!ROPE && lane < 8) w[j] = *(const u32x4_t*)(p.src_kpe + t * p.kpe_s0 + 8 * lane);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (row[j] < 0) continue;
-      if (lane < 8) *(u32x4_t*)(p.kpe + row[j] * (2 * kDPe) + 16 * lane) = w[j];
+      if (!ROPE && lane < 8) *(u32x4_t*)(p.kpe + row[j] * (2 * kDPe) + 16 * lane) = w[j];
       if constexpr (!MX4) {
         *(u32x4_t*)(p.ckv + row[j] * (2 * kDLat) + 16 * lane) = v[j];
       } else {
@@ -152,8 +213,17 @@ hipError_t launch_append(const AppendParams& p, hipStream_t s) {
   const int64_t waves = (p.T + p.wave_toks - 1) / p.wave_toks;
   const int64_t grid = (waves + 3) / 4;
   if (grid <= 0) return hipSuccess;
-  if (p.mx4) hipLaunchKernelGGL(append_kernel<true>, dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL(append_kernel<false>, dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  if (p.mx4) hipLaunchKernelGGL((append_kernel<true, AppendParams>), dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((append_kernel<false, AppendParams>), dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_append(const RopeAppendParams& p, hipStream_t s) {
+  const int64_t waves = (p.a.T + p.a.wave_toks - 1) / p.a.wave_toks;
+  const int64_t grid = (waves + 3) / 4;
+  if (grid <= 0) return hipSuccess;
+  if (p.a.mx4) hipLaunchKernelGGL((append_kernel<true, RopeAppendParams>), dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((append_kernel<false, RopeAppendParams>), dim3((uint32_t)grid), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

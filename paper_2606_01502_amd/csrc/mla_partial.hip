@@ -763,12 +763,13 @@ __device__ __forceinline__ int compact_tokens(const PartialParams& p, int r, int
 struct Window {
   int n_tok;            // tokens the sequence's table holds
   int pos0, qn, window;
+  int lo_mask;          // of the first token in a window: -1, or -64 where windows begin with blocks
   int n_sink;
   int hi_all, lo_all;   // every row of the tile sees lo_all .. hi_all
   // of query row i: the last token it sees (-1: none), and the first in its window
   __device__ __forceinline__ int hi_of(int i) const { return i < qn ? min(pos0 + i, n_tok - 1) : -1; }
   __device__ __forceinline__ int lo_of(int i) const {
-    return window ? (int)max((int64_t)pos0 + i - window + 1, (int64_t)0) : 0;
+    return window ? (int)max((int64_t)pos0 + i - window + 1, (int64_t)0) & lo_mask : 0;
   }
   // whether some row of the tile may not see all of tokens t0 .. t0 + n - 1
   __device__ __forceinline__ bool cuts(int t0, int n) const {
@@ -794,8 +795,66 @@ __device__ __forceinline__ Window window_of(const PartialParams& p, int len, int
   w.qn = min(max(q_len, 0), p.Mq);
   w.pos0 = len - w.qn;
   w.window = p.window;
+  w.lo_mask = p.win_lo_mask;
   w.n_tok = (int)min((int64_t)len, (int64_t)p.NB * kBlock);
   w.n_sink = p.window ? p.n_sink : 0;
+  return w;
+}
+
+// Shared prefixes (kSelPrefix): jobs are groups, whose rows are those of all requests
+// of a group, next to each other, and requests, over what they have of their own.
+struct PrefixItem {
+  bool prefix;
+  int job;              // group, or request
+  int i0, rows;         // first query row in the batch's B Mq, rows (query rows x heads)
+  int rt, s, n_splits;  // row tile, split
+};
+
+// The work item of workgroup `bid`; false: there is none.  Prefixes first, their row
+// tiles next to each other (one XCD's workgroups then read much the same tokens), an
+// eighth of them to each XCD.  Of the batch's rows, those of group g begin with tile
+// floor(first row / 64) + g, which leaves every group as many tiles as it may have.
+__device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int lane, PrefixItem& it) {
+  if (bid >= p.grp_grid) {  // a request's own tokens; its last rows, which see most, first
+    const int w = bid - p.grp_grid, a = div_by(w, p.by_splits), b = div_by(a, p.by_tiles);
+    it.prefix = false;
+    it.job = b;
+    it.i0 = b * p.Mq;
+    it.rows = p.rows;
+    it.rt = p.row_tiles - 1 - (a - b * p.row_tiles);
+    it.s = w - a * p.n_splits;
+    it.n_splits = p.n_splits;
+    return true;
+  }
+  const int w = (bid & 7) * (p.grp_grid >> 3) + (bid >> 3);
+  const int s = div_by(w, p.by_grp_tiles), tile = w - s * p.grp_tiles;
+  if (s >= p.grp_splits) return false;
+  auto start = [&](int g) { return g <= 0 ? 0 : g >= p.G ? p.q_jobs : min(max(p.grp_starts[g], 0), p.q_jobs); };
+  auto first_tile = [&](int g) { return (int)(((int64_t)start(g) * p.rows) >> 6) + g; };
+  // the last group whose first tile is not past this one, by two looks at 64 of them
+  const int step = (p.G + 63) >> 6;
+  int g = 0;
+  if (step > 1) g = (63 - __builtin_clzll(__ballot(lane == 0 || (lane * step < p.G && first_tile(lane * step) <= tile)))) * step;
+  g += 63 - __builtin_clzll(__ballot(lane == 0 || (lane < (step > 1 ? step : 64) && g + lane < p.G && first_tile(g + lane) <= tile)));
+  g = __builtin_amdgcn_readfirstlane(g);
+  const int b0 = __builtin_amdgcn_readfirstlane(start(g)), b1 = __builtin_amdgcn_readfirstlane(start(g + 1));
+  it.prefix = true;
+  it.job = g;
+  it.i0 = b0 * p.Mq;
+  it.rows = (b1 - b0) * p.rows;
+  it.rt = tile - ((int)(((int64_t)b0 * p.rows) >> 6) + g);
+  it.s = s;
+  it.n_splits = p.grp_splits;
+  return it.rt >= 0 && it.rt * 64 < it.rows;
+}
+
+__device__ __forceinline__ Window prefix_window(const PartialParams& p, const PrefixItem& it) {
+  if (!it.prefix) return window_of(p, p.win_lens[it.job], p.win_qlens ? p.win_qlens[it.job] : p.Mq);
+  // every row sees all of it
+  Window w{};
+  w.n_tok = (int)min((int64_t)max(p.grp_lens[it.job], 0), (int64_t)p.grp_NB * kBlock);
+  w.pos0 = w.n_tok - 1;
+  w.qn = INT32_MAX;
   return w;
 }
 
@@ -895,8 +954,8 @@ __device__ __forceinline__ bool window_shares(const PartialParams& p, int w_id, 
 // into the place of the row masks.  Those whose table entry names no pool block are
 // left out.  Returns their number.
 template <class L, int SHIFT>
-__device__ __forceinline__ int compact_window(const PartialParams& p, int r, int s, int n_splits, int i0, int n_i, int cap,
-                                              Window& w,                                              LDS uint8_t* smem, int tid) {
+__device__ __forceinline__ int compact_window(const PartialParams& p, const int32_t* table, int s, int n_splits, int i0, int n_i,
+                                              int cap, Window& w, LDS uint8_t* smem, int tid) {
   constexpr bool FP8 = L::kFp8;
   constexpr int kHalves = SHIFT == 5 ? 1 : 0;
   const int lane = tid & 63;
@@ -905,7 +964,6 @@ __device__ __forceinline__ int compact_window(const PartialParams& p, int r, int
   LDS int* first = (LDS int*)(smem + L::kMasks);
   LDS float* scales = (LDS float*)(smem + L::kScales);
   LDS int* wave_cnt = (LDS int*)(smem + L::kWaveCnt);
-  w = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
   const int i1 = i0 + n_i - 1;  // the tile's last row
   w.hi_all = i1 < w.qn ? w.hi_of(i0) : -1;
   w.lo_all = w.lo_of(i1);
@@ -919,7 +977,7 @@ __device__ __forceinline__ int compact_window(const PartialParams& p, int r, int
     int b = -1, u = 0;
     if (base + tid < n_e) {
       u = e < un.sinks ? e : un.lo + (e - un.sinks);
-      const int bb = p.table[r * p.table_s0 + (u >> kHalves)];
+      const int bb = table[u >> kHalves];
       if (bb >= 0 && bb < p.P) b = bb;
     }
     const uint64_t m = __ballot(b >= 0);
@@ -1130,7 +1188,8 @@ void partial_kernel(const PartialParams p) {
   int n_tok = 0;  // token selections: the listed tokens (n_valid counts virtual blocks)
   Window win{};
   if constexpr (WIN) {
-    n_valid = compact_window<L, 6>(p, r, s_idx, n_of, i0, n_i, L::kPerRowCap, win, smem, tid);
+    win = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
+    n_valid = compact_window<L, 6>(p, p.table + r * p.table_s0, s_idx, n_of, i0, n_i, L::kPerRowCap, win, smem, tid);
   } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                    p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
@@ -2164,7 +2223,8 @@ void tile64_kernel(const PartialParams p) {
   constexpr bool MX4 = KV == kKvMx4;
   constexpr bool PR = SEL == kSelPerRow;
   constexpr bool TOK = SEL == kSelTokens;
-  constexpr bool WIN = SEL == kSelWindow;
+  constexpr bool GRP = SEL == kSelPrefix;  // windows without bounds, over own tokens or a group's prefix
+  constexpr bool WIN = SEL == kSelWindow || GRP;
   constexpr bool kSplitScales = KV == kKvFp8Split;
   using L = Tile<FP8, PR, MX4, WIN>;
   __shared__ __attribute__((aligned(MX4 ? 1024 : 16))) uint8_t smem_raw[L::kTotal];
@@ -2182,7 +2242,11 @@ void tile64_kernel(const PartialParams p) {
   const int n16 = lane & 15, g = lane >> 4;  // S^T: row (or token) and dim group
   const int n32 = lane & 31, g2 = lane >> 5;  // O^T: row (or column) and token group
 
-  const int w_id = WIN ? window_item(p, blockIdx.x)
+  PrefixItem item{};
+  if constexpr (GRP) {
+    if (!prefix_item(p, blockIdx.x, lane, item)) return;
+  }
+  const int w_id = GRP ? 0 : WIN ? window_item(p, blockIdx.x)
                        : p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
   const bool tiles_fast = PR && p.tiles_fast;
   int s_idx, rt, r_num;
@@ -2198,7 +2262,11 @@ void tile64_kernel(const PartialParams p) {
     rt = a - r_num * p.row_tiles;
   }
   int n_of = p.n_splits, part0 = 0;  // windows: the splits of the request, and its first one
-  if constexpr (WIN) {
+  if constexpr (GRP) {
+    s_idx = item.s;
+    rt = item.rt;
+    n_of = item.n_splits;
+  } else if constexpr (WIN) {
     part0 = r_num * n_of;
     if (p.ws_share) {
       Share sh;
@@ -2216,6 +2284,9 @@ void tile64_kernel(const PartialParams p) {
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
   const int r = p.q_rep > 1 ? (r_num - rep * p.q_rep) * p.q_jobs + rep : r_num;
   const int qj = p.q_rep > 1 ? rep : r_num;
+  const int n_rows = GRP ? item.rows : p.rows;
+  // the first of the job's query rows in q
+  const int64_t q_lat0 = GRP ? item.i0 * p.ql_s1 : qj * p.ql_s0, q_pe0 = GRP ? item.i0 * p.qp_s1 : qj * p.qp_s0;
   const int slot0 = s_idx * p.slots_per_split;
   const int nslots = max(0, min(p.K - slot0, p.slots_per_split));
 
@@ -2228,7 +2299,7 @@ void tile64_kernel(const PartialParams p) {
   auto asks = [&](int stage) { return smem + L::kAsk + ask_place(stage); };
   const int row_wg0 = rt * 64;
   const int i0 = div_by(row_wg0, p.by_H);
-  const int n_i = PR || WIN ? div_by(min(row_wg0 + 64, p.rows) - 1, p.by_H) - i0 + 1 : 1;
+  const int n_i = PR || WIN ? div_by(min(row_wg0 + 64, n_rows) - 1, p.by_H) - i0 + 1 : 1;
   const int c_slot0 = PR && p.split_by_id ? 0 : slot0;
   const int c_nslots = PR && p.split_by_id ? p.K : nslots;
   int first_id = -1;
@@ -2246,10 +2317,10 @@ void tile64_kernel(const PartialParams p) {
   auto issue_q = [&]() {
     if (!act) return;
     const int row0 = row_wg0 + 8 * wave;
-    const int rc = min(row0, p.rows - 1);
+    const int rc = min(row0, n_rows - 1);
     const int qi = __builtin_amdgcn_readfirstlane(div_by(rc, p.by_H));
     int qh = rc - qi * p.H;
-    const uint16_t* ql = p.q_lat + (qj * p.ql_s0 + qi * p.ql_s1 + qh * p.ql_s2);
+    const uint16_t* ql = p.q_lat + (q_lat0 + qi * p.ql_s1 + qh * p.ql_s2);
     const int64_t wrap = p.ql_s1 - (int64_t)(p.H - 1) * p.ql_s2;
     // key32 of rows 8 w + j, less j's part
     const uint32_t lat = (uint32_t)((lane ^ (((wave & 1) << 1) | ((wave >> 1) & 1))) << 4);
@@ -2257,17 +2328,17 @@ void tile64_kernel(const PartialParams p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       Issue32<false, false>::go(lat ^ (uint32_t)((j & 3) << 6), (const uint8_t*)ql, dst + (uint32_t)j * 1024u);
-      if (row0 + j + 1 < p.rows) {
+      if (row0 + j + 1 < n_rows) {
         const bool w = qh + 1 == p.H;
         ql += w ? wrap : p.ql_s2;
         qh = w ? 0 : qh + 1;
       }
     }
     const int t = 8 * wave + (lane >> 3);
-    const int row = min(row_wg0 + t, p.rows - 1);
+    const int row = min(row_wg0 + t, n_rows - 1);
     const int i = div_by(row, p.by_H), h = row - i * p.H;
     const int c = (lane & 7) ^ rope_key32<false>(t);
-    const uint16_t* src = p.q_pe + (qj * p.qp_s0 + i * p.qp_s1 + h * p.qp_s2) + 8 * c;
+    const uint16_t* src = p.q_pe + (q_pe0 + i * p.qp_s1 + h * p.qp_s2) + 8 * c;
     Issue32<false, false>::go64((const uint8_t*)src, lds0 + L::kQ + 65536 + wave * 1024);
   };
   // (the per-row compaction's counters may reach into the query rows' place)
@@ -2283,10 +2354,26 @@ void tile64_kernel(const PartialParams p) {
   Window win{};
   int hi_row = -1, lo_row = 0;  // of the lane's score row
   if constexpr (WIN) {
-    n_valid = compact_window<L, 5>(p, r, s_idx, n_of, i0, n_i, L::kCap, win, smem, tid);
+    const int32_t* table = p.table + r * p.table_s0;
+    if constexpr (GRP) {
+      win = prefix_window(p, item);
+      table = item.prefix ? p.grp_table + item.job * p.grp_table_s0 : p.table + item.job * p.table_s0;
+    } else {
+      win = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
+    }
+    n_valid = compact_window<L, 5>(p, table, s_idx, n_of, i0, n_i, L::kCap, win, smem, tid);
     const int i_row = div_by(row_wg0 + 16 * rq + n16, p.by_H);
     hi_row = win.hi_of(i_row);
     lo_row = win.lo_of(i_row);
+    if constexpr (GRP) {
+      // a prefix's rows that their requests do not have see nothing
+      if (item.prefix && p.win_qlens) {
+        const int iv = item.i0 + i_row, b = min(div_by(iv, p.by_Mq), p.q_jobs - 1);
+        const bool none = iv - b * p.Mq >= p.win_qlens[b];
+        if (none) hi_row = -1;
+        if (__ballot(none) != 0) win.hi_all = -1;
+      }
+    }
   } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                  p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
@@ -2829,9 +2916,12 @@ void tile64_kernel(const PartialParams p) {
   // ---- epilogue.  The waves exchange the rows' sums (two token halves),
   // largest scores and, for fp16 split rows, largest magnitudes (eight column
   // groups) through the weights' place, then each writes its 64 columns.
-  const bool direct = p.n_splits == 1;
+  const bool direct = !GRP && p.n_splits == 1;
   const bool half = !direct && p.ws_f16;
   const int64_t part = (WIN ? part0 : (int64_t)r * p.n_splits) + s_idx;
+  // the tile's rows in the workspace, less `row`
+  const int64_t ws_row0 = GRP ? (item.prefix ? s_idx : p.grp_splits + s_idx) * (int64_t)p.all_rows + (int64_t)item.i0 * p.H
+                              : part * p.rows;
   if constexpr (WIN) {
     if (p.ws_share && rt == 0 && s_idx == 0 && tid == 0) {
       p.ws_share[2 * r] = part0;
@@ -2888,7 +2978,7 @@ void tile64_kernel(const PartialParams p) {
       const float l_tot = ls[k][0] + ls[k][1];
       // (a sum that is NaN, of a row that attends one, is no empty row's)
       const bool some = l_tot != 0.f;
-      none[k] = !some && row < p.rows;
+      none[k] = !some && row < n_rows;
       mult[k] = some ? recip(lw[k][0] + lw[k][1]) : 0.f;
       float row_scale = 1.f;
       if (half) {
@@ -2897,7 +2987,7 @@ void tile64_kernel(const PartialParams p) {
         row_scale = amax > 0.f ? amax : 1.f;
         mult[k] *= 1.f / row_scale;
       }
-      if (wave == k && g2 == 0 && row < p.rows) {
+      if (wave == k && g2 == 0 && row < n_rows) {
         const float lse = some ? (m_all[k] + __log2f(l_tot)) * kLn2 : -INFINITY;
         const f32x2_t mt2 = *(LDS const f32x2_t*)(xtrue + 2 * rl);
         const float mt = fmaxf(mt2[0], mt2[1]);
@@ -2914,9 +3004,9 @@ void tile64_kernel(const PartialParams p) {
             p.lse[lo] = lse;
           }
         } else {
-          p.ws_lse[part * p.rows + row] = lse;
-          if (half) p.ws_scale[part * p.rows + row] = row_scale;
-          if (p.out_wire) p.ws_max[part * p.rows + row] = mt;
+          p.ws_lse[ws_row0 + row] = lse;
+          if (half) p.ws_scale[ws_row0 + row] = row_scale;
+          if (p.out_wire) p.ws_max[ws_row0 + row] = mt;
         }
       }
     }
@@ -2955,12 +3045,12 @@ void tile64_kernel(const PartialParams p) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int row = row_wg0 + 32 * k + 16 * j + (lane & 15);
-      ok[j] = row < p.rows;
+      ok[j] = row < n_rows;
       if (direct) {
         const int i = div_by(row, p.by_H), hd = row - i * p.H;
         off[j] = r * p.out_s0 + i * p.out_s1 + hd * p.out_s2;
       } else {
-        off[j] = (part * p.rows + row) * kDLat;
+        off[j] = (ws_row0 + row) * kDLat;
       }
     }
     if (half || (direct && p.out_wire)) {
@@ -3034,9 +3124,9 @@ void tile64_kernel(const PartialParams p) {
 #pragma unroll
     for (int k = 0; k < 4 * NK; ++k) {
       const int t = 4 * NK * wave + k, row = row_wg0 + t;
-      if (row >= p.rows) break;
+      if (row >= n_rows) break;
       const int i = div_by(row, p.by_H), hd = row - i * p.H;
-      const int64_t off = direct ? r * p.out_s0 + i * p.out_s1 + hd * p.out_s2 : (part * p.rows + row) * kDLat;
+      const int64_t off = direct ? r * p.out_s0 + i * p.out_s1 + hd * p.out_s2 : (ws_row0 + row) * kDLat;
       if (b16) {
         *(u32x4_t*)(dst + 2 * off + 16 * lane) = *(const LDS u32x4_t*)(smem + t * 1024 + ((lane ^ (t & 15)) << 4));
       } else {
@@ -3093,6 +3183,16 @@ static void launch_kv(const PartialParams& p, int grid, int row_groups, hipStrea
     launch_items(tile64_kernel<KV, SEL, 1>, p, grid, 512, s);
   else
     launch_items(tile64_kernel<KV, SEL, 2>, p, grid, 512, s);
+}
+
+// Prefixes of groups and own tokens: 64-row tiles, one launch.
+hipError_t launch_prefix(const PartialParams& p, int kv, hipStream_t s) {
+  const dim3 grid((uint32_t)(p.grp_grid + p.own_items)), wg(512);
+  if (kv == kKvMx4) hipLaunchKernelGGL((tile64_kernel<kKvMx4, kSelPrefix, 2>), grid, wg, 0, s, p);
+  else if (kv == kKvFp8Shared) hipLaunchKernelGGL((tile64_kernel<kKvFp8Shared, kSelPrefix, 2>), grid, wg, 0, s, p);
+  else if (kv == kKvFp8Split) hipLaunchKernelGGL((tile64_kernel<kKvFp8Split, kSelPrefix, 2>), grid, wg, 0, s, p);
+  else hipLaunchKernelGGL((tile64_kernel<kKvBf16, kSelPrefix, 2>), grid, wg, 0, s, p);
+  return hipGetLastError();
 }
 
 hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups, int sel_kind,

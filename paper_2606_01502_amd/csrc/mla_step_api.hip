@@ -80,6 +80,62 @@ mla_status_t check_rope_opts(const mla_rope_opts_t* o, int64_t D) {
   return MLA_OK;
 }
 
+// The checks and parameters that mla_cache_append and mla_rope_append share.
+mla_status_t append_params(const mla_tensor_t* ckv, const mla_tensor_t* kpe, const mla_tensor_t* slots,
+                           const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool, mla::AppendParams& p) {
+  mla_status_t st;
+  if ((st = check_tensor(ckv, "ckv", MLA_DTYPE_BF16, 2)) != MLA_OK) return st;
+  if ((st = check_tensor(kpe, "kpe", MLA_DTYPE_BF16, 2)) != MLA_OK) return st;
+  if ((st = check_tensor(slots, "slots", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+  if (ckv_pool && ckv_pool->dtype == MLA_DTYPE_FP8_E4M3FN)
+    return fail(MLA_ERR_UNSUPPORTED, "ckv_pool: an fp8 pool has one scale a block, which new tokens may exceed");
+  const bool mx4 = ckv_pool && ckv_pool->dtype == MLA_DTYPE_MXFP4;
+  if ((st = check_tensor(ckv_pool, "ckv_pool", mx4 ? MLA_DTYPE_MXFP4 : MLA_DTYPE_BF16, 3)) != MLA_OK) return st;
+  if ((st = check_tensor(kpe_pool, "kpe_pool", MLA_DTYPE_BF16, 3)) != MLA_OK) return st;
+  const int64_t T = ckv->shape[0], P = ckv_pool->shape[0];
+  if (ckv->shape[1] != MLA_DLAT || kpe->shape[0] != T || kpe->shape[1] != MLA_DPE)
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv / kpe: shapes must be [T, 512] / [T, 64]");
+  if (!contiguous(*slots, {T})) return fail(MLA_ERR_INVALID_ARGUMENT, "slots: must be contiguous [T]");
+  if (!contiguous(*ckv_pool, {P, MLA_BLOCK, mx4 ? MLA_MX4_ROW : MLA_DLAT}) ||
+      !contiguous(*kpe_pool, {P, MLA_BLOCK, MLA_DPE}))
+    return fail(MLA_ERR_INVALID_ARGUMENT,
+                "pools must be contiguous [P, 64, 512] (MXFP4: [P, 64, 272]) and [P, 64, 64]");
+  if (!rows_aligned(*ckv, 2) || !rows_aligned(*kpe, 2))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "ckv / kpe rows must be 16-byte aligned");
+  if (!aligned16(ckv_pool->data) || !aligned16(kpe_pool->data))
+    return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
+  const mla_tensor_t* const outs[] = {ckv_pool, kpe_pool};
+  const mla_tensor_t* const ins[] = {ckv, kpe, slots};
+  if ((st = check_apart(outs, ins)) != MLA_OK) return st;
+  if (T > INT32_MAX || P > (INT32_MAX >> 6)) return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the index range");
+  p.src_ckv = (const uint16_t*)ckv->data;
+  p.src_kpe = (const uint16_t*)kpe->data;
+  p.ckv_s0 = ckv->stride[0];
+  p.kpe_s0 = kpe->stride[0];
+  p.slots = (const int32_t*)slots->data;
+  p.ckv = (uint8_t*)ckv_pool->data;
+  p.kpe = (uint8_t*)kpe_pool->data;
+  p.T = T;
+  p.n_slots = P * MLA_BLOCK;
+  p.mx4 = mx4;
+  // one token a wave until that fills the chip, then four, whose loads overlap: 2048
+  // tokens into a 4-bit cache 3.2 us with one, 3.4 with four, 8192 4.6 and 4.1, 30,001
+  // 11.4 and 9.3 (bf16 3.3 and 3.3, 5.1 and 4.0, 13.2 and 11.1)
+  p.wave_toks = T <= 4096 ? 1 : 4;
+  return MLA_OK;
+}
+
+// What a position of 2^31 leaves of a turn: a double holds 2^31 turns to 2^-22 of one,
+// more of them to less, 2^51 (a pair of 2^20 turns) to half a turn.
+mla_status_t check_turns(const double* turns, int pairs) {
+  for (int i = 0; i < pairs; ++i)
+    if (!(turns[i] <= 1.0))
+      return fail(MLA_ERR_INVALID_ARGUMENT,
+                  "opts: a pair turns more than once a position, where far positions lose their angle (at 2^20 turns "
+                  "a position of 2^31 all of it)");
+  return MLA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -197,13 +253,7 @@ mla_status_t mla_rope(const mla_tensor_t* x, const mla_tensor_t* positions, cons
     p.mscale = (float)opts->mscale;
     p.sin_scale = opts->inverse ? -p.mscale : p.mscale;
     rope_turns(*opts, p.turns);
-    // What a position of 2^31 leaves of a turn: a double holds 2^31 turns to 2^-22 of one,
-    // more of them to less, 2^51 (a pair of 2^20 turns) to half a turn.
-    for (int i = 0; i < half; ++i)
-      if (!(p.turns[i] <= 1.0))
-        return fail(MLA_ERR_INVALID_ARGUMENT,
-                    "opts: a pair turns more than once a position, where far positions lose their angle (at 2^20 turns "
-                    "a position of 2^31 all of it)");
+    if ((st = check_turns(p.turns, half)) != MLA_OK) return st;
     return launched(mla::launch_rope(p, reinterpret_cast<hipStream_t>(stream)), "rope");
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");
@@ -215,47 +265,38 @@ mla_status_t mla_cache_append(const mla_tensor_t* ckv, const mla_tensor_t* kpe,
                               const mla_tensor_t* kpe_pool, void* stream) {
   try {
     g_last_error.clear();
-    mla_status_t st;
-    if ((st = check_tensor(ckv, "ckv", MLA_DTYPE_BF16, 2)) != MLA_OK) return st;
-    if ((st = check_tensor(kpe, "kpe", MLA_DTYPE_BF16, 2)) != MLA_OK) return st;
-    if ((st = check_tensor(slots, "slots", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
-    if (ckv_pool && ckv_pool->dtype == MLA_DTYPE_FP8_E4M3FN)
-      return fail(MLA_ERR_UNSUPPORTED, "ckv_pool: an fp8 pool has one scale a block, which new tokens may exceed");
-    const bool mx4 = ckv_pool && ckv_pool->dtype == MLA_DTYPE_MXFP4;
-    if ((st = check_tensor(ckv_pool, "ckv_pool", mx4 ? MLA_DTYPE_MXFP4 : MLA_DTYPE_BF16, 3)) != MLA_OK) return st;
-    if ((st = check_tensor(kpe_pool, "kpe_pool", MLA_DTYPE_BF16, 3)) != MLA_OK) return st;
-    const int64_t T = ckv->shape[0], P = ckv_pool->shape[0];
-    if (ckv->shape[1] != MLA_DLAT || kpe->shape[0] != T || kpe->shape[1] != MLA_DPE)
-      return fail(MLA_ERR_INVALID_ARGUMENT, "ckv / kpe: shapes must be [T, 512] / [T, 64]");
-    if (!contiguous(*slots, {T})) return fail(MLA_ERR_INVALID_ARGUMENT, "slots: must be contiguous [T]");
-    if (!contiguous(*ckv_pool, {P, MLA_BLOCK, mx4 ? MLA_MX4_ROW : MLA_DLAT}) ||
-        !contiguous(*kpe_pool, {P, MLA_BLOCK, MLA_DPE}))
-      return fail(MLA_ERR_INVALID_ARGUMENT,
-                  "pools must be contiguous [P, 64, 512] (MXFP4: [P, 64, 272]) and [P, 64, 64]");
-    if (!rows_aligned(*ckv, 2) || !rows_aligned(*kpe, 2))
-      return fail(MLA_ERR_INVALID_ARGUMENT, "ckv / kpe rows must be 16-byte aligned");
-    if (!aligned16(ckv_pool->data) || !aligned16(kpe_pool->data))
-      return fail(MLA_ERR_INVALID_ARGUMENT, "pools must be 16-byte aligned");
-    const mla_tensor_t* const outs[] = {ckv_pool, kpe_pool};
-    const mla_tensor_t* const ins[] = {ckv, kpe, slots};
-    if ((st = check_apart(outs, ins)) != MLA_OK) return st;
-    if (T > INT32_MAX || P > (INT32_MAX >> 6)) return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the index range");
     mla::AppendParams p{};
-    p.src_ckv = (const uint16_t*)ckv->data;
-    p.src_kpe = (const uint16_t*)kpe->data;
-    p.ckv_s0 = ckv->stride[0];
-    p.kpe_s0 = kpe->stride[0];
-    p.slots = (const int32_t*)slots->data;
-    p.ckv = (uint8_t*)ckv_pool->data;
-    p.kpe = (uint8_t*)kpe_pool->data;
-    p.T = T;
-    p.n_slots = P * MLA_BLOCK;
-    p.mx4 = mx4;
-    // one token a wave until that fills the chip, then four, whose loads overlap: 2048
-    // tokens into a 4-bit cache 3.2 us with one, 3.4 with four, 8192 4.6 and 4.1, 30,001
-    // 11.4 and 9.3 (bf16 3.3 and 3.3, 5.1 and 4.0, 13.2 and 11.1)
-    p.wave_toks = T <= 4096 ? 1 : 4;
+    const mla_status_t st = append_params(ckv, kpe, slots, ckv_pool, kpe_pool, p);
+    if (st != MLA_OK) return st;
     return launched(mla::launch_append(p, reinterpret_cast<hipStream_t>(stream)), "append");
+  } catch (...) {
+    return fail(MLA_ERR_HIP, "internal error");
+  }
+}
+
+mla_status_t mla_rope_append(const mla_tensor_t* ckv, const mla_tensor_t* kpe, const mla_tensor_t* positions,
+                             const mla_tensor_t* slots, const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
+                             const mla_rope_opts_t* opts, void* stream) {
+  try {
+    g_last_error.clear();
+    mla::RopeAppendParams p{};
+    mla_status_t st = append_params(ckv, kpe, slots, ckv_pool, kpe_pool, p.a);
+    if (st != MLA_OK) return st;
+    if ((st = check_tensor(positions, "positions", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
+    if (!contiguous(*positions, {p.a.T})) return fail(MLA_ERR_INVALID_ARGUMENT, "positions: must be contiguous [T]");
+    if ((st = check_rope_opts(opts, MLA_DPE)) != MLA_OK) return st;
+    const mla_tensor_t* const outs[] = {ckv_pool, kpe_pool};
+    const mla_tensor_t* const ins[] = {positions};
+    if ((st = check_apart(outs, ins)) != MLA_OK) return st;
+    p.pos = (const int32_t*)positions->data;
+    p.at = opts->rot_offset;
+    p.rot = opts->rot_dim;
+    p.pairing = opts->pairing;
+    p.mscale = (float)opts->mscale;
+    p.sin_scale = opts->inverse ? -p.mscale : p.mscale;
+    rope_turns(*opts, p.turns);
+    if ((st = check_turns(p.turns, p.rot / 2)) != MLA_OK) return st;
+    return launched(mla::launch_rope_append(p, reinterpret_cast<hipStream_t>(stream)), "append");
   } catch (...) {
     return fail(MLA_ERR_HIP, "internal error");
   }

@@ -32,7 +32,8 @@ EXPORTS = ("mla_sparse_partial_attn", "mla_sparse_partial_attn_ex",
            "mla_sparse_partial_attn_tokens", "mla_merge_partials", "mla_merge_partials_ex",
            "mla_last_error", "mla_version", "mla_primitive_costs", "mla_fetch_gather",
            "mla_fetch_splice", "mla_sparse_partial_attn_noalloc", "mla_batch_slots", "mla_rope",
-           "mla_cache_append", "mla_window_attn")
+           "mla_cache_append", "mla_window_attn", "mla_rope_append", "mla_block_means",
+           "mla_block_scores", "mla_select_topk", "mla_prefix_attn")
 
 
 class MlaError(RuntimeError):
@@ -83,10 +84,25 @@ class PartialOpts(ctypes.Structure):
 OUT_FP32, OUT_BF16_WIRE = 0, 1
 
 
+class _WindowTail(ctypes.Union):
+    # (whole_blocks has the first of what were three reserved fields)
+    _fields_ = [("whole_blocks", ctypes.c_int32), ("reserved", ctypes.c_int32 * 3)]
+
+
 class WindowOpts(ctypes.Structure):
+    _anonymous_ = ("tail",)
     _fields_ = [("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_splits", ctypes.c_int32),
-                ("out_format", ctypes.c_int32), ("row_tile", ctypes.c_int32),
-                ("reserved", ctypes.c_int32 * 3)]
+                ("out_format", ctypes.c_int32), ("row_tile", ctypes.c_int32), ("tail", _WindowTail)]
+
+
+class ScoresOpts(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_splits", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 5)]
+
+
+class PrefixOpts(ctypes.Structure):
+    _fields_ = [("n_splits", ctypes.c_int32), ("own_splits", ctypes.c_int32),
+                ("out_format", ctypes.c_int32), ("reserved", ctypes.c_int32 * 5)]
 
 
 class RopeOpts(ctypes.Structure):
@@ -141,6 +157,16 @@ def load(path: str = LIB_PATH):
     lib.mla_rope.argtypes = [P, P, P, ctypes.POINTER(RopeOpts), vp]
     lib.mla_cache_append.restype = ctypes.c_int
     lib.mla_cache_append.argtypes = [P] * 5 + [vp]
+    lib.mla_rope_append.restype = ctypes.c_int
+    lib.mla_rope_append.argtypes = [P] * 6 + [ctypes.POINTER(RopeOpts), vp]
+    lib.mla_block_means.restype = ctypes.c_int
+    lib.mla_block_means.argtypes = [P] * 4 + [vp]
+    lib.mla_block_scores.restype = ctypes.c_int
+    lib.mla_block_scores.argtypes = [P] * 6 + [ctypes.c_float, P, ctypes.POINTER(ScoresOpts), vp]
+    lib.mla_select_topk.restype = ctypes.c_int
+    lib.mla_select_topk.argtypes = [P] * 2 + [vp]
+    lib.mla_prefix_attn.restype = ctypes.c_int
+    lib.mla_prefix_attn.argtypes = [P] * 10 + [ctypes.c_float, P, P, ctypes.POINTER(PrefixOpts), vp]
     lib.mla_primitive_costs.restype = ctypes.c_int
     lib.mla_primitive_costs.argtypes = [ctypes.POINTER(CostModel), ctypes.POINTER(CostCase),
                                         ctypes.POINTER(Cost)]
@@ -342,13 +368,14 @@ def sparse_partial_attn(q_lat, q_pe, ckv_pool, kpe_pool, chunk_block_table, sel_
 
 def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
                    q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None,
-                   n_splits=0, stream=None, wire=False, row_tile=0):
+                   n_splits=0, stream=None, wire=False, row_tile=0, whole_blocks=False):
     """window_attn with every argument fixed (see prepare_partial)."""
     out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
     dev = _on_current_gpu(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, q_lens, *out, ckv_scale,
                           kpe_scale, stream=stream)
     o = WindowOpts(int(window), int(n_sink), int(n_splits), OUT_BF16_WIRE if wire else OUT_FP32,
                    int(row_tile))
+    o.whole_blocks = int(bool(whole_blocks))
     d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale),
          describe(kpe_pool, kpe_scale), describe(block_table), describe(seq_lens), describe(q_lens))
     do = tuple(describe(t) for t in out)
@@ -361,16 +388,105 @@ def prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale
 
 def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window=0, n_sink=0,
                 q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None, n_splits=0,
-                stream=None, wire=False, row_tile=0):
+                stream=None, wire=False, row_tile=0, whole_blocks=False):
     """Attention of each request's last q_lens[b] tokens (default: all Mq query
     rows) over its paged sequence of seq_lens[b] tokens, each row seeing the
-    last `window` tokens up to its own (0: all) and the first n_sink.  Pools
+    last `window` tokens up to its own (0: all; whole_blocks: from the beginning
+    of the block that the first of them lies in) and the first n_sink.  Pools
     are bf16, fp8 (uint8 with scales) or 4-bit (uint8 rows of MX4_ROW bytes,
     the RoPE pool bf16).  Returns partials as sparse_partial_attn does, in
     either form, for merge_partials or as they are."""
     return prepare_window(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, window,
                           n_sink, q_lens, out_lat, out_lse, ckv_scale, kpe_scale, n_splits, stream,
-                          wire, row_tile)()
+                          wire, row_tile, whole_blocks)()
+
+
+def prepare_prefix(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table,
+                   seq_lens, scale, q_lens=None, out_lat=None, out_lse=None, ckv_scale=None,
+                   kpe_scale=None, n_splits=0, own_splits=0, stream=None, wire=False):
+    """prefix_attn with every argument fixed (see prepare_partial)."""
+    out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
+    keep = (q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table, seq_lens,
+            q_lens, ckv_scale, kpe_scale)
+    dev = _on_current_gpu(*keep, *out, stream=stream)
+    o = PrefixOpts(int(n_splits), int(own_splits), OUT_BF16_WIRE if wire else OUT_FP32)
+    d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale), describe(kpe_pool, kpe_scale),
+         *[describe(t) for t in keep[4:10]])
+    do = tuple(describe(t) for t in out)
+    args = (*[_ref(x) for x in d], ctypes.c_float(scale), *[_ref(x) for x in do], ctypes.byref(o),
+            _stream(stream))
+    return _Prepared(load().mla_prefix_attn, args, (d, do, o, keep), out, dev)
+
+
+def prefix_attn(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table,
+                seq_lens, scale, q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None,
+                n_splits=0, own_splits=0, stream=None, wire=False):
+    """Attention of each request's rows over the prefix that its group shares
+    (prefix_table [G, NBP], prefix_lens [G]; group g is the requests
+    group_starts[g] .. group_starts[g + 1] - 1), read once for all of them, and
+    over its own tokens behind it (block_table, seq_lens, q_lens as in
+    window_attn, causal).  Pools and results as there."""
+    return prepare_prefix(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts,
+                          block_table, seq_lens, scale, q_lens, out_lat, out_lse, ckv_scale, kpe_scale,
+                          n_splits, own_splits, stream, wire)()
+
+
+def prepare_block_means(ckv_pool, kpe_pool, slots, means, ckv_scale=None, kpe_scale=None, stream=None):
+    """block_means with every argument fixed (see prepare_partial)."""
+    keep = (ckv_pool, kpe_pool, slots, means, ckv_scale, kpe_scale)
+    dev = _on_current_gpu(*keep, stream=stream)
+    d = [_describe_latent(ckv_pool, ckv_scale), describe(kpe_pool, kpe_scale), describe(slots), describe(means)]
+    return _Prepared(load().mla_block_means, (*[_ref(x) for x in d], _stream(stream)), (d, keep), means, dev)
+
+
+def block_means(ckv_pool, kpe_pool, slots, means, ckv_scale=None, kpe_scale=None, stream=None):
+    """Mean keys of the blocks that new tokens at slots [T] (block * 64 + row)
+    have made whole, those with a slot in row 63: rows of means [P, 576] bf16,
+    written in place and returned.  Pools of any kind that attention takes."""
+    return prepare_block_means(ckv_pool, kpe_pool, slots, means, ckv_scale, kpe_scale, stream)()
+
+
+def prepare_block_scores(q_lat, q_pe, means, block_table, seq_lens, scale, window=0, n_sink=0, q_lens=None,
+                         scores=None, n_splits=0, stream=None):
+    """block_scores with every argument fixed (see prepare_partial)."""
+    if scores is None:
+        scores = torch.empty((*q_lat.shape[:2], block_table.shape[1]), dtype=torch.float32, device=q_lat.device)
+    keep = (q_lat, q_pe, means, block_table, seq_lens, q_lens)
+    dev = _on_current_gpu(*keep, scores, stream=stream)
+    o = ScoresOpts(int(window), int(n_sink), int(n_splits))
+    d = [describe(t) for t in (*keep, scores)]
+    args = (*[_ref(x) for x in d[:6]], ctypes.c_float(scale), _ref(d[6]), ctypes.byref(o), _stream(stream))
+    return _Prepared(load().mla_block_scores, args, (d, o, keep), scores, dev)
+
+
+def block_scores(q_lat, q_pe, means, block_table, seq_lens, scale, window=0, n_sink=0, q_lens=None,
+                 scores=None, n_splits=0, stream=None):
+    """Scores [B, Mq, NB] of the blocks of each request's sequence for each
+    query row: the share of its attention that each head would give a block if
+    its keys were their mean (means [P, 576] of block_means), summed over the
+    heads; -inf for blocks that are not whole, that the last `window` tokens
+    reach into (window_attn with whole_blocks attends those) or the first
+    n_sink.  For select_topk."""
+    return prepare_block_scores(q_lat, q_pe, means, block_table, seq_lens, scale, window, n_sink, q_lens,
+                                scores, n_splits, stream)()
+
+
+def prepare_select_topk(scores, k=None, ids=None, stream=None):
+    """select_topk with every argument fixed (see prepare_partial)."""
+    if ids is None:
+        if k is None:
+            raise ValueError("give k (picks of a row) or ids")
+        ids = torch.empty((*scores.shape[:-1], k), dtype=torch.int32, device=scores.device)
+    dev = _on_current_gpu(scores, ids, stream=stream)
+    d = (describe(scores), describe(ids))
+    return _Prepared(load().mla_select_topk, (*[_ref(x) for x in d], _stream(stream)), (d, scores), ids, dev)
+
+
+def select_topk(scores, k=None, ids=None, stream=None):
+    """The places of the k largest of each row's scores ([B, Mq, N] or [R, N]
+    fp32) in rising order, as a selection for sparse_partial_attn: of equal
+    ones the first, never -inf (-1 behind the last of a row with fewer)."""
+    return prepare_select_topk(scores, k, ids, stream)()
 
 
 def fetch_gather(ckv_pool, kpe_pool, chunk_block_table, sel_token_ids, out_ckv=None,
@@ -507,6 +623,29 @@ def cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream=None):
     [P, 64, 512] as they are, a 4-bit one [P, 64, 272] (uint8) as E2M1 codes
     under a power of two per 32 columns.  Returns the pools."""
     return prepare_cache_append(ckv, kpe, slots, ckv_pool, kpe_pool, stream)()
+
+
+def prepare_rope_append(ckv, kpe, positions, slots, ckv_pool, kpe_pool, rot_offset=0, rot_dim=None,
+                        pairing=0, base=10000.0, scaling="none", factor=1.0, orig_len=0, beta_fast=32.0,
+                        beta_slow=1.0, mscale=1.0, stream=None):
+    """rope_append with every argument fixed (see prepare_partial)."""
+    keep = (ckv, kpe, positions, slots)
+    dev = _on_current_gpu(*keep, ckv_pool, kpe_pool, stream=stream)
+    o = RopeOpts(int(rot_offset), int(DPE - rot_offset if rot_dim is None else rot_dim), int(pairing),
+                 ROPE_SCALINGS.index(scaling), 0, 0, float(base), float(factor), float(beta_fast),
+                 float(beta_slow), float(mscale), int(orig_len))
+    d = [*[describe(t) for t in keep], _describe_latent(ckv_pool), describe(kpe_pool)]
+    return _Prepared(load().mla_rope_append, (*[_ref(t) for t in d], ctypes.byref(o), _stream(stream)),
+                     (d, o, keep), (ckv_pool, kpe_pool), dev)
+
+
+def rope_append(ckv, kpe, positions, slots, ckv_pool, kpe_pool, rot_offset=0, rot_dim=None, pairing=0,
+                base=10000.0, scaling="none", factor=1.0, orig_len=0, beta_fast=32.0, beta_slow=1.0,
+                mscale=1.0, stream=None):
+    """rope of the RoPE parts kpe [T, 64] at positions [T] and cache_append of
+    the turned tokens, in one call.  Returns the pools."""
+    return prepare_rope_append(ckv, kpe, positions, slots, ckv_pool, kpe_pool, rot_offset, rot_dim, pairing,
+                               base, scaling, factor, orig_len, beta_fast, beta_slow, mscale, stream)()
 
 
 def primitive_costs(mq, chunk_tokens, q_bytes=1152, p_bytes=1032, kv_bytes=1152, **model):
