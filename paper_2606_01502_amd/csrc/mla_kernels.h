@@ -247,12 +247,18 @@ struct MeansParams {
   const int32_t* slots;    // [T]; of those of n_slots that are a block's last row, that block's mean
   uint16_t* means;         // [P][576] bf16
   int64_t T, n_slots;
+  int32_t sharers;         // workgroups to kMeanWindow slots (set by the launch)
+  Div by_sharers;
 };
+constexpr int kMeanWindow = 1024;
 hipError_t launch_means(const MeansParams& p, int kv, hipStream_t s);
 
 // Scores of blocks by their mean keys: one workgroup a request, group of query rows
 // and split of its blocks.
-constexpr int kScoreChunks = 2;  // 16-row chunks a wave holds
+// Rows (16-row chunks of heads) of a workgroup and blocks of a tile.
+enum { kScores128, kScores64, kScores32, kScores16 };
+constexpr int kScoreChunksOf[] = {8, 4, 2, 1};
+constexpr int kScoreColsOf[] = {32, 64, 64, 64};
 struct ScoresParams {
   const uint16_t* q_lat;
   const uint16_t* q_pe;
@@ -269,7 +275,7 @@ struct ScoresParams {
   int32_t window, first_block;
   int32_t row_chunks;      // chunks of a query row
   int32_t group_rows, group_chunks, n_groups;  // query rows and chunks of a group
-  int32_t n_splits, wave_rows;
+  int32_t n_splits, shape;  // shape: kScores*
   float scale_log2;        // softmax scale * log2(e)
   Div by_splits, by_groups, by_chunks;
 };

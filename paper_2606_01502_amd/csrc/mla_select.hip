@@ -25,9 +25,11 @@ __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(
 // bf16, in which the scores' matrix products take it.  fp8: the sum of 64 codes is
 // exact in fp32 (multiples of 2^-9 below 2^15), the block's scale comes after it.
 //
-// A workgroup takes every n-th of the slots and, of those that are a block's last
-// row, that block, all of whose 18 loads a thread are out before the first sum: a
-// stream through HBM, bound by the launch and two trips where few blocks are whole.
+// Several workgroups look at the same 1024 slots and share out the blocks that end
+// there in their order, so that each has its part both of a prompt's tokens, every
+// 64th of which ends a block, and of a list of ends.  A block's 18 loads a thread are
+// all out before the first sum: a stream through HBM, bound by the launch and two
+// trips where few blocks are whole.
 constexpr int kMeanCols = kDLat + kDPe;
 
 // Adds the eight bf16 of v to a.
@@ -122,39 +124,53 @@ __device__ __forceinline__ void block_sums(const MeansParams& p, int64_t b, floa
 template <int KV>
 __global__ __launch_bounds__(kThreads) void means_kernel(const MeansParams p) {
   __shared__ float sums[4][kMeanCols];
-  __shared__ int32_t whole[kThreads];
-  __shared__ int n_whole;
-  const int tid = threadIdx.x;
-  const int64_t step = gridDim.x;
-  for (int64_t k0 = 0; blockIdx.x + k0 * step < p.T; k0 += kThreads) {
-    const int64_t t = blockIdx.x + (k0 + tid) * step;
-    const int32_t s = t < p.T ? p.slots[t] : -1;
-    if (tid == 0) n_whole = 0;
-    __syncthreads();
-    // (their order does not matter)
-    if (s >= 0 && s < p.n_slots && s % kBlock == kBlock - 1) whole[atomicAdd(&n_whole, 1)] = s / kBlock;
-    __syncthreads();
-    const int n = n_whole;
-    for (int k = 0; k < n; ++k) {
-      const int64_t b = whole[k];
-      block_sums<KV>(p, b, sums);
-      __syncthreads();
-      float lat = 1.f / kBlock, pe = 1.f / kBlock;
-      if constexpr (KV == kKvFp8Shared) {
-        lat *= p.ckv_scale[b];
-        pe *= p.kpe_scale[b];
-      }
-      uint32_t* const out = (uint32_t*)(p.means + b * kMeanCols);
-      for (int c = tid; c < kMeanCols / 2; c += kThreads) {
-        float v[2];
+  __shared__ int32_t whole[kMeanWindow];
+  __shared__ int counts[kMeanWindow / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int window = div_by((int)blockIdx.x, p.by_sharers), own = (int)blockIdx.x - window * p.sharers;
+  const int64_t t0 = (int64_t)window * kMeanWindow;
+  constexpr int kPer = kMeanWindow / kThreads;
+  int32_t block[kPer];
+  uint64_t ends[kPer];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          v[i] = ((sums[0][2 * c + i] + sums[1][2 * c + i]) + (sums[2][2 * c + i] + sums[3][2 * c + i])) *
-                 (c < kDLat / 2 ? lat : pe);
-        out[c] = (uint32_t)bf16_bits(v[0]) | (uint32_t)bf16_bits(v[1]) << 16;
-      }
-      __syncthreads();
+  for (int k = 0; k < kPer; ++k) {
+    const int64_t t = t0 + k * kThreads + tid;
+    const int32_t s = t < p.T ? p.slots[t] : -1;
+    const bool end = s >= 0 && s < p.n_slots && s % kBlock == kBlock - 1;
+    block[k] = end ? s / kBlock : -1;
+    ends[k] = __ballot(end);
+    if (lane == 0) counts[4 * k + wave] = (int)__popcll(ends[k]);
+  }
+  __syncthreads();
+  int n = 0, at[kPer] = {};  // of the window, and before the wave's
+#pragma unroll
+  for (int k = 0; k < kMeanWindow / 64; ++k) {
+    if ((k & 3) == wave) at[k >> 2] = n;
+    n += counts[k];
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+    if (block[k] >= 0) whole[at[k] + (int)__popcll(ends[k] & ((1ull << lane) - 1))] = block[k];
+  __syncthreads();
+  for (int k = own; k < n; k += p.sharers) {
+    const int64_t b = __builtin_amdgcn_readfirstlane(whole[k]);
+    block_sums<KV>(p, b, sums);
+    __syncthreads();
+    float lat = 1.f / kBlock, pe = 1.f / kBlock;
+    if constexpr (KV == kKvFp8Shared) {
+      lat *= p.ckv_scale[b];
+      pe *= p.kpe_scale[b];
     }
+    uint32_t* const out = (uint32_t*)(p.means + b * kMeanCols);
+    for (int c = tid; c < kMeanCols / 2; c += kThreads) {
+      float v[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        v[i] = ((sums[0][2 * c + i] + sums[1][2 * c + i]) + (sums[2][2 * c + i] + sums[3][2 * c + i])) *
+               (c < kDLat / 2 ? lat : pe);
+      out[c] = (uint32_t)bf16_bits(v[0]) | (uint32_t)bf16_bits(v[1]) << 16;
+    }
+    __syncthreads();
   }
 }
 
@@ -173,36 +189,58 @@ __global__ __launch_bounds__(kThreads) void means_kernel(const MeansParams p) {
 // is one split).  Logits kept between the passes would move 8 bytes a head and
 // block, the keys again 1152 a block for all heads, mostly out of the caches.
 //
-// A workgroup takes 64 blocks at a time into LDS; its waves share out 16-row chunks
-// (the heads of one query row, padded) and the blocks' four columns of 16.  bf16
-// MFMA 16x16x32 with the query rows in registers for the whole kernel.
-constexpr int kTileCols = 64;                  // blocks of a tile
+// A workgroup takes a tile of blocks at a time in LDS, the next tile's keys on their
+// way (direct-to-LDS loads); its waves share out 16-row chunks (the heads of one query row,
+// padded) and the tile's columns of 16 blocks.  bf16 MFMA 16x16x32 with the query
+// rows in registers for the whole kernel.  128 rows a workgroup where there are as
+// many, and two workgroups a compute unit: one's loads and exponentials run beside the
+// other's products.
 constexpr int kKeyBytes = 2 * kMeanCols;       // 1152: 72 chunks of 16 bytes
 constexpr int kSteps = kMeanCols / 32;         // of a product: 18
-constexpr int kChunks = kScoreChunks;          // 16-row chunks a wave holds
 
-// 16-byte chunk c of a key in LDS row n sits in place c ^ key_swizzle(n): the LDS
-// serves 16 lanes of a 16-byte read at once, rows {0..3, 8..11} (or the others) of
-// two neighbouring chunks; rows of 1152 bytes lie 0 or 128 bytes apart modulo the 64
-// banks, by their lowest bit, and the key puts their other two bits beside the
-// chunk's.
+// A tile's keys in LDS: nine pieces of 128 bytes a row, [piece][row][128], 16-byte
+// chunk c of a piece in place c ^ key_swizzle(row).  The LDS serves 16 lanes of a
+// 16-byte read at once, rows {0..3, 8..11} (or the others) of two neighbouring chunks;
+// rows lie 0 or 128 bytes apart modulo the 64 banks, by their lowest bit, and the key
+// puts their other two bits beside the chunk's.
 __device__ __forceinline__ int key_swizzle(int n) { return ((n >> 1) & 1) << 1 | ((n >> 3) & 1) << 2; }
+
+// 16 bytes a lane from src to dst + 16 * lane, dst the same in every lane.  The wait for
+// it is the code's own: written as asm, since the compiler would wait before every LDS
+// read that follows.
+__device__ __forceinline__ void to_lds(const uint8_t* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"(src), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
+}
+constexpr int kWaitLoads = (7 << 4) | (15 << 8);  // s_waitcnt vmcnt(0)
 
 __device__ __forceinline__ float over_rows(float v) {  // of lanes l, l ^ 16, l ^ 32, l ^ 48
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
 
-// WR waves along the rows, 4 / WR along the columns.  PASS 0: both passes; 1: the
-// statistics of a split; 2: the scores, given those of all splits.
-template <int WR, int PASS>
-__global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) {
-  constexpr int WK = 4 / WR, kCols = 4 / WK;  // 16-block columns of a wave
-  constexpr int kSlots = WR * kChunks;        // chunks of the workgroup
-  __shared__ __attribute__((aligned(16))) uint8_t keys[kTileCols * kKeyBytes];
-  __shared__ float part[kSlots][kTileCols];
+// Statistics (largest logit, sum of exponentials against it) of two sets, joined.
+__device__ __forceinline__ f32x2_t join(f32x2_t a, f32x2_t b) {
+  const float m = fmaxf(a[0], b[0]), top = fmaxf(m, -3.4e38f);
+  return f32x2_t{m, a[1] * __builtin_amdgcn_exp2f(a[0] - top) + b[1] * __builtin_amdgcn_exp2f(b[0] - top)};
+}
+// What a logit is taken off by so that the exponentials of all are weights.
+__device__ __forceinline__ float norm_of(f32x2_t a) { return fmaxf(a[0], -3.4e38f) + __builtin_amdgcn_logf(a[1]); }
+
+// WR waves along the rows, 4 / WR along the columns, NC chunks and COLS columns of 16
+// blocks a wave.  PASS 0: both passes; 1: the statistics of a split; 2: the scores,
+// given those of all splits.
+template <int WR, int NC, int COLS, int PASS>
+__global__ __launch_bounds__(kThreads, 2) void scores_kernel(const ScoresParams p) {
+  constexpr int WK = 4 / WR;
+  constexpr int kTile = WK * COLS * 16;        // blocks of a tile
+  constexpr int kSlots = WR * NC;              // chunks of the workgroup
+  constexpr int kRows = kTile / 32;            // keys a lane loads its part of
+  constexpr int kPieces = kKeyBytes / 128, kPiece = kTile * 128, kBuffer = kTile * kKeyBytes;
+  __shared__ __attribute__((aligned(16))) uint8_t keys[2 * kBuffer];
+  __shared__ float part[kSlots][kTile];
   __shared__ f32x2_t stat[WK][kSlots][16];
-  __shared__ uint64_t live_cols;
+  __shared__ int32_t is_block[2][kTile];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n16 = lane & 15, g = lane >> 4;
   const int wr = wave / WK, wk = wave % WK;
@@ -222,23 +260,47 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) 
     return i < qn && past > 0 ? (int)min(past / kBlock, (int64_t)p.NB) : 0;
   };
   const int end = i0 < qn ? end_of(min(i0 + n_i, qn) - 1) : 0;
-  const int tile0 = lo / kTileCols, tiles = end > lo ? (end - 1) / kTileCols - tile0 + 1 : 0;
+  const int tile0 = lo / kTile, tiles = end > lo ? (end - 1) / kTile - tile0 + 1 : 0;
   const int t0 = tile0 + (int)((int64_t)tiles * split / p.n_splits);
   const int t1 = tile0 + (int)((int64_t)tiles * (split + 1) / p.n_splits);
 
   float* const out = p.out + (int64_t)b * p.out_s0;
   if constexpr (PASS != 1) {
-    // columns of no tile
-    if (split == p.n_splits - 1) {
-      const int c0 = tiles > 0 ? tile0 * kTileCols : 0, c1 = tiles > 0 ? (tile0 + tiles) * kTileCols : 0;
-      for (int i = i0; i < i0 + n_i; ++i) {
-        float* const row = out + (int64_t)i * p.out_s1;
-        for (int c = tid; c < p.NB; c += kThreads)
-          if (c < c0 || c >= c1) row[c] = -INFINITY;
-      }
+    // columns of no tile, shared out over the splits
+    const int c0 = tiles > 0 ? tile0 * kTile : 0, c1 = tiles > 0 ? (tile0 + tiles) * kTile : 0;
+    for (int i = i0; i < i0 + n_i; ++i) {
+      float* const row = out + (int64_t)i * p.out_s1;
+      for (int c = split * kThreads + tid; c < p.NB; c += p.n_splits * kThreads)
+        if (c < c0 || c >= c1) row[c] = -INFINITY;
     }
   }
   if (t0 == t1 && PASS != 1) return;
+
+  // the keys on their way: wave w loads rows 8 w .. 8 w + 7 (and 32 on), 8 lanes a row
+  const int32_t* const table = p.table + b * p.table_s0;
+  const int kr = tid >> 3;
+  const uint32_t chunk = (uint32_t)(((tid & 7) ^ key_swizzle(kr & 15)) << 4);
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)keys;
+  int32_t id[kRows];  // of the tile that is loaded next
+  auto ids_of = [&](int t) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int j = t * kTile + kr + 32 * r;
+      id[r] = j >= lo && j < end ? table[j] : -1;
+    }
+  };
+  auto load_keys = [&](int buffer) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const bool is = id[r] >= 0 && id[r] < p.P;
+      const uint8_t* const key = p.means + (int64_t)(is ? id[r] : 0) * kKeyBytes + chunk;
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x)
+        to_lds(key + 128 * x, lds + (uint32_t)(buffer * kBuffer + x * kPiece + (8 * wave + 32 * r) * 128));
+      if ((tid & 7) == 0) is_block[buffer][kr + 32 * r] = is;
+    }
+  };
+  constexpr int kFirst = PASS == 2 ? 2 : 1, kLast = PASS == 1 ? 1 : 2;
 
   // head chunks of the query rows: chunk c of the group is heads 16 (c mod C) .. of
   // row i0 + c / C; more than kSlots of them (one query row of many heads) go in
@@ -247,19 +309,28 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) 
   const int n_chunks = n_i * C;
   const int rounds = (n_chunks + kSlots - 1) / kSlots;
   for (int round = 0; round < rounds; ++round) {
-    bf16x8_t q[kChunks][kSteps];
-    int row_i[kChunks], h0[kChunks];
+    // tiles t0 .. t1 - 1, in each pass; the one after t (in the second pass the first
+    // again)
+    auto after = [&](int t) { return t + 1 < t1 ? t + 1 : t0; };
+    int buffer = 0;
+    if (t0 < t1) {
+      ids_of(t0);
+      load_keys(buffer);
+      ids_of(after(t0));
+    }
+    bf16x8_t q[NC][kSteps];
+    int h0[NC], chunk_end[NC];
 #pragma unroll
-    for (int k = 0; k < kChunks; ++k) {
-      const int c = round * kSlots + wr * kChunks + k;
+    for (int k = 0; k < NC; ++k) {
+      const int c = round * kSlots + wr * NC + k;
       const bool is = c < n_chunks;
-      const int ci = is ? div_by(c, p.by_chunks) : 0;
-      row_i[k] = is ? i0 + ci : -1;
+      const int ci = is ? div_by(c, p.by_chunks) : 0, i = i0 + ci;
       h0[k] = is ? 16 * (c - ci * C) : p.H;
+      chunk_end[k] = is ? end_of(i) : 0;
       const int h = h0[k] + n16;
       if (h < p.H) {
-        const uint16_t* const ql = p.q_lat + b * p.ql_s0 + (int64_t)row_i[k] * p.ql_s1 + h * p.ql_s2 + 8 * g;
-        const uint16_t* const qp = p.q_pe + b * p.qp_s0 + (int64_t)row_i[k] * p.qp_s1 + h * p.qp_s2 + 8 * g;
+        const uint16_t* const ql = p.q_lat + b * p.ql_s0 + (int64_t)i * p.ql_s1 + h * p.ql_s2 + 8 * g;
+        const uint16_t* const qp = p.q_pe + b * p.qp_s0 + (int64_t)i * p.qp_s1 + h * p.qp_s2 + 8 * g;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
           q[k][s] = s < kDLat / 32 ? *(const bf16x8_t*)(ql + 32 * s) : *(const bf16x8_t*)(qp + 32 * (s - kDLat / 32));
@@ -268,155 +339,106 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) 
         for (int s = 0; s < kSteps; ++s) q[k][s] = bf16x8_t{};
       }
     }
-    // of rows 16 chunk + 4 g + r: the largest logit and sum of this lane's columns,
-    // then the row's log2 of the sum of all
-    float m[kChunks][4], l[kChunks][4];
+    // of rows 16 chunk + 4 g + r: the largest logit and sum of this lane's columns
+    // (log2 units), in the second pass what norm_of gives of all
+    f32x2_t st[NC][4];
 #pragma unroll
-    for (int k = 0; k < kChunks; ++k)
+    for (int k = 0; k < NC; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        m[k][r] = -INFINITY;
-        l[k][r] = 0.f;
+      for (int r = 0; r < 4; ++r) st[k][r] = f32x2_t{-INFINITY, 0.f};
+    if constexpr (PASS == 2) {
+#pragma unroll
+      for (int k = 0; k < NC; ++k) {
+        const int c = round * kSlots + wr * NC + k;
+        if (c >= n_chunks) continue;
+        const f32x2_t* const at = (const f32x2_t*)p.stats + (((int64_t)a * p.group_chunks + c) * 16 + 4 * g) * p.n_splits;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          // (lane n16 takes splits n16, n16 + 16, ...)
+          f32x2_t x{-INFINITY, 0.f};
+          for (int s = n16; s < p.n_splits; s += 16) x = join(x, at[r * p.n_splits + s]);
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) x = join(x, f32x2_t{__shfl_xor(x[0], o), __shfl_xor(x[1], o)});
+          st[k][r][0] = norm_of(x);
+        }
       }
+    }
 
-    for (int pass = PASS == 2 ? 2 : 1; pass <= (PASS == 1 ? 1 : 2); ++pass) {
-      if (pass == 2) {
-        // the rows' statistics: those of all splits, or of this workgroup's waves
-        if constexpr (PASS == 0) {
-#pragma unroll
-          for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-              for (int w = 0; w < WK; ++w) mm = fmaxf(mm, stat[w][wr * kChunks + k][4 * g + r][0]);
-              const float top = fmaxf(mm, -3.4e38f);
-#pragma unroll
-              for (int w = 0; w < WK; ++w) {
-                const f32x2_t st = stat[w][wr * kChunks + k][4 * g + r];
-                ll += st[1] * __builtin_amdgcn_exp2f(st[0] - top);
-              }
-              m[k][r] = top + __builtin_amdgcn_logf(ll);
-            }
-        } else {
-#pragma unroll
-          for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              // (lane n16 takes splits n16, n16 + 16, ...)
-              float mm = -INFINITY, ll = 0.f;
-              const int c = round * kSlots + wr * kChunks + k;
-              const f32x2_t* const st = (const f32x2_t*)p.stats +
-                                        (((int64_t)a * p.group_chunks + c) * 16 + 4 * g + r) * p.n_splits;
-              if (c < n_chunks) {
-                for (int s = n16; s < p.n_splits; s += 16) mm = fmaxf(mm, st[s][0]);
-#pragma unroll
-                for (int o = 1; o < 16; o <<= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
-                const float top = fmaxf(mm, -3.4e38f);
-                for (int s = n16; s < p.n_splits; s += 16) ll += st[s][1] * __builtin_amdgcn_exp2f(st[s][0] - top);
-#pragma unroll
-                for (int o = 1; o < 16; o <<= 1) ll += __shfl_xor(ll, o);
-                m[k][r] = top + __builtin_amdgcn_logf(ll);
-              }
-            }
-        }
-      }
+    for (int pass = kFirst; pass <= kLast; ++pass) {
       for (int t = t0; t < t1; ++t) {
-        __syncthreads();  // the last tile's keys and parts are read
-        // keys of blocks 64 t .. +63 and which of them there are
-        if (tid < kTileCols) {
-          const int j = t * kTileCols + tid;
-          int32_t blk = -1;
-          if (j >= lo && j < end) {
-            blk = p.table[b * p.table_s0 + j];
-            if (blk >= p.P) blk = -1;
-          }
-          const uint64_t is = __ballot(blk >= 0);
-          if (tid == 0) live_cols = is;
-          ((int32_t*)part)[tid] = max(blk, 0);
-        }
+        // the tile has landed, and every wave is past the one before it
+        __builtin_amdgcn_s_waitcnt(kWaitLoads);
         __syncthreads();
-        u32x4_t v[kTileCols * kKeyBytes / 16 / kThreads];
-#pragma unroll
-        for (int x = 0; x < kTileCols * kKeyBytes / 16 / kThreads; ++x) {
-          const int e = x * kThreads + tid, n = e / (kKeyBytes / 16), c = e - n * (kKeyBytes / 16);
-          v[x] = *(const u32x4_t*)(p.means + (int64_t)((const int32_t*)part)[n] * kKeyBytes + 16 * c);
+        const uint8_t* const here = keys + buffer * kBuffer;
+        const int32_t* const blocks = is_block[buffer];
+        buffer ^= 1;
+        if (t + 1 < t1 || pass < kLast) {
+          load_keys(buffer);
+          ids_of(after(after(t)));
         }
+        f32x4_t acc[NC][COLS];
 #pragma unroll
-        for (int x = 0; x < kTileCols * kKeyBytes / 16 / kThreads; ++x) {
-          const int e = x * kThreads + tid, n = e / (kKeyBytes / 16), c = e - n * (kKeyBytes / 16);
-          *(u32x4_t*)(keys + n * kKeyBytes + ((c ^ key_swizzle(n & 15)) << 4)) = v[x];
-        }
-        __syncthreads();
-        const uint64_t cols = live_cols;
-        f32x4_t acc[kChunks][kCols];
+        for (int k = 0; k < NC; ++k)
 #pragma unroll
-        for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) acc[k][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          for (int c = 0; c < COLS; ++c) acc[k][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            const int n = 16 * (wk * kCols + c) + n16;
-            const bf16x8_t kf = *(const bf16x8_t*)(keys + n * kKeyBytes + (((4 * s + g) ^ key_swizzle(n16)) << 4));
+          for (int c = 0; c < COLS; ++c) {
+            const int n = 16 * (wk * COLS + c) + n16;
+            const bf16x8_t kf = *(const bf16x8_t*)(here + (s >> 1) * kPiece + n * 128 +
+                                                   (((4 * (s & 1) + g) ^ key_swizzle(n16)) << 4));
 #pragma unroll
-            for (int k = 0; k < kChunks; ++k)
+            for (int k = 0; k < NC; ++k)
               acc[k][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[k][s], kf, acc[k][c], 0, 0, 0);
           }
         }
-        float w[kChunks][kCols];
+        bool block[COLS];
+        int col[COLS];
 #pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-          const int ci_end = row_i[k] >= 0 ? end_of(row_i[k]) : 0;
-          bool may[kCols];
+        for (int c = 0; c < COLS; ++c) {
+          const int n = 16 * (wk * COLS + c) + n16;
+          block[c] = blocks[n] != 0;
+          col[c] = t * kTile + n;
+        }
+        if (pass == 1) {
 #pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            const int n = 16 * (wk * kCols + c) + n16;
-            may[c] = (cols >> n & 1) != 0 && t * kTileCols + n < ci_end;
-          }
-          if (pass == 1) {
+          for (int k = 0; k < NC; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x[kCols], mx = m[k][r];
+              float x[COLS], mx = st[k][r][0];
 #pragma unroll
-              for (int c = 0; c < kCols; ++c) {
-                x[c] = may[c] ? acc[k][c][r] * p.scale_log2 : -INFINITY;
+              for (int c = 0; c < COLS; ++c) {
+                x[c] = block[c] && col[c] < chunk_end[k] ? acc[k][c][r] * p.scale_log2 : -INFINITY;
                 mx = fmaxf(mx, x[c]);
               }
               const float top = fmaxf(mx, -3.4e38f);
-              float sum = l[k][r] * __builtin_amdgcn_exp2f(m[k][r] - top);
+              float sum = st[k][r][1] * __builtin_amdgcn_exp2f(st[k][r][0] - top);
 #pragma unroll
-              for (int c = 0; c < kCols; ++c) sum += __builtin_amdgcn_exp2f(x[c] - top);
-              l[k][r] = sum;
-              m[k][r] = mx;
+              for (int c = 0; c < COLS; ++c) sum += __builtin_amdgcn_exp2f(x[c] - top);
+              st[k][r] = f32x2_t{mx, sum};
             }
-          } else {
+        } else {
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) {
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) {
               float sum = 0.f;
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(acc[k][c][r] * p.scale_log2 - m[k][r]);
+                const float e = __builtin_amdgcn_exp2f(acc[k][c][r] * p.scale_log2 - st[k][r][0]);
                 sum += h0[k] + 4 * g + r < p.H ? e : 0.f;
               }
               sum = over_rows(sum);
-              w[k][c] = may[c] ? sum : -INFINITY;
+              if (g == 0)
+                part[wr * NC + k][16 * (wk * COLS + c) + n16] = block[c] && col[c] < chunk_end[k] ? sum : -INFINITY;
             }
-          }
-        }
-        if (pass == 2) {
-#pragma unroll
-          for (int k = 0; k < kChunks; ++k)
-#pragma unroll
-            for (int c = 0; c < kCols; ++c)
-              if (g == 0) part[wr * kChunks + k][16 * (wk * kCols + c) + n16] = w[k][c];
           __syncthreads();
           // a query row's chunks, in order; more than one round's are added up in
-          // place (the same thread's)
+          // place (by the same thread)
           const int c0 = round * kSlots, c1 = min(n_chunks, c0 + kSlots);
-          for (int e = tid; e < n_i * kTileCols; e += kThreads) {
-            const int ii = e / kTileCols, n = e % kTileCols, j = t * kTileCols + n;
+          for (int e = tid; e < n_i * kTile; e += kThreads) {
+            const int ii = e / kTile, n = e % kTile, j = t * kTile + n;
             const int from = max(ii * C, c0), to = min((ii + 1) * C, c1);
             if (from >= to || j >= p.NB) continue;
             float* const at = out + (int64_t)(i0 + ii) * p.out_s1 + j;
@@ -427,34 +449,36 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) 
         }
       }
       if (pass == 1) {
-        // the lanes' statistics of a row to one
+        // a row's statistics: of the lanes that share it, then of the waves
 #pragma unroll
-        for (int k = 0; k < kChunks; ++k)
+        for (int k = 0; k < NC; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            float mm = m[k][r];
+            f32x2_t x = st[k][r];
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
-            const float top = fmaxf(mm, -3.4e38f);
-            float ll = l[k][r] * __builtin_amdgcn_exp2f(m[k][r] - top);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) ll += __shfl_xor(ll, o);
-            if (n16 == 0) stat[wk][wr * kChunks + k][4 * g + r] = f32x2_t{mm, ll};
+            for (int o = 1; o < 16; o <<= 1) x = join(x, f32x2_t{__shfl_xor(x[0], o), __shfl_xor(x[1], o)});
+            if (n16 == 0) stat[wk][wr * NC + k][4 * g + r] = x;
           }
         __syncthreads();
         if constexpr (PASS == 1) {
           for (int e = tid; e < kSlots * 16; e += kThreads) {
             const int c = round * kSlots + e / 16, r = e % 16;
             if (c >= n_chunks) continue;
-            float mm = -INFINITY, ll = 0.f;
+            f32x2_t x = stat[0][e / 16][r];
 #pragma unroll
-            for (int w = 0; w < WK; ++w) mm = fmaxf(mm, stat[w][e / 16][r][0]);
-            const float top = fmaxf(mm, -3.4e38f);
-#pragma unroll
-            for (int w = 0; w < WK; ++w) ll += stat[w][e / 16][r][1] * __builtin_amdgcn_exp2f(stat[w][e / 16][r][0] - top);
-            ((f32x2_t*)p.stats)[(((int64_t)a * p.group_chunks + c) * 16 + r) * p.n_splits + split] = f32x2_t{mm, ll};
+            for (int w = 1; w < WK; ++w) x = join(x, stat[w][e / 16][r]);
+            ((f32x2_t*)p.stats)[(((int64_t)a * p.group_chunks + c) * 16 + r) * p.n_splits + split] = x;
           }
-          __syncthreads();
+        } else {
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              f32x2_t x = stat[0][wr * NC + k][4 * g + r];
+#pragma unroll
+              for (int w = 1; w < WK; ++w) x = join(x, stat[w][wr * NC + k][4 * g + r]);
+              st[k][r][0] = norm_of(x);
+            }
         }
       }
     }
@@ -464,10 +488,16 @@ __global__ __launch_bounds__(kThreads) void scores_kernel(const ScoresParams p) 
 
 // ---- the K best of each row.
 //
-// Values are ordered as 32-bit keys that grow with them (NaN above all, -0 as 0);
-// the K-th largest key T is found a bit at a time from the top, counting the values
-// at or above each candidate; then all values above T are taken, and of those equal
-// to it the first ones, in the order of their places.  -inf is never taken.
+// Values are ordered as 32-bit keys that grow with them (NaN above all, -0 as 0).  A
+// workgroup holds a row's keys in registers and narrows down the range in which the
+// K-th largest lies: a histogram of the keys in the range over 256 bins (an eighth of
+// the range's bits at a time, so that the bins follow the values there are), then the
+// bin that holds it.  All keys above the range are then taken, and those in it where
+// it comes down to one key, the first ones in the order of their places.  -inf is
+// never taken.
+//
+// Read once, written once; few rows are bound by the launch and by the dependent
+// steps of the search.
 
 __device__ __forceinline__ uint32_t order_key(float v) {
   if (v != v) return 0xFFFFFFFFu;
@@ -475,52 +505,171 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 constexpr uint32_t kLowestKey = 0x007FFFFFu;  // of -inf
+constexpr int kBins = 256;
 
-// A row by one wave, E values a lane: value e of lane l is place 64 e + l.
-template <int E>
-__global__ __launch_bounds__(kThreads) void topk_wave_kernel(const TopkParams p) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= p.rows) return;
-  const int lane = threadIdx.x & 63;
+// Of a histogram of `bins`, the bin that holds the `want`-th key from the top, and how
+// many of the wanted lie in it (by the first wave; want <= the number of keys).
+__device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, int lane, int* bin, uint32_t* left,
+                                         uint32_t* in_bin) {
+  // lane l holds bins 255 - 4 l .. 252 - 4 l, from the top
+  uint32_t c[4], sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    c[j] = hist[kBins - 1 - 4 * lane - j];
+    sum += c[j];
+  }
+  uint32_t up = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = __shfl_up(up, o);
+    if (lane >= o) up += v;
+  }
+  uint32_t past = up - sum;  // in the bins above the lane's
+  const uint64_t few = __ballot(past < want);
+  if (lane == 63 - __builtin_clzll(few)) {  // the last lane with fewer than `want` above it
+    int j = 0;
+    while (j < 3 && past + c[j] < want) past += c[j++];
+    *bin = kBins - 1 - 4 * lane - j;
+    *left = want - past;
+    *in_bin = c[j];
+  }
+}
+
+// A row by THREADS threads, E values each: value e of thread t is place e THREADS + t.
+template <int THREADS, int E>
+__global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
+  constexpr int kWaves = THREADS / 64;
+  __shared__ uint32_t hist[2][kBins];
+  __shared__ uint32_t wave_lo[kWaves], wave_hi[kWaves];
+  __shared__ int wave_n[kWaves];
+  // of 64 neighbours: (above, equal << 16), then the places taken before them; equal ones before them
+  __shared__ int counts[E * kWaves], eq_before[E * kWaves];
+  __shared__ int n_taken;
+  __shared__ int found;
+  __shared__ uint32_t left, in_bin;
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
   const float* const x = p.x + b * p.x_s0 + i * p.x_s1;
   int32_t* const ids = p.ids + b * p.ids_s0 + i * p.ids_s1;
-  uint32_t key[E];
+  uint32_t key[E];  // (0: no place)
+  {
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e * THREADS + tid < p.N ? x[e * THREADS + tid] : -INFINITY;
+#pragma unroll
+    for (int e = 0; e < E; ++e) key[e] = order_key(v[e]);
+  }
+  // the range of the keys above -inf, and their number
+  uint32_t lo = 0xFFFFFFFFu, hi = 0u;
   int n = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    key[e] = 64 * e + lane < p.N ? order_key(x[64 * e + lane]) : 0u;
-    n += __popcll(__ballot(key[e] > kLowestKey));
+    const bool is = key[e] > kLowestKey;
+    lo = is ? min(lo, key[e]) : lo;
+    hi = is ? max(hi, key[e]) : hi;
+    n += is ? 1 : 0;
   }
-  // the K-th largest key, if there are more than K above -inf
-  uint32_t top = kLowestKey + 1;
-  if (n > p.K) {
-    top = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t at = top | 1u << bit;
-      int c = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) c += __popcll(__ballot(key[e] >= at));
-      if (c >= p.K) top = at;
-      if (c == p.K) break;
+  for (int o = 1; o < 64; o <<= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+    n += __shfl_xor(n, o);
+  }
+  for (int t = tid; t < 2 * kBins; t += THREADS) ((uint32_t*)hist)[t] = 0;
+  if (lane == 0) {
+    wave_lo[wave] = lo;
+    wave_hi[wave] = hi;
+    wave_n[wave] = n;
+  }
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    lo = min(lo, wave_lo[w]);
+    hi = max(hi, wave_hi[w]);
+    n += wave_n[w];
+  }
+  // keys above hi are taken; of those in lo .. hi `want`
+  uint32_t want = (uint32_t)min(p.K, n);
+  if (n <= p.K) {
+    hi = kLowestKey;
+    lo = kLowestKey;
+    want = 0;
+  }
+  for (int turn = 0; lo < hi; turn ^= 1) {
+    const int bits = 32 - __builtin_clz(hi - lo), shift = max(bits - 8, 0);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (key[e] >= lo && key[e] <= hi) atomicAdd(&hist[turn][(key[e] - lo) >> shift], 1u);
+    __syncthreads();
+    if (wave == 0) find_bin(hist[turn], want, lane, &found, &left, &in_bin);
+    for (int t = tid; t < kBins; t += THREADS) hist[turn ^ 1][t] = 0;
+    __syncthreads();
+    want = left;
+    lo += (uint32_t)found << shift;
+    hi = lo + min(hi - lo, (1u << shift) - 1);
+    if (want == in_bin) {  // all of the bin
+      hi = lo - 1;
+      want = 0;
     }
   }
-  int above = 0;
+  // places before each 64 neighbours'
 #pragma unroll
-  for (int e = 0; e < E; ++e) above += __popcll(__ballot(key[e] > top));
-  int ties = p.K - above;  // of those equal to it, so many
-  int at = 0;
+  for (int e = 0; e < E; ++e) {
+    const uint64_t gt = __ballot(key[e] > hi), eq = __ballot(want != 0 && key[e] == hi);
+    if (lane == 0) counts[e * kWaves + wave] = (int)__popcll(gt) | (int)__popcll(eq) << 16;
+  }
+  __syncthreads();
+  // one wave sums them up, some neighbours a lane
+  if (wave == 0) {
+    constexpr int kPer = (E * kWaves + 63) / 64;
+    int above = 0, equal = 0;
+#pragma unroll 4
+    for (int k = 0; k < kPer; ++k) {
+      const int at = lane * kPer + k;
+      const int c = at < E * kWaves ? counts[at] : 0;
+      above += c & 0xFFFF;
+      equal += c >> 16;
+    }
+    int a = above, q = equal;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int va = __shfl_up(a, o), vq = __shfl_up(q, o);
+      if (lane >= o) {
+        a += va;
+        q += vq;
+      }
+    }
+    a -= above;
+    q -= equal;
+#pragma unroll 4
+    for (int k = 0; k < kPer; ++k) {
+      const int at = lane * kPer + k;
+      if (at < E * kWaves) {
+        const int c = counts[at];
+        // (of equal keys, no more count than are wanted)
+        counts[at] = a + min(q, (int)want);
+        eq_before[at] = q;
+        a += c & 0xFFFF;
+        q += c >> 16;
+      }
+    }
+    if (lane == 63) n_taken = a + min(q, (int)want);
+  }
+  __syncthreads();
   const uint64_t before = (1ull << lane) - 1;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const uint64_t eq = __ballot(key[e] == top);
-    const bool take = key[e] > top || (key[e] == top && (int)__popcll(eq & before) < ties);
-    const uint64_t m = __ballot(take);
-    if (take) ids[at + __popcll(m & before)] = 64 * e + lane;
-    at += __popcll(m);
-    ties -= (int)__popcll(eq);  // (below 0 once they are taken)
+    const uint64_t gt = __ballot(key[e] > hi), eq = __ballot(want != 0 && key[e] == hi);
+    if ((gt | eq) == 0) continue;
+    const int base = counts[e * kWaves + wave], q0 = eq_before[e * kWaves + wave];
+    const int mine = q0 + (int)__popcll(eq & before);
+    const bool take = key[e] > hi || (want != 0 && key[e] == hi && mine < (int)want);
+    if (take)
+      ids[base + (int)__popcll(gt & before) + min(mine, (int)want) - min(q0, (int)want)] = e * THREADS + tid;
   }
-  for (int k = at + lane; k < p.K; k += 64) ids[k] = -1;
+  for (int k = n_taken + tid; k < p.K; k += THREADS) ids[k] = -1;
 }
 
 // A row of any length by one workgroup, read from memory in each round: eight bits
@@ -528,53 +677,29 @@ __global__ __launch_bounds__(kThreads) void topk_wave_kernel(const TopkParams p)
 // found before.
 constexpr int kTopThreads = 1024;
 __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams p) {
-  __shared__ uint32_t hist[256];
+  __shared__ uint32_t hist[kBins];
   __shared__ int wave_above[kTopThreads / 64], wave_equal[kTopThreads / 64];
-  __shared__ uint32_t found;
-  __shared__ int left;
+  __shared__ int found;
+  __shared__ uint32_t left, in_bin;
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
   const float* const x = p.x + b * p.x_s0 + i * p.x_s1;
   int32_t* const ids = p.ids + b * p.ids_s0 + i * p.ids_s1;
   uint32_t top = 0;
-  int want = p.K;  // of the values that share top's bits so far, so many are taken
+  int want = min(p.K, p.N);  // of the values that share top's bits so far, so many are taken
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+    if (tid < kBins) hist[tid] = 0;
     __syncthreads();
     for (int e = tid; e < p.N; e += kTopThreads) {
       const uint32_t k = order_key(x[e]);
       if (shift == 24 || k >> (shift + 8) == top >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1u);
     }
     __syncthreads();
-    if (tid < 64) {
-      // lane l holds bins 255 - 4 l .. 252 - 4 l, from the top
-      uint32_t c[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c[j] = hist[255 - 4 * lane - j];
-        sum += c[j];
-      }
-      uint32_t up = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t v = __shfl_up(up, o);
-        if (lane >= o) up += v;
-      }
-      uint32_t past = up - sum;  // in the bins above the lane's
-      // (the last lane that has fewer than `want` above it holds the bin, or the
-      // lowest bin does where the row has fewer values)
-      const uint64_t few = __ballot(past < (uint32_t)want);
-      if (lane == 63 - __builtin_clzll(few)) {
-        int j = 0;
-        while (j < 3 && past + c[j] < (uint32_t)want) past += c[j++];
-        found = top | (uint32_t)(255 - 4 * lane - j) << shift;
-        left = want - (int)past;
-      }
-    }
+    if (wave == 0) find_bin(hist, (uint32_t)want, lane, &found, &left, &in_bin);
     __syncthreads();
-    top = found;
-    want = left;
+    top |= (uint32_t)found << shift;
+    want = (int)left;
     __syncthreads();
   }
   if (top <= kLowestKey) {  // fewer than K above -inf: all of those
@@ -588,8 +713,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
     const uint32_t k = e < p.N ? order_key(x[e]) : 0u;
     const uint64_t gt = __ballot(k > top), eq = __ballot(k == top);
     if (lane == 0) {
-      wave_above[wave] = __popcll(gt);
-      wave_equal[wave] = __popcll(eq);
+      wave_above[wave] = (int)__popcll(gt);
+      wave_equal[wave] = (int)__popcll(eq);
     }
     __syncthreads();
     int a0 = 0, q0 = 0, an = 0, qn = 0;
@@ -603,9 +728,9 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
       qn += wave_equal[w];
     }
     // places taken before this one: those above, and of those equal at most `want`
-    const int eq_before = q0 + __popcll(eq & before);
+    const int eq_before = q0 + (int)__popcll(eq & before);
     const bool take = k > top || (k == top && eq_before < want);
-    if (take) ids[at + a0 + __popcll(gt & before) + min(eq_before, want)] = e;
+    if (take) ids[at + a0 + (int)__popcll(gt & before) + min(eq_before, want)] = e;
     at += an + min(qn, want);
     want -= min(qn, want);
     __syncthreads();
@@ -615,42 +740,50 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
 
 }  // namespace
 
-hipError_t launch_means(const MeansParams& p, int kv, hipStream_t s) {
-  if (p.T <= 0) return hipSuccess;
-  // An odd number of workgroups: of the tokens that follow each other in a request
-  // every 64th completes a block, which would all be one workgroup's.
-  const int grid = (int)(p.T < 2047 ? p.T : 2047);
-  if (kv == kKvMx4) hipLaunchKernelGGL(means_kernel<kKvMx4>, dim3(grid), dim3(kThreads), 0, s, p);
-  else if (kv == kKvBf16) hipLaunchKernelGGL(means_kernel<kKvBf16>, dim3(grid), dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL(means_kernel<kKvFp8Shared>, dim3(grid), dim3(kThreads), 0, s, p);
+hipError_t launch_means(const MeansParams& p0, int kv, hipStream_t s) {
+  if (p0.T <= 0) return hipSuccess;
+  // about 2048 workgroups, one a slot below that
+  MeansParams p = p0;
+  const int64_t per = (p.T + 2047) / 2048, window = p.T < kMeanWindow ? p.T : kMeanWindow;
+  p.sharers = (int32_t)((window + per - 1) / per);
+  p.by_sharers = make_div(p.sharers);
+  const int64_t grid = (p.T + kMeanWindow - 1) / kMeanWindow * p.sharers;
+  const dim3 g((uint32_t)grid), b(kThreads);
+  if (kv == kKvMx4) hipLaunchKernelGGL(means_kernel<kKvMx4>, g, b, 0, s, p);
+  else if (kv == kKvBf16) hipLaunchKernelGGL(means_kernel<kKvBf16>, g, b, 0, s, p);
+  else hipLaunchKernelGGL(means_kernel<kKvFp8Shared>, g, b, 0, s, p);
   return hipGetLastError();
 }
 
-template <int WR>
+template <int WR, int NC, int COLS>
 static void launch_scores_rows(const ScoresParams& p, int grid, hipStream_t s) {
   if (p.n_splits == 1) {
-    hipLaunchKernelGGL((scores_kernel<WR, 0>), dim3(grid), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 0>), dim3(grid), dim3(kThreads), 0, s, p);
     return;
   }
-  hipLaunchKernelGGL((scores_kernel<WR, 1>), dim3(grid), dim3(kThreads), 0, s, p);
-  hipLaunchKernelGGL((scores_kernel<WR, 2>), dim3(grid), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 1>), dim3(grid), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 2>), dim3(grid), dim3(kThreads), 0, s, p);
 }
 
 hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s) {
   const int grid = B * p.n_groups * p.n_splits;
   if (grid <= 0) return hipSuccess;
-  if (p.wave_rows == 4) launch_scores_rows<4>(p, grid, s);
-  else if (p.wave_rows == 2) launch_scores_rows<2>(p, grid, s);
-  else launch_scores_rows<1>(p, grid, s);
+  if (p.shape == kScores128) launch_scores_rows<4, 2, 2>(p, grid, s);
+  else if (p.shape == kScores64) launch_scores_rows<2, 2, 2>(p, grid, s);
+  else if (p.shape == kScores32) launch_scores_rows<1, 2, 1>(p, grid, s);
+  else launch_scores_rows<1, 1, 1>(p, grid, s);
   return hipGetLastError();
 }
 
 hipError_t launch_topk(const TopkParams& p, hipStream_t s) {
   if (p.rows <= 0) return hipSuccess;
-  const dim3 waves((uint32_t)((p.rows + 3) / 4));
-  if (p.N <= 256) hipLaunchKernelGGL(topk_wave_kernel<4>, waves, dim3(kThreads), 0, s, p);
-  else if (p.N <= 1024) hipLaunchKernelGGL(topk_wave_kernel<16>, waves, dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL(topk_row_kernel, dim3((uint32_t)p.rows), dim3(kTopThreads), 0, s, p);
+  const dim3 g((uint32_t)p.rows);
+  if (p.N <= 256) hipLaunchKernelGGL((topk_kernel<64, 4>), g, dim3(64), 0, s, p);
+  else if (p.N <= 1024) hipLaunchKernelGGL((topk_kernel<256, 4>), g, dim3(256), 0, s, p);
+  else if (p.N <= 4096) hipLaunchKernelGGL((topk_kernel<512, 8>), g, dim3(512), 0, s, p);
+  else if (p.N <= 16384) hipLaunchKernelGGL((topk_kernel<1024, 16>), g, dim3(1024), 0, s, p);
+  else if (p.N <= 65536) hipLaunchKernelGGL((topk_kernel<1024, 64>), g, dim3(1024), 0, s, p);
+  else hipLaunchKernelGGL(topk_row_kernel, g, dim3(kTopThreads), 0, s, p);
   return hipGetLastError();
 }
 
