@@ -256,9 +256,10 @@ hipError_t launch_means(const MeansParams& p, int kv, hipStream_t s);
 // Scores of blocks by their mean keys: one workgroup a request, group of query rows
 // and split of its blocks.
 // Rows (16-row chunks of heads) of a workgroup and blocks of a tile.
-enum { kScores128, kScores64, kScores32, kScores16 };
-constexpr int kScoreChunksOf[] = {8, 4, 2, 1};
-constexpr int kScoreColsOf[] = {32, 64, 64, 64};
+enum { kScores128, kScores64, kScores32 };
+constexpr int kScoreChunksOf[] = {8, 4, 2};
+constexpr int kScoreThreads = 512;
+constexpr int kScoreCols = 64;
 struct ScoresParams {
   const uint16_t* q_lat;
   const uint16_t* q_pe;

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "mla_kernels.h"
 #include "mla_mx4.h"
 
@@ -198,25 +200,53 @@ __global__ __launch_bounds__(kThreads) void means_kernel(const MeansParams p) {
 constexpr int kKeyBytes = 2 * kMeanCols;       // 1152: 72 chunks of 16 bytes
 constexpr int kSteps = kMeanCols / 32;         // of a product: 18
 
-// A tile's keys in LDS: nine pieces of 128 bytes a row, [piece][row][128], 16-byte
-// chunk c of a piece in place c ^ key_swizzle(row).  The LDS serves 16 lanes of a
-// 16-byte read at once, rows {0..3, 8..11} (or the others) of two neighbouring chunks;
-// rows lie 0 or 128 bytes apart modulo the 64 banks, by their lowest bit, and the key
-// puts their other two bits beside the chunk's.
-__device__ __forceinline__ int key_swizzle(int n) { return ((n >> 1) & 1) << 1 | ((n >> 3) & 1) << 2; }
+// A tile's keys in LDS: latent rows of 1 KiB, 16-byte chunk c of row t in place c ^
+// lat_swizzle(t), then RoPE rows of 128 bytes, chunk c in place c ^ rope_swizzle(t).  The
+// LDS serves 16 lanes of a 16-byte read at once, rows {0..3, 8..11} of 16 (or the others)
+// of two neighbouring chunks: latent rows all begin in one bank, RoPE rows in one of two
+// by their lowest bit, and the swizzles put the rest of the row's bits beside the
+// chunk's.
+__device__ __forceinline__ int lat_swizzle(int t) { return (t & 3) << 2 | ((t >> 3) & 1) << 1; }
+__device__ __forceinline__ int rope_swizzle(int t) { return ((t >> 1) & 1) << 1 | ((t >> 3) & 1) << 2; }
 
-// 16 bytes a lane from src to dst + 16 * lane, dst the same in every lane.  The wait for
-// it is the code's own: written as asm, since the compiler would wait before every LDS
-// read that follows.
+// 16 bytes a lane from base + off to dst + 16 * lane; base and dst the same in every lane.
+// The wait for it is the code's own: written as asm, since the compiler would wait before
+// every LDS read that follows.
+__device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
+}
 __device__ __forceinline__ void to_lds(const uint8_t* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :: "v"(src), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
 }
+__device__ __forceinline__ bf16x8_t lds_read(uint32_t at, int offset) {
+  return *(const __attribute__((address_space(3))) bf16x8_t*)(uintptr_t)(at + (uint32_t)offset);
+}
 constexpr int kWaitLoads = (7 << 4) | (15 << 8);  // s_waitcnt vmcnt(0)
 
-__device__ __forceinline__ float over_rows(float v) {  // of lanes l, l ^ 16, l ^ 32, l ^ 48
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+// Sum over lanes l, l ^ 16, l ^ 32, l ^ 48 by the row-swap permutes, which leave the
+// other's value beside the own one.
+__device__ __forceinline__ float over_rows(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const uint32_t w = __float_as_uint(v);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// op over the 16 lanes of a row of lanes, by rotations within it.
+template <class Op>
+__device__ __forceinline__ float over_cols(float v, Op op) {
+  auto turned = [](float x, auto by) {
+    const int u = __float_as_int(x);
+    return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0x120 + decltype(by)::value, 0xF, 0xF, false));
+  };
+  v = op(v, turned(v, std::integral_constant<int, 1>{}));
+  v = op(v, turned(v, std::integral_constant<int, 2>{}));
+  v = op(v, turned(v, std::integral_constant<int, 4>{}));
+  return op(v, turned(v, std::integral_constant<int, 8>{}));
 }
 
 // Statistics (largest logit, sum of exponentials against it) of two sets, joined.
@@ -227,27 +257,31 @@ __device__ __forceinline__ f32x2_t join(f32x2_t a, f32x2_t b) {
 // What a logit is taken off by so that the exponentials of all are weights.
 __device__ __forceinline__ float norm_of(f32x2_t a) { return fmaxf(a[0], -3.4e38f) + __builtin_amdgcn_logf(a[1]); }
 
-// WR waves along the rows, 4 / WR along the columns, NC chunks and COLS columns of 16
+// WR waves along the rows, 8 / WR along the columns, NC chunks and COLS columns of 16
 // blocks a wave.  PASS 0: both passes; 1: the statistics of a split; 2: the scores,
 // given those of all splits.
 template <int WR, int NC, int COLS, int PASS>
-__global__ __launch_bounds__(kThreads, 2) void scores_kernel(const ScoresParams p) {
-  constexpr int WK = 4 / WR;
-  constexpr int kTile = WK * COLS * 16;        // blocks of a tile
+__global__ __launch_bounds__(kScoreThreads, 2) void scores_kernel(const ScoresParams p) {
+  constexpr int kThreads = kScoreThreads, WK = kThreads / 64 / WR;
+  constexpr int kTile = kScoreCols;            // blocks of a tile
+  static_assert(WK * COLS * 16 == kTile, "a wave's columns");
   constexpr int kSlots = WR * NC;              // chunks of the workgroup
-  constexpr int kRows = kTile / 32;            // keys a lane loads its part of
-  constexpr int kPieces = kKeyBytes / 128, kPiece = kTile * 128, kBuffer = kTile * kKeyBytes;
-  __shared__ __attribute__((aligned(16))) uint8_t keys[2 * kBuffer];
-  __shared__ float part[kSlots][kTile];
+  constexpr int kRope = kTile * 2 * kDLat, kBuffer = kTile * kKeyBytes;
+  constexpr int kLoads = 9;                    // of a wave for a tile
+  static_assert(kTile == 8 * (kThreads / 64) && kSteps == 2 * kLoads, "a load of the next tile beside two steps' products");
+  __shared__ __attribute__((aligned(1024))) uint8_t keys[2 * kBuffer];
+  __shared__ float part[2][kSlots][kTile];
   __shared__ f32x2_t stat[WK][kSlots][16];
   __shared__ int32_t is_block[2][kTile];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int wr = wave / WK, wk = wave % WK;
 
   // work item: request, group of query rows, split
-  const int a = div_by((int)blockIdx.x, p.by_splits);
-  const int split = (int)blockIdx.x - a * p.n_splits;
+  // (a request's splits on one XCD, whose L2 then holds its query rows)
+  const int w = gridDim.x % 8 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * (int)(gridDim.x / 8) + (int)(blockIdx.x / 8);
+  const int a = div_by(w, p.by_splits);
+  const int split = w - a * p.n_splits;
   const int b = div_by(a, p.by_groups);
   const int i0 = (a - b * p.n_groups) * p.group_rows;
   const int n_i = min(p.group_rows, p.Mq - i0);
@@ -276,31 +310,48 @@ __global__ __launch_bounds__(kThreads, 2) void scores_kernel(const ScoresParams 
   }
   if (t0 == t1 && PASS != 1) return;
 
-  // the keys on their way: wave w loads rows 8 w .. 8 w + 7 (and 32 on), 8 lanes a row
+  // the keys on their way: wave w loads rows 8 w .. 8 w + 7, a latent row a load, then
+  // their RoPE rows in one
   const int32_t* const table = p.table + b * p.table_s0;
-  const int kr = tid >> 3;
-  const uint32_t chunk = (uint32_t)(((tid & 7) ^ key_swizzle(kr & 15)) << 4);
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)keys;
-  int32_t id[kRows];  // of the tile that is loaded next
+  // of row 8 w + (lane & 7): the table's entry of the tile that is loaded next, and its
+  // tile (read a tile ahead, whatever it is: a read under a condition would be waited for
+  // where the condition ends)
+  int id = 0, id_tile = 0, row_of = 0;
   auto ids_of = [&](int t) {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const int j = t * kTile + kr + 32 * r;
-      id[r] = j >= lo && j < end ? table[j] : -1;
-    }
+    int l = (int)threadIdx.x & 7;
+    asm volatile("" : "+v"(l));
+    const int j = t * kTile + 8 * wave + l;
+    id = table[min(max(j, lo), end - 1)];
+    id_tile = t;
   };
-  auto load_keys = [&](int buffer) {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const bool is = id[r] >= 0 && id[r] < p.P;
-      const uint8_t* const key = p.means + (int64_t)(is ? id[r] : 0) * kKeyBytes + chunk;
-#pragma unroll
-      for (int x = 0; x < kPieces; ++x)
-        to_lds(key + 128 * x, lds + (uint32_t)(buffer * kBuffer + x * kPiece + (8 * wave + 32 * r) * 128));
-      if ((tid & 7) == 0) is_block[buffer][kr + 32 * r] = is;
+  auto aim_keys = [&](int buffer) {
+    const int j = id_tile * kTile + 8 * wave + (lane & 7);
+    const bool is = j >= lo && j < end && id >= 0 && id < p.P;
+    row_of = is ? id : 0;
+    if (lane < 8) is_block[buffer][8 * wave + lane] = is;
+  };
+  const int half8 = wave & 1;  // the wave's rows are the upper eight of 16
+  auto load_key = [&](int buffer, int s) {  // of kLoads
+    const uint32_t to = lds + (uint32_t)(buffer * kBuffer);
+    // (the lane's offsets are formed here, not held: registers are short)
+    int lane = (int)(threadIdx.x & 63);
+    asm volatile("" : "+v"(lane));
+    if (s < 8) {
+      const int64_t row = __builtin_amdgcn_readlane(row_of, s);
+      to_lds(p.means + row * kKeyBytes, (uint32_t)((lane ^ lat_swizzle(s) ^ half8 << 1) << 4),
+             to + (uint32_t)((8 * wave + s) * 1024));
+    } else {
+      const int t = lane >> 3;
+      const int64_t row = __shfl(row_of, t);
+      to_lds(p.means + row * kKeyBytes + 2 * kDLat + (((lane & 7) ^ rope_swizzle(t) ^ half8 << 2) << 4),
+             to + (uint32_t)(kRope + 8 * wave * 128));
     }
   };
   constexpr int kFirst = PASS == 2 ? 2 : 1, kLast = PASS == 1 ? 1 : 2;
+  // tiles t0 .. t1 - 1, in each pass; the one after t (in the second pass the first
+  // again)
+  auto after = [&](int t) { return t + 1 < t1 ? t + 1 : t0; };
 
   // head chunks of the query rows: chunk c of the group is heads 16 (c mod C) .. of
   // row i0 + c / C; more than kSlots of them (one query row of many heads) go in
@@ -309,179 +360,226 @@ __global__ __launch_bounds__(kThreads, 2) void scores_kernel(const ScoresParams 
   const int n_chunks = n_i * C;
   const int rounds = (n_chunks + kSlots - 1) / kSlots;
   for (int round = 0; round < rounds; ++round) {
-    // tiles t0 .. t1 - 1, in each pass; the one after t (in the second pass the first
-    // again)
-    auto after = [&](int t) { return t + 1 < t1 ? t + 1 : t0; };
-    int buffer = 0;
-    if (t0 < t1) {
-      ids_of(t0);
-      load_keys(buffer);
-      ids_of(after(t0));
+    // The query rows come through the keys' place in LDS, a chunk by each of the first
+    // waves: read from memory as the products take them, 16 rows a load by 64 bytes each,
+    // they took longer than four tiles.
+    constexpr int kQRope = kSlots * 16 * 2 * kDLat;
+    static_assert(kQRope + kSlots * 16 * 2 * kDPe <= 2 * kBuffer, "the query rows fit the keys' place");
+    if (wave < kSlots) {
+      const int c = min(round * kSlots + wave, n_chunks - 1), ci = div_by(c, p.by_chunks), h = 16 * (c - ci * C);
+      const uint16_t* const ql = p.q_lat + b * p.ql_s0 + (int64_t)(i0 + ci) * p.ql_s1;
+      const uint16_t* const qp = p.q_pe + b * p.qp_s0 + (int64_t)(i0 + ci) * p.qp_s1;
+      // (rows past the heads repeat the last one: a key that is infinite is then no NaN
+      // that the head does not have)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        to_lds((const uint8_t*)(ql + min(h + r, p.H - 1) * p.ql_s2), (uint32_t)((lane ^ lat_swizzle(r)) << 4),
+               lds + (uint32_t)((16 * wave + r) * 1024));
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int t = 8 * r + (lane >> 3);
+        to_lds((const uint8_t*)(qp + min(h + t, p.H - 1) * p.qp_s2) + (((lane & 7) ^ rope_swizzle(t)) << 4),
+               lds + (uint32_t)(kQRope + (16 * wave + 8 * r) * 128));
+      }
     }
+    if (t0 < t1) ids_of(t0);
+    if constexpr (PASS == 2) {
+      // what the rows' weights are taken off by: of all splits, four threads a row
+      int e0 = (int)threadIdx.x;
+      asm volatile("" : "+v"(e0));
+      for (int e = e0; e < kSlots * 64; e += kThreads) {
+        const int c = min(round * kSlots + e / 64, n_chunks - 1), r = e / 4 % 16;
+        const f32x2_t* const at = (const f32x2_t*)p.stats + (((int64_t)a * p.group_chunks + c) * 16 + r) * p.n_splits;
+        f32x2_t y{-INFINITY, 0.f};
+        for (int s = e & 3; s < p.n_splits; s += 4) y = join(y, at[s]);
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) y = join(y, f32x2_t{__shfl_xor(y[0], o), __shfl_xor(y[1], o)});
+        if ((e & 3) == 0) stat[0][e / 64][r] = f32x2_t{norm_of(y), 0.f};
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLoads);
+    __syncthreads();
     bf16x8_t q[NC][kSteps];
     int h0[NC], chunk_end[NC];
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
       const int c = round * kSlots + wr * NC + k;
       const bool is = c < n_chunks;
-      const int ci = is ? div_by(c, p.by_chunks) : 0, i = i0 + ci;
+      const int ci = is ? div_by(c, p.by_chunks) : 0;
       h0[k] = is ? 16 * (c - ci * C) : p.H;
-      chunk_end[k] = is ? end_of(i) : 0;
-      const int h = h0[k] + n16;
-      if (h < p.H) {
-        const uint16_t* const ql = p.q_lat + b * p.ql_s0 + (int64_t)i * p.ql_s1 + h * p.ql_s2 + 8 * g;
-        const uint16_t* const qp = p.q_pe + b * p.qp_s0 + (int64_t)i * p.qp_s1 + h * p.qp_s2 + 8 * g;
+      chunk_end[k] = is ? end_of(i0 + ci) : 0;
+      const uint32_t ql = lds + (uint32_t)((16 * (wr * NC + k) + n16) * 1024 + ((g ^ lat_swizzle(n16)) << 4));
+      const uint32_t qp = lds + (uint32_t)(kQRope + (16 * (wr * NC + k) + n16) * 128 + ((g ^ rope_swizzle(n16)) << 4));
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-          q[k][s] = s < kDLat / 32 ? *(const bf16x8_t*)(ql + 32 * s) : *(const bf16x8_t*)(qp + 32 * (s - kDLat / 32));
-      } else {
+      for (int s = 0; s < kSteps; ++s)
+        q[k][s] = s < kDLat / 32 ? lds_read(ql ^ (uint32_t)((s & 3) << 6), (s >> 2) * 256) : lds_read(qp ^ (uint32_t)((s & 1) << 6), 0);
+    }
+    __syncthreads();  // every wave holds its query rows: their place takes keys
+    int buffer = 0;
+    if (t0 < t1) {
+      aim_keys(buffer);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[k][s] = bf16x8_t{};
-      }
+      for (int s = 0; s < kLoads; ++s) load_key(buffer, s);
+      ids_of(after(t0));
     }
     // of rows 16 chunk + 4 g + r: the largest logit and sum of this lane's columns
-    // (log2 units), in the second pass what norm_of gives of all
-    f32x2_t st[NC][4];
+    // (log2 units), in the second pass what norm_of gives of all (of no head: +inf, so
+    // that its weights are 0)
+    float m[NC][4], l[NC][4];
 #pragma unroll
     for (int k = 0; k < NC; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) st[k][r] = f32x2_t{-INFINITY, 0.f};
-    if constexpr (PASS == 2) {
-#pragma unroll
-      for (int k = 0; k < NC; ++k) {
-        const int c = round * kSlots + wr * NC + k;
-        if (c >= n_chunks) continue;
-        const f32x2_t* const at = (const f32x2_t*)p.stats + (((int64_t)a * p.group_chunks + c) * 16 + 4 * g) * p.n_splits;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          // (lane n16 takes splits n16, n16 + 16, ...)
-          f32x2_t x{-INFINITY, 0.f};
-          for (int s = n16; s < p.n_splits; s += 16) x = join(x, at[r * p.n_splits + s]);
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) x = join(x, f32x2_t{__shfl_xor(x[0], o), __shfl_xor(x[1], o)});
-          st[k][r][0] = norm_of(x);
-        }
+      for (int r = 0; r < 4; ++r) {
+        m[k][r] = -INFINITY;
+        l[k][r] = 0.f;
       }
-    }
+    auto norms = [&](auto of) {
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m[k][r] = h0[k] + 4 * g + r < p.H ? of(wr * NC + k, 4 * g + r) : INFINITY;
+    };
+    if constexpr (PASS == 2) norms([&](int c, int r) { return stat[0][c][r][0]; });
 
-    for (int pass = kFirst; pass <= kLast; ++pass) {
+    // Of the scores that a pass has summed up to a row's chunks in part: a query row's
+    // chunks, in order; more than one round's are added up in place (by the same thread)
+    auto finish = [&](int t) {
+      const int c0 = round * kSlots, c1 = min(n_chunks, c0 + kSlots);
+      int e0 = (int)threadIdx.x;
+      asm volatile("" : "+v"(e0));
+      for (int e = e0; e < n_i * kTile; e += kThreads) {
+        const int ii = e / kTile, n = e % kTile, j = t * kTile + n;
+        const int from = max(ii * C, c0), to = min((ii + 1) * C, c1);
+        if (from >= to || j >= p.NB) continue;
+        float* const at = out + (int64_t)(i0 + ii) * p.out_s1 + j;
+        float sum = from > ii * C ? *at : 0.f;
+        for (int c = from; c < to; ++c) sum += part[t & 1][c - c0][n];
+        *at = sum;
+      }
+    };
+    // the lane's places in a tile of its key fragments: chunk 4 s + g of row 16 c + n16;
+    // s moves the place by an XOR of the two bits above g's and by whole 256 (128) bytes
+    const uint32_t lat_at = lds + (uint32_t)((16 * wk * COLS + n16) * 1024 + ((g ^ lat_swizzle(n16)) << 4));
+    const uint32_t rope_at = lds + (uint32_t)(kRope + (16 * wk * COLS + n16) * 128 + ((g ^ rope_swizzle(n16)) << 4));
+
+    auto run = [&](auto second) {
+      constexpr bool kScores = decltype(second)::value;  // the second pass
       for (int t = t0; t < t1; ++t) {
         // the tile has landed, and every wave is past the one before it
         __builtin_amdgcn_s_waitcnt(kWaitLoads);
         __syncthreads();
-        const uint8_t* const here = keys + buffer * kBuffer;
-        const int32_t* const blocks = is_block[buffer];
-        buffer ^= 1;
-        if (t + 1 < t1 || pass < kLast) {
-          load_keys(buffer);
-          ids_of(after(after(t)));
-        }
-        f32x4_t acc[NC][COLS];
-#pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-          for (int c = 0; c < COLS; ++c) acc[k][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-#pragma unroll
-          for (int c = 0; c < COLS; ++c) {
-            const int n = 16 * (wk * COLS + c) + n16;
-            const bf16x8_t kf = *(const bf16x8_t*)(here + (s >> 1) * kPiece + n * 128 +
-                                                   (((4 * (s & 1) + g) ^ key_swizzle(n16)) << 4));
-#pragma unroll
-            for (int k = 0; k < NC; ++k)
-              acc[k][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[k][s], kf, acc[k][c], 0, 0, 0);
-          }
-        }
-        bool block[COLS];
-        int col[COLS];
+        const uint32_t here = (uint32_t)(buffer * kBuffer);
+        bool may[NC][COLS];
 #pragma unroll
         for (int c = 0; c < COLS; ++c) {
           const int n = 16 * (wk * COLS + c) + n16;
-          block[c] = blocks[n] != 0;
-          col[c] = t * kTile + n;
+          const int is = is_block[buffer][n];
+#pragma unroll
+          for (int k = 0; k < NC; ++k) may[k][c] = (is & (int)(t * kTile + n < chunk_end[k])) != 0;
         }
-        if (pass == 1) {
+        buffer ^= 1;
+        const bool more = t + 1 < t1 || (PASS == 0 && !kScores);
+        if (more) aim_keys(buffer);
+        if (kScores && t > t0) finish(t - 1);
+        // key fragments are read two steps before their products, into the registers that
+        // the last ones' have left (left to itself the compiler waits for each where it is
+        // used); the fences keep it so
+        constexpr int kAhead = 2;
+        bf16x8_t kf[kAhead][COLS];
+        const uint32_t la = lat_at + here, ra = rope_at + here;
+        auto read_step = [&](int s) {
+#pragma unroll
+          for (int c = 0; c < COLS; ++c)
+            kf[s % kAhead][c] = s < kDLat / 32 ? lds_read(la ^ (uint32_t)((s & 3) << 6), (s >> 2) * 256 + c * 16384)
+                                          : lds_read(ra ^ (uint32_t)((s & 1) << 6), c * 2048);
+        };
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) read_step(s);
+        f32x4_t acc[NC][COLS];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          if (more && (s & 1) == 0) load_key(buffer, s >> 1);
+#pragma unroll
+          for (int c = 0; c < COLS; ++c)
+#pragma unroll
+            for (int k = 0; k < NC; ++k)
+              acc[k][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  q[k][s], kf[s % kAhead][c], s == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc[k][c], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          if (s + kAhead < kSteps) read_step(s + kAhead);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (more) ids_of(after(after(t)));
+        if constexpr (!kScores) {
 #pragma unroll
           for (int k = 0; k < NC; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float x[COLS], mx = st[k][r][0];
+              float x[COLS], mx = m[k][r];
 #pragma unroll
               for (int c = 0; c < COLS; ++c) {
-                x[c] = block[c] && col[c] < chunk_end[k] ? acc[k][c][r] * p.scale_log2 : -INFINITY;
+                x[c] = acc[k][c][r] * p.scale_log2;
+                x[c] = may[k][c] ? x[c] : -INFINITY;
                 mx = fmaxf(mx, x[c]);
               }
               const float top = fmaxf(mx, -3.4e38f);
-              float sum = st[k][r][1] * __builtin_amdgcn_exp2f(st[k][r][0] - top);
+              float sum = l[k][r] * __builtin_amdgcn_exp2f(m[k][r] - top);
 #pragma unroll
               for (int c = 0; c < COLS; ++c) sum += __builtin_amdgcn_exp2f(x[c] - top);
-              st[k][r] = f32x2_t{mx, sum};
+              l[k][r] = sum;
+              m[k][r] = mx;
             }
         } else {
 #pragma unroll
           for (int k = 0; k < NC; ++k)
 #pragma unroll
             for (int c = 0; c < COLS; ++c) {
-              float sum = 0.f;
+              float x[4];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(acc[k][c][r] * p.scale_log2 - st[k][r][0]);
-                sum += h0[k] + 4 * g + r < p.H ? e : 0.f;
-              }
-              sum = over_rows(sum);
-              if (g == 0)
-                part[wr * NC + k][16 * (wk * COLS + c) + n16] = block[c] && col[c] < chunk_end[k] ? sum : -INFINITY;
+              for (int r = 0; r < 4; ++r) x[r] = __builtin_amdgcn_exp2f(acc[k][c][r] * p.scale_log2 - m[k][r]);
+              const float sum = over_rows((x[0] + x[1]) + (x[2] + x[3]));
+              if (g == 0) part[t & 1][wr * NC + k][16 * (wk * COLS + c) + n16] = may[k][c] ? sum : -INFINITY;
             }
-          __syncthreads();
-          // a query row's chunks, in order; more than one round's are added up in
-          // place (by the same thread)
-          const int c0 = round * kSlots, c1 = min(n_chunks, c0 + kSlots);
-          for (int e = tid; e < n_i * kTile; e += kThreads) {
-            const int ii = e / kTile, n = e % kTile, j = t * kTile + n;
-            const int from = max(ii * C, c0), to = min((ii + 1) * C, c1);
-            if (from >= to || j >= p.NB) continue;
-            float* const at = out + (int64_t)(i0 + ii) * p.out_s1 + j;
-            float sum = from > ii * C ? *at : 0.f;
-            for (int c = from; c < to; ++c) sum += part[c - c0][n];
-            *at = sum;
-          }
         }
       }
-      if (pass == 1) {
-        // a row's statistics: of the lanes that share it, then of the waves
-#pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            f32x2_t x = st[k][r];
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) x = join(x, f32x2_t{__shfl_xor(x[0], o), __shfl_xor(x[1], o)});
-            if (n16 == 0) stat[wk][wr * NC + k][4 * g + r] = x;
-          }
+      if constexpr (kScores) {
         __syncthreads();
-        if constexpr (PASS == 1) {
-          for (int e = tid; e < kSlots * 16; e += kThreads) {
-            const int c = round * kSlots + e / 16, r = e % 16;
-            if (c >= n_chunks) continue;
-            f32x2_t x = stat[0][e / 16][r];
+        if (t0 < t1) finish(t1 - 1);
+      }
+    };
+    if constexpr (PASS != 2) {
+      run(std::false_type{});
+      // a row's statistics: of the lanes that share it, then of the waves
 #pragma unroll
-            for (int w = 1; w < WK; ++w) x = join(x, stat[w][e / 16][r]);
-            ((f32x2_t*)p.stats)[(((int64_t)a * p.group_chunks + c) * 16 + r) * p.n_splits + split] = x;
-          }
-        } else {
+      for (int k = 0; k < NC; ++k)
 #pragma unroll
-          for (int k = 0; k < NC; ++k)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              f32x2_t x = stat[0][wr * NC + k][4 * g + r];
-#pragma unroll
-              for (int w = 1; w < WK; ++w) x = join(x, stat[w][wr * NC + k][4 * g + r]);
-              st[k][r][0] = norm_of(x);
-            }
+        for (int r = 0; r < 4; ++r) {
+          const float mm = over_cols(m[k][r], [](float u, float v) { return fmaxf(u, v); });
+          const float ll = over_cols(l[k][r] * __builtin_amdgcn_exp2f(m[k][r] - fmaxf(mm, -3.4e38f)),
+                                     [](float u, float v) { return u + v; });
+          const f32x2_t y{mm, ll};
+          if (n16 == 0) stat[wk][wr * NC + k][4 * g + r] = y;
         }
+      __syncthreads();
+      if constexpr (PASS == 1) {
+        for (int e = tid; e < kSlots * 16; e += kThreads) {
+          const int c = round * kSlots + e / 16, r = e % 16;
+          if (c >= n_chunks) continue;
+          f32x2_t y = stat[0][e / 16][r];
+#pragma unroll
+          for (int k = 1; k < WK; ++k) y = join(y, stat[k][e / 16][r]);
+          ((f32x2_t*)p.stats)[(((int64_t)a * p.group_chunks + c) * 16 + r) * p.n_splits + split] = y;
+        }
+      } else {
+        norms([&](int c, int r) {
+          f32x2_t y = stat[0][c][r];
+#pragma unroll
+          for (int v = 1; v < WK; ++v) y = join(y, stat[v][c][r]);
+          return norm_of(y);
+        });
       }
     }
+    if constexpr (PASS != 1) run(std::true_type{});
     __syncthreads();
   }
 }
@@ -757,21 +855,21 @@ hipError_t launch_means(const MeansParams& p0, int kv, hipStream_t s) {
 
 template <int WR, int NC, int COLS>
 static void launch_scores_rows(const ScoresParams& p, int grid, hipStream_t s) {
+  const dim3 g((uint32_t)grid), b(kScoreThreads);
   if (p.n_splits == 1) {
-    hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 0>), dim3(grid), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 0>), g, b, 0, s, p);
     return;
   }
-  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 1>), dim3(grid), dim3(kThreads), 0, s, p);
-  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 2>), dim3(grid), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 1>), g, b, 0, s, p);
+  hipLaunchKernelGGL((scores_kernel<WR, NC, COLS, 2>), g, b, 0, s, p);
 }
 
 hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s) {
   const int grid = B * p.n_groups * p.n_splits;
   if (grid <= 0) return hipSuccess;
   if (p.shape == kScores128) launch_scores_rows<4, 2, 2>(p, grid, s);
-  else if (p.shape == kScores64) launch_scores_rows<2, 2, 2>(p, grid, s);
-  else if (p.shape == kScores32) launch_scores_rows<1, 2, 1>(p, grid, s);
-  else launch_scores_rows<1, 1, 1>(p, grid, s);
+  else if (p.shape == kScores64) launch_scores_rows<2, 2, 1>(p, grid, s);
+  else launch_scores_rows<2, 1, 1>(p, grid, s);
   return hipGetLastError();
 }
 

@@ -118,12 +118,12 @@ mla_status_t scores_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   p.first_block = (int32_t)(((int64_t)opts->n_sink + MLA_BLOCK - 1) / MLA_BLOCK);
   p.scale_log2 = (float)((double)scale * 1.4426950408889634074);
   const int64_t C = (H + 15) / 16;
-  const int shape = Mq * C > 4 ? mla::kScores128 : Mq * C > 2 ? mla::kScores64 : Mq * C > 1 ? mla::kScores32 : mla::kScores16;
+  const int shape = Mq * C > 4 ? mla::kScores128 : Mq * C > 2 ? mla::kScores64 : mla::kScores32;
   const int64_t slots = mla::kScoreChunksOf[shape];
   const int64_t group_rows = C >= slots ? 1 : std::min<int64_t>(Mq, slots / C);
   const int64_t n_groups = (Mq + group_rows - 1) / group_rows;
-  const int64_t tile = mla::kScoreColsOf[shape], tiles = (NB + tile - 1) / tile, items = B * n_groups;
-  int64_t S = opts->n_splits ? opts->n_splits : (2 * device_cus() + items - 1) / items;
+  const int64_t tiles = (NB + mla::kScoreCols - 1) / mla::kScoreCols, items = B * n_groups;
+  int64_t S = opts->n_splits ? opts->n_splits : (device_cus() + items - 1) / items;
   S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
   if (items * S > INT32_MAX) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
   p.shape = shape;
