@@ -291,8 +291,13 @@ struct TopkParams {
   int32_t N, K;
   Div by_Mq;
   int32_t Mq;
+  const int32_t* places;  // [rows][N] of values that are the best of pieces; null: their own
+  float* best;            // [rows][pieces][K] beside the ids; null: not asked for
 };
-hipError_t launch_topk(const TopkParams& p, hipStream_t s);
+constexpr int kTopPiece = 8192;   // of a row that goes in pieces
+constexpr int kTopMost = 65536;   // values of a row that one workgroup holds
+// (pieces > 1: ids and best of each piece of kTopPiece, rows apart by ids_s0 and ids_s1)
+hipError_t launch_topk(const TopkParams& p, int pieces, hipStream_t s);
 
 // Cache kinds of the partial kernel.
 constexpr int kKvBf16 = 0;

@@ -633,7 +633,10 @@ __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, in
   }
 }
 
-// A row by THREADS threads, E values each: value e of thread t is place e THREADS + t.
+// A row, or a piece of THREADS E places of it, by THREADS threads, E values each: value e
+// of thread t is place e THREADS + t.  A long row goes in pieces first, whose best make
+// up a shorter row (with their places beside them, in order): of a piece's values no
+// more than K can be among the row's K best.
 template <int THREADS, int E>
 __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
   constexpr int kWaves = THREADS / 64;
@@ -648,13 +651,16 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
-  const float* const x = p.x + b * p.x_s0 + i * p.x_s1;
-  int32_t* const ids = p.ids + b * p.ids_s0 + i * p.ids_s1;
+  const int first = (int)blockIdx.y * (THREADS * E), N = min(p.N - first, THREADS * E);
+  const float* const x = p.x + b * p.x_s0 + i * p.x_s1 + first;
+  const int32_t* const places = p.places ? p.places + row * p.N + first : nullptr;
+  int32_t* const ids = p.ids + b * p.ids_s0 + i * p.ids_s1 + (int64_t)blockIdx.y * p.K;
+  float* const best = p.best ? p.best + (row * gridDim.y + blockIdx.y) * p.K : nullptr;
   uint32_t key[E];  // (0: no place)
   {
     float v[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = e * THREADS + tid < p.N ? x[e * THREADS + tid] : -INFINITY;
+    for (int e = 0; e < E; ++e) v[e] = e * THREADS + tid < N ? x[e * THREADS + tid] : -INFINITY;
 #pragma unroll
     for (int e = 0; e < E; ++e) key[e] = order_key(v[e]);
   }
@@ -764,10 +770,17 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
     const int base = counts[e * kWaves + wave], q0 = eq_before[e * kWaves + wave];
     const int mine = q0 + (int)__popcll(eq & before);
     const bool take = key[e] > hi || (want != 0 && key[e] == hi && mine < (int)want);
-    if (take)
-      ids[base + (int)__popcll(gt & before) + min(mine, (int)want) - min(q0, (int)want)] = e * THREADS + tid;
+    if (take) {
+      const int at = base + (int)__popcll(gt & before) + min(mine, (int)want) - min(q0, (int)want);
+      const int place = e * THREADS + tid;
+      ids[at] = places ? places[place] : first + place;
+      if (best) best[at] = x[place];
+    }
   }
-  for (int k = n_taken + tid; k < p.K; k += THREADS) ids[k] = -1;
+  for (int k = n_taken + tid; k < p.K; k += THREADS) {
+    ids[k] = -1;
+    if (best) best[k] = -INFINITY;
+  }
 }
 
 // A row of any length by one workgroup, read from memory in each round: eight bits
@@ -873,15 +886,26 @@ hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_topk(const TopkParams& p, hipStream_t s) {
+hipError_t launch_topk(const TopkParams& p, int pieces, hipStream_t s) {
   if (p.rows <= 0) return hipSuccess;
-  const dim3 g((uint32_t)p.rows);
-  if (p.N <= 256) hipLaunchKernelGGL((topk_kernel<64, 4>), g, dim3(64), 0, s, p);
-  else if (p.N <= 1024) hipLaunchKernelGGL((topk_kernel<256, 4>), g, dim3(256), 0, s, p);
-  else if (p.N <= 4096) hipLaunchKernelGGL((topk_kernel<512, 8>), g, dim3(512), 0, s, p);
-  else if (p.N <= 16384) hipLaunchKernelGGL((topk_kernel<1024, 16>), g, dim3(1024), 0, s, p);
-  else if (p.N <= 65536) hipLaunchKernelGGL((topk_kernel<1024, 64>), g, dim3(1024), 0, s, p);
-  else hipLaunchKernelGGL(topk_row_kernel, g, dim3(kTopThreads), 0, s, p);
+  const dim3 g((uint32_t)p.rows, (uint32_t)pieces);
+  if (pieces > 1) {
+    static_assert(kTopPiece == 1024 * 8, "a piece of the kernel");
+    hipLaunchKernelGGL((topk_kernel<1024, 8>), g, dim3(1024), 0, s, p);
+  } else if (p.N <= 256) {
+    hipLaunchKernelGGL((topk_kernel<64, 4>), g, dim3(64), 0, s, p);
+  } else if (p.N <= 1024) {
+    hipLaunchKernelGGL((topk_kernel<256, 4>), g, dim3(256), 0, s, p);
+  } else if (p.N <= 4096) {
+    hipLaunchKernelGGL((topk_kernel<512, 8>), g, dim3(512), 0, s, p);
+  } else if (p.N <= 16384) {
+    hipLaunchKernelGGL((topk_kernel<1024, 16>), g, dim3(1024), 0, s, p);
+  } else if (p.N <= kTopMost) {
+    static_assert(kTopMost == 1024 * 64, "the longest row of the kernel");
+    hipLaunchKernelGGL((topk_kernel<1024, 64>), g, dim3(1024), 0, s, p);
+  } else {
+    hipLaunchKernelGGL(topk_row_kernel, g, dim3(kTopThreads), 0, s, p);
+  }
   return hipGetLastError();
 }
 

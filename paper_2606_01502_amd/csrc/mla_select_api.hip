@@ -174,7 +174,42 @@ mla_status_t topk_call(const mla_tensor_t* scores, const mla_tensor_t* ids, void
   p.K = (int32_t)K;
   p.Mq = (int32_t)Mq;
   p.by_Mq = mla::make_div(Mq);
-  return launched(mla::launch_topk(p, reinterpret_cast<hipStream_t>(stream)), "topk");
+  const hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  // Long rows in pieces, each the best of its piece, until one workgroup holds them
+  // well: 32 rows of 65,536 are 32 workgroups' work in one go, 256 in pieces.  Two
+  // halves of the workspace take turns.
+  std::unique_lock<std::mutex> lock;  // held until the last step is queued
+  char* half[2] = {};
+  int turn = 0;
+  while (p.N > 2 * mla::kTopPiece) {
+    const int64_t pieces = (p.N + mla::kTopPiece - 1) / mla::kTopPiece, best = std::min<int64_t>(p.K, mla::kTopPiece);
+    const int64_t n = pieces * best, bytes = p.rows * n * 8;
+    if (2 * n > p.N || pieces > 65535 || bytes > (64ll << 20)) break;
+    if (!half[0]) {
+      // (the first step's are the most)
+      void* ws = nullptr;
+      if (get_workspace(hs, 2 * (size_t)bytes, &ws, lock) != MLA_OK) {
+        g_last_error.clear();  // (it cannot grow here: a row is one workgroup's)
+        break;
+      }
+      half[0] = (char*)ws;
+      half[1] = half[0] + bytes;
+    }
+    mla::TopkParams q = p;
+    q.K = (int32_t)best;
+    q.best = (float*)half[turn];
+    q.ids = (int32_t*)(half[turn] + p.rows * n * 4);
+    q.ids_s0 = n * p.Mq;
+    q.ids_s1 = n;
+    if ((st = launched(mla::launch_topk(q, (int)pieces, hs), "topk")) != MLA_OK) return st;
+    p.x = q.best;
+    p.x_s0 = q.ids_s0;
+    p.x_s1 = q.ids_s1;
+    p.places = q.ids;
+    p.N = (int32_t)n;
+    turn ^= 1;
+  }
+  return launched(mla::launch_topk(p, 1, hs), "topk");
 }
 
 }  // namespace

@@ -263,6 +263,46 @@ def test_topk_all_equal_and_sorted(N):
         check_topk(x, N // 2)
 
 
+@pytest.mark.parametrize("N,K", [(16385, 100), (30000, 1), (65536, 2048), (65537, 5), (70001, 2048), (100003, 3000),
+                                 (100003, 40000), (300000, 500), (1 << 20, 2048)])
+@pytest.mark.parametrize("how", ["random", "ties", "holes"])
+def test_topk_of_long_rows(N, K, how):
+    """Rows that go in pieces, once and twice, and those that do not."""
+    print(f"case: topk {N} {K} {how}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(N + K)
+    x = torch.rand((2, 2, N), generator=g, device="cuda")
+    if how == "ties":
+        x = torch.round(x * 30)
+    if how == "holes":
+        x[0, 0, 9000:] = -float("inf")
+        x[0, 1] = -float("inf")
+        x[1, 0, :17000] = -float("inf")
+    got = mla.select_topk(x, K)
+    v, at = torch.sort(x, dim=-1, descending=True, stable=True)
+    at = torch.where(v[..., :K] == -float("inf"), N, at[..., :K])
+    want = torch.sort(at, dim=-1).values
+    assert torch.equal(got.long(), torch.where(want == N, -1, want))
+
+
+def test_topk_of_long_rows_captured_without_a_workspace():
+    x = torch.rand((3, 70000), device="cuda")
+    s = torch.cuda.Stream()
+    sync()
+    with torch.cuda.stream(s):
+        call = mla.prepare_select_topk(x, 64)
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call()
+        for _ in range(3):
+            x.uniform_()
+            g.replay()
+            s.synchronize()
+            ids = call.result.clone()
+            assert torch.equal(ids, mla.select_topk(x, 64))
+            s.synchronize()
+
+
 def test_topk_strided_rows_and_given_ids():
     x = torch.randn((3, 5, 90), device="cuda")
     ids = torch.full((3, 5, 20), 9, dtype=torch.int32, device="cuda")
