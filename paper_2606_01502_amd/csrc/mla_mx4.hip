@@ -119,7 +119,6 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const Params pp) {
   for (int k0 = 0; k0 < n; k0 += kAhead) {
     u32x4_t v[kAhead], w[kAhead];
     int64_t row[kAhead];
-    if constexpr (ROPE) rope_tokens(pp, t0 + k0, min(n - k0, kAhead), lane);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int64_t t = t0 + min(k0 + j, n - 1);  // past the end: loaded, not stored
@@ -128,6 +127,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const Params pp) {
       v[j] = *(const u32x4_t*)(p.src_ckv + t * p.ckv_s0 + 8 * lane);
       if (!ROPE && lane < 8) w[j] = *(const u32x4_t*)(p.src_kpe + t * p.kpe_s0 + 8 * lane);
     }
+    // (behind the latent rows' loads, whose trip the angles' arithmetic then shares)
+    if constexpr (ROPE) rope_tokens(pp, t0 + k0, min(n - k0, kAhead), lane);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (row[j] < 0) continue;

@@ -605,6 +605,33 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 constexpr uint32_t kLowestKey = 0x007FFFFFu;  // of -inf
 constexpr int kBins = 256;
 
+// op over a wave, in every lane: by rotations within 16 lanes, then by the row swaps.
+template <class Op>
+__device__ __forceinline__ uint32_t over_wave(uint32_t v, Op op) {
+  auto turned = [](uint32_t x, auto by) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x120 + decltype(by)::value, 0xF, 0xF, false);
+  };
+  v = op(v, turned(v, std::integral_constant<int, 1>{}));
+  v = op(v, turned(v, std::integral_constant<int, 2>{}));
+  v = op(v, turned(v, std::integral_constant<int, 4>{}));
+  v = op(v, turned(v, std::integral_constant<int, 8>{}));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = op(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return op(b[0], b[1]);
+}
+
+// Sum of v over lanes 0 .. the own one.
+__device__ __forceinline__ int lanes_up(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);   // within rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 to row 1, 47 to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+  return v;
+}
+
 // Of a histogram of `bins`, the bin that holds the `want`-th key from the top, and how
 // many of the wanted lie in it (by the first wave; want <= the number of keys).
 __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, int lane, int* bin, uint32_t* left,
@@ -616,13 +643,7 @@ __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, in
     c[j] = hist[kBins - 1 - 4 * lane - j];
     sum += c[j];
   }
-  uint32_t up = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t v = __shfl_up(up, o);
-    if (lane >= o) up += v;
-  }
-  uint32_t past = up - sum;  // in the bins above the lane's
+  uint32_t past = (uint32_t)lanes_up((int)sum) - sum;  // in the bins above the lane's
   const uint64_t few = __ballot(past < want);
   if (lane == 63 - __builtin_clzll(few)) {  // the last lane with fewer than `want` above it
     int j = 0;
@@ -674,12 +695,9 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
     hi = is ? max(hi, key[e]) : hi;
     n += is ? 1 : 0;
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-    n += __shfl_xor(n, o);
-  }
+  lo = over_wave(lo, [](uint32_t u, uint32_t v) { return min(u, v); });
+  hi = over_wave(hi, [](uint32_t u, uint32_t v) { return max(u, v); });
+  n = (int)over_wave((uint32_t)n, [](uint32_t u, uint32_t v) { return u + v; });
   for (int t = tid; t < 2 * kBins; t += THREADS) ((uint32_t*)hist)[t] = 0;
   if (lane == 0) {
     wave_lo[wave] = lo;
@@ -736,17 +754,7 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
       above += c & 0xFFFF;
       equal += c >> 16;
     }
-    int a = above, q = equal;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int va = __shfl_up(a, o), vq = __shfl_up(q, o);
-      if (lane >= o) {
-        a += va;
-        q += vq;
-      }
-    }
-    a -= above;
-    q -= equal;
+    int a = lanes_up(above) - above, q = lanes_up(equal) - equal;
 #pragma unroll 4
     for (int k = 0; k < kPer; ++k) {
       const int at = lane * kPer + k;
