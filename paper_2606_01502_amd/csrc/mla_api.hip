@@ -559,6 +559,7 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   p.grp_NB = (int32_t)NBP;
   p.grp_splits = (int32_t)plan.S;
   p.grp_tiles = (int32_t)plan.tiles;
+  p.grp_tile_step = (int32_t)plan.tile_step;
   p.grp_grid = (int32_t)plan.prefix_grid;
   p.own_items = (int32_t)plan.own_items;
   p.all_rows = (int32_t)(B * p.rows);

@@ -108,7 +108,7 @@ struct PartialParams {
   const int32_t* grp_lens;
   const int32_t* grp_table;
   int64_t grp_table_s0;
-  int32_t G, grp_NB, grp_splits, grp_tiles, grp_grid, own_items, all_rows;
+  int32_t G, grp_NB, grp_splits, grp_tiles, grp_tile_step, grp_grid, own_items, all_rows;
   Div by_grp_tiles, by_Mq;
   // windows: work items next to each other that one XCD takes, and the grid's
   // part that goes in whole rounds of them (see window_item)

@@ -813,7 +813,8 @@ struct PrefixItem {
 // The work item of workgroup `bid`; false: there is none.  Prefixes first, their row
 // tiles next to each other (one XCD's workgroups then read much the same tokens), an
 // eighth of them to each XCD.  Of the batch's rows, those of group g begin with tile
-// floor(first row / 64) + g, which leaves every group as many tiles as it may have.
+// floor(first row / 64) + g, which leaves every group as many tiles as it may have, or
+// (grp_tile_step 0) with that of their first row where no tile holds two requests' rows.
 __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int lane, PrefixItem& it) {
   if (bid >= p.grp_grid) {  // a request's own tokens; its last rows, which see most, first
     const int w = bid - p.grp_grid, a = div_by(w, p.by_splits), b = div_by(a, p.by_tiles);
@@ -830,7 +831,7 @@ __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int
   const int s = div_by(w, p.by_grp_tiles), tile = w - s * p.grp_tiles;
   if (s >= p.grp_splits) return false;
   auto start = [&](int g) { return g <= 0 ? 0 : g >= p.G ? p.q_jobs : min(max(p.grp_starts[g], 0), p.q_jobs); };
-  auto first_tile = [&](int g) { return (int)(((int64_t)start(g) * p.rows) >> 6) + g; };
+  auto first_tile = [&](int g) { return (int)(((int64_t)start(g) * p.rows) >> 6) + g * p.grp_tile_step; };
   // the last group whose first tile is not past this one, by two looks at 64 of them
   const int step = (p.G + 63) >> 6;
   int g = 0;
@@ -842,7 +843,7 @@ __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int
   it.job = g;
   it.i0 = b0 * p.Mq;
   it.rows = (b1 - b0) * p.rows;
-  it.rt = tile - ((int)(((int64_t)b0 * p.rows) >> 6) + g);
+  it.rt = tile - ((int)(((int64_t)b0 * p.rows) >> 6) + g * p.grp_tile_step);
   it.s = s;
   it.n_splits = p.grp_splits;
   return it.rt >= 0 && it.rt * 64 < it.rows;

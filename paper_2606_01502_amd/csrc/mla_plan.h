@@ -304,47 +304,56 @@ struct PrefixArgs {
 struct PrefixPlan {
   int64_t S, tiles, prefix_grid;         // splits of a prefix, tiles of all groups' rows, their workgroups
   int64_t own_S, own_tiles, own_items;   // splits and tiles of a request's own tokens
-  int64_t grid;
+  int64_t tile_step, grid;
   bool ws_f16;
   uint64_t ws_bytes;
+  double us;
 };
 inline PrefixPlan plan_prefix(const PrefixArgs& a) {
   PrefixPlan q{};
-  // (group g's rows begin with tile floor(first row / 64) + g)
-  q.tiles = a.B * a.rows / 64 + a.G;
-  const int64_t live = std::max<int64_t>(1, (a.B * a.rows + 63) / 64);  // tiles that hold rows, about
-  q.own_tiles = (a.rows + 63) / 64;
-  const int64_t own = a.B * q.own_tiles, cap = kWindowList / 2;
-  const double fixed = a.mx4 ? 11.0 : a.fp8 ? 9.4 : 8.2, block = a.fp8 || a.mx4 ? 2.3 : 1.85;
   auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
-  const int64_t least = up(a.NBP, cap), own_least = up(a.NB, cap);
-  double best = 0;
-  // as many blocks a split for both kinds of work item: the fewest that the whole takes
-  // with its work items going out in waves of one a compute unit
-  for (int64_t u = std::max<int64_t>(1, std::max(a.NBP, a.NB)); u >= 1; u = u > 16 ? u * 7 / 8 : u - 1) {
-    const int64_t S = std::max<int64_t>({1, least, a.n_splits ? std::min<int64_t>(a.n_splits, std::max<int64_t>(a.NBP, 1)) : up(a.NBP, u)});
-    const int64_t T = std::max<int64_t>({1, own_least, a.own_splits ? std::min<int64_t>(a.own_splits, std::max<int64_t>(a.NB, 1)) : up(a.NB, u)});
-    const double pre = fixed + block * (double)up(std::max<int64_t>(a.NBP, 1), S), mine = fixed + block * (double)up(std::max<int64_t>(a.NB, 1), T);
-    const double all = (double)(live * S) * pre + (double)(own * T) * mine;
-    // (the longest item last at worst)
-    const double items = (double)(live * S + own * T), waves = items / (double)a.cus;
-    const double whole = std::max(pre, mine) * std::ceil(waves), even = all / (double)a.cus;
-    const double rows = (double)(a.B * a.rows) * (double)(S + T);
-    const double us = std::max(even, std::min(whole, even + std::max(pre, mine) * 0.5)) + 0.4e-6 * rows * kDLat * 2 +
-                      (S + T > 16 ? 0.2 * (double)(S + T - 16) : 0.0);
-    if (q.S == 0 || us < best) {
-      best = us;
-      q.S = S;
-      q.own_S = T;
-    }
-    if (a.n_splits && a.own_splits) break;
+  // Group g's rows begin with tile floor(first row / 64) + g, or where every request fills
+  // whole tiles with that of its first row.
+  q.tile_step = a.rows % 64 ? 1 : 0;
+  q.tiles = up(a.B * a.rows, 64) + q.tile_step * (a.G - 1);
+  q.own_tiles = up(a.rows, 64);
+  const int64_t own = a.B * q.own_tiles, cap = kWindowList / 2;
+  const int64_t nbp = std::max<int64_t>(a.NBP, 1), nb = std::max<int64_t>(a.NB, 1);
+  // (rates of the 64-row kernel's windows, see Planner::plan_of)
+  const double fixed = a.mx4 ? 11.0 : a.fp8 ? 9.4 : 8.2, block = a.fp8 || a.mx4 ? 2.3 : 1.85;
+  // What the launch takes: prefix items go out first, one to a compute unit at a time,
+  // the requests' own where compute units come free.
+  auto span = [&](int64_t n, double p, int64_t m, double o) {
+    const int64_t rounds = n / a.cus, rest = n % a.cus, free = a.cus - rest;
+    const double base = (double)rounds * p;
+    if (rest == 0) return base + (double)up(m, a.cus) * o;
+    const int64_t beside = free * (int64_t)(p / o);
+    return m <= beside ? base + p : base + p + (double)up(m - beside, a.cus) * o;
+  };
+  auto offer = [&](int64_t S, int64_t T) {
+    S = std::max<int64_t>({1, up(a.NBP, cap), a.n_splits ? std::min<int64_t>(a.n_splits, nbp) : std::min(S, nbp)});
+    T = std::max<int64_t>({1, up(a.NB, cap), a.own_splits ? std::min<int64_t>(a.own_splits, nb) : std::min(T, nb)});
+    const uint64_t rows = (uint64_t)(S + T) * a.B * a.rows;
+    const bool half = rows * kDLat * 4 >= kWsHalfMinBytes;
+    PrefixPlan c = q;
+    c.us = span(q.tiles * S, fixed + block * (double)up(nbp, S), own * T, fixed + block * (double)up(nb, T)) +
+           0.4e-6 * (double)(rows * kDLat * (half ? 2 : 4)) + (S + T > 16 ? 0.2 * (double)(S + T - 16) : 0.0);
+    if (q.S != 0 && c.us >= q.us) return;
+    c.S = S;
+    c.own_S = T;
+    c.ws_f16 = half;
+    c.ws_bytes = rows * (kDLat * (half ? 2 : 4) + 3 * 4);
+    q = c;
+  };
+  static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+  for (int64_t T = 1; T == 1 || (T <= a.NB && own * T <= 2 * a.cus); T *= 2) {
+    for (int64_t S : kCounts)
+      if (S == 1 || (S <= nbp && q.tiles * S <= 3 * a.cus)) offer(S, T);
+    for (int waves = 1; waves <= 4; ++waves) offer(std::max<int64_t>(1, waves * a.cus / q.tiles), T);
   }
   q.prefix_grid = up(q.tiles * q.S, 8) * 8;
   q.own_items = own * q.own_S;
   q.grid = q.prefix_grid + q.own_items;
-  const uint64_t n = (uint64_t)(q.S + q.own_S) * a.B * a.rows;
-  q.ws_f16 = n * kDLat * 4 >= kWsHalfMinBytes;
-  q.ws_bytes = n * (kDLat * (q.ws_f16 ? 2 : 4) + 3 * 4);
   return q;
 }
 
