@@ -489,10 +489,14 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   if ((st = check_tensor(seq_lens, "seq_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (q_lens && (st = check_tensor(q_lens, "q_lens", MLA_DTYPE_INT32, 1)) != MLA_OK) return st;
   if (!opts) return bad("opts: null pointer");
-  for (int i = 0; i < 5; ++i)
+  for (int i = 0; i < 4; ++i)
     if (opts->reserved[i]) return bad("opts.reserved must be zero");
   if (opts->n_splits < 0) return bad("opts.n_splits must be >= 0");
   if (opts->own_splits < 0) return bad("opts.own_splits must be >= 0");
+  if (opts->row_tile != 0 && opts->row_tile != 64 && opts->row_tile != 128)
+    return bad("opts.row_tile must be 0, 64 or 128");
+  if (opts->row_tile == 128 && ckv_pool->dtype == MLA_DTYPE_MXFP4)
+    return fail(MLA_ERR_UNSUPPORTED, "4-bit caches take 64-row tiles");
   if (opts->out_format != MLA_OUT_FP32 && opts->out_format != MLA_OUT_BF16_WIRE)
     return bad("opts.out_format must be MLA_OUT_FP32 or MLA_OUT_BF16_WIRE");
   const bool wire = opts->out_format == MLA_OUT_BF16_WIRE;
@@ -544,7 +548,7 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   if (!one_dim(*q_lat, &p.ql_s1) || !one_dim(*q_pe, &p.qp_s1) || !one_dim(*out_lat, &p.out_s1) ||
       !one_dim(*out_lse, &p.lse_s1))
     return fail(MLA_ERR_UNSUPPORTED, "q and out: requests and query rows must be one dim");
-  const mla::PrefixPlan plan = mla::plan_prefix({B, G, NBP, NB, p.rows, device_cus(), opts->n_splits, opts->own_splits, fp8, mx4});
+  const mla::PrefixPlan plan = mla::plan_prefix({B, G, NBP, NB, p.rows, device_cus(), opts->n_splits, opts->own_splits, opts->row_tile, fp8, mx4});
   if (plan.grid > (1 << 22)) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
   p.q_jobs = (int32_t)B;
   p.q_rep = 1;
@@ -560,6 +564,7 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   p.grp_splits = (int32_t)plan.S;
   p.grp_tiles = (int32_t)plan.tiles;
   p.grp_tile_step = (int32_t)plan.tile_step;
+  p.grp_shift = plan.row_groups == 2 ? 7 : 6;
   p.grp_grid = (int32_t)plan.prefix_grid;
   p.own_items = (int32_t)plan.own_items;
   p.all_rows = (int32_t)(B * p.rows);
@@ -580,7 +585,7 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   p.ws_scale = (float*)((char*)ws + (uint64_t)n_part_rows * mla::kDLat * (plan.ws_f16 ? 2 : 4));
   p.ws_lse = p.ws_scale + n_part_rows;
   p.ws_max = p.ws_lse + n_part_rows;
-  hipError_t e = mla::launch_prefix(p, cache_kind(*ckv_pool, *kpe_pool), hs);
+  hipError_t e = mla::launch_prefix(p, cache_kind(*ckv_pool, *kpe_pool), plan.row_groups, hs);
   if (e != hipSuccess) return fail(MLA_ERR_HIP, std::string("prefix kernel launch: ") + hipGetErrorString(e));
   // all rows as one job's, whose splits lie one after another
   mla::CombineParams c{};

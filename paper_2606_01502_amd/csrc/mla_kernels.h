@@ -102,13 +102,13 @@ struct PartialParams {
   int32_t window, n_sink;
   int32_t win_lo_mask;  // -64: windows begin with whole blocks; else -1
   // shared prefixes: groups of requests (first requests [G + 1], tokens, block tables),
-  // splits of a prefix and tiles of all prefixes' rows, workgroups of those (a multiple
+  // splits of a prefix and tiles (of 2^shift) of all prefixes' rows, workgroups of those (a multiple
   // of 8), work items of the requests' own tokens, rows of the batch
   const int32_t* grp_starts;
   const int32_t* grp_lens;
   const int32_t* grp_table;
   int64_t grp_table_s0;
-  int32_t G, grp_NB, grp_splits, grp_tiles, grp_tile_step, grp_grid, own_items, all_rows;
+  int32_t G, grp_NB, grp_splits, grp_tiles, grp_tile_step, grp_shift, grp_grid, own_items, all_rows;
   Div by_grp_tiles, by_Mq;
   // windows: work items next to each other that one XCD takes, and the grid's
   // part that goes in whole rounds of them (see window_item)
@@ -346,7 +346,7 @@ constexpr int kShareMost = 64;
 // row_groups: 2 (row tiles of 128 rows) or 1 (row tiles of 64 rows)
 hipError_t launch_partial(const PartialParams& p, int R, int kv, int row_groups, int sel_kind,
                           hipStream_t s);
-hipError_t launch_prefix(const PartialParams& p, int kv, hipStream_t s);
+hipError_t launch_prefix(const PartialParams& p, int kv, int row_groups, hipStream_t s);
 hipError_t launch_combine(const CombineParams& p, hipStream_t s);
 hipError_t launch_merge(const MergeParams& p, hipStream_t s);
 

@@ -813,7 +813,7 @@ struct PrefixItem {
 // The work item of workgroup `bid`; false: there is none.  Prefixes first, their row
 // tiles next to each other (one XCD's workgroups then read much the same tokens), an
 // eighth of them to each XCD.  Of the batch's rows, those of group g begin with tile
-// floor(first row / 64) + g, which leaves every group as many tiles as it may have, or
+// floor(first row / tile) + g, which leaves every group as many tiles as it may have, or
 // (grp_tile_step 0) with that of their first row where no tile holds two requests' rows.
 __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int lane, PrefixItem& it) {
   if (bid >= p.grp_grid) {  // a request's own tokens; its last rows, which see most, first
@@ -831,7 +831,7 @@ __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int
   const int s = div_by(w, p.by_grp_tiles), tile = w - s * p.grp_tiles;
   if (s >= p.grp_splits) return false;
   auto start = [&](int g) { return g <= 0 ? 0 : g >= p.G ? p.q_jobs : min(max(p.grp_starts[g], 0), p.q_jobs); };
-  auto first_tile = [&](int g) { return (int)(((int64_t)start(g) * p.rows) >> 6) + g * p.grp_tile_step; };
+  auto first_tile = [&](int g) { return (int)(((int64_t)start(g) * p.rows) >> p.grp_shift) + g * p.grp_tile_step; };
   // the last group whose first tile is not past this one, by two looks at 64 of them
   const int step = (p.G + 63) >> 6;
   int g = 0;
@@ -843,10 +843,21 @@ __device__ __forceinline__ bool prefix_item(const PartialParams& p, int bid, int
   it.job = g;
   it.i0 = b0 * p.Mq;
   it.rows = (b1 - b0) * p.rows;
-  it.rt = tile - ((int)(((int64_t)b0 * p.rows) >> 6) + g * p.grp_tile_step);
+  it.rt = tile - ((int)(((int64_t)b0 * p.rows) >> p.grp_shift) + g * p.grp_tile_step);
   it.s = s;
   it.n_splits = p.grp_splits;
-  return it.rt >= 0 && it.rt * 64 < it.rows;
+  return it.rt >= 0 && it.rt << p.grp_shift < it.rows;
+}
+
+// Whether query row iv of the batch is one that its request does not have.
+__device__ __forceinline__ bool prefix_row_empty(const PartialParams& p, int iv) {
+  const int b = min(div_by(iv, p.by_Mq), p.q_jobs - 1);
+  return iv - b * p.Mq >= p.win_qlens[b];
+}
+// The item's first row in the workspace: splits of the prefixes, then of own tokens, each
+// with the rows of the batch.
+__device__ __forceinline__ int64_t prefix_ws_row(const PartialParams& p, const PrefixItem& it) {
+  return (int64_t)(it.prefix ? it.s : p.grp_splits + it.s) * p.all_rows + (int64_t)it.i0 * p.H;
 }
 
 __device__ __forceinline__ Window prefix_window(const PartialParams& p, const PrefixItem& it) {
@@ -1072,7 +1083,8 @@ void partial_kernel(const PartialParams p) {
   constexpr bool FP8 = KV != kKvBf16;
   constexpr bool PR = SEL == kSelPerRow;   // a block selection per query row
   constexpr bool TOK = SEL == kSelTokens;  // token selections, 64 to a virtual block
-  constexpr bool WIN = SEL == kSelWindow;  // no selection: the tokens each row sees
+  constexpr bool GRP = SEL == kSelPrefix;  // windows without bounds, over own tokens or a group's prefix
+  constexpr bool WIN = SEL == kSelWindow || GRP;  // no selection: the tokens each row sees
   constexpr bool kSplitScales = KV == kKvFp8Split;
   using L = Layout<FP8>;
   constexpr int kTau4 = kBlock / 16;   // 16-token tiles per block
@@ -1097,7 +1109,11 @@ void partial_kernel(const PartialParams p) {
   // of the same residue class, which then meet in the L2 of one or two XCDs
   // instead of all eight (the query rows, read once per split, are what is
   // fetched more than once instead, the smaller of the two).
-  const int w_id = WIN ? window_item(p, blockIdx.x)
+  PrefixItem item{};
+  if constexpr (GRP) {
+    if (!prefix_item(p, blockIdx.x, lane, item)) return;
+  }
+  const int w_id = GRP ? 0 : WIN ? window_item(p, blockIdx.x)
                        : p.first + (p.grid8 == 0 ? (int)blockIdx.x : (int)(blockIdx.x % 8) * p.grid8 + (int)(blockIdx.x / 8));
   const bool tiles_fast = PR && p.tiles_fast;
   int s_idx, rt, r_num;
@@ -1113,7 +1129,11 @@ void partial_kernel(const PartialParams p) {
     rt = a - r_num * p.row_tiles;
   }
   int n_of = p.n_splits, part0 = 0;  // windows: the splits of the request, and its first one
-  if constexpr (WIN) {
+  if constexpr (GRP) {
+    s_idx = item.s;
+    rt = item.rt;
+    n_of = item.n_splits;
+  } else if constexpr (WIN) {
     part0 = r_num * n_of;
     if (p.ws_share) {
       Share sh;
@@ -1132,6 +1152,9 @@ void partial_kernel(const PartialParams p) {
   const int rep = p.q_rep > 1 ? div_by(r_num, p.by_rep) : 0;
   const int r = p.q_rep > 1 ? (r_num - rep * p.q_rep) * p.q_jobs + rep : r_num;
   const int rq = p.q_rep > 1 ? rep : r_num;
+  const int n_rows = GRP ? item.rows : p.rows;
+  // the first of the job's query rows in q
+  const int64_t q_lat0 = GRP ? item.i0 * p.ql_s1 : rq * p.ql_s0, q_pe0 = GRP ? item.i0 * p.qp_s1 : rq * p.qp_s0;
   const int slot0 = s_idx * p.slots_per_split;
   const int nslots = max(0, min(p.K - slot0, p.slots_per_split));
 
@@ -1147,7 +1170,7 @@ void partial_kernel(const PartialParams p) {
   // (split s takes blocks s, s + S, ... from every slot), so that rows which
   // chose one block in different slots share its load, or by slot range when
   // a tile's slots may not fit one list
-  const int n_i = PR || WIN ? div_by(min((rt + 1) * kRowsWg, p.rows) - 1, p.by_H) - i0 + 1 : 1;
+  const int n_i = PR || WIN ? div_by(min((rt + 1) * kRowsWg, n_rows) - 1, p.by_H) - i0 + 1 : 1;
   const int c_slot0 = PR && p.split_by_id ? 0 : slot0;
   const int c_nslots = PR && p.split_by_id ? p.K : nslots;
   // the slot id this thread compacts first
@@ -1169,10 +1192,10 @@ void partial_kernel(const PartialParams p) {
 #pragma unroll
   for (int rg = 0; rg < RG; ++rg) {
     const int row = row_wg0 + wave * 16 * RG + rg * 16 + n16;
-    if (row < p.rows) {
+    if (row < n_rows) {
       const int i = div_by(row, p.by_H), h = row - i * p.H;
-      const uint16_t* ql = p.q_lat + rq * p.ql_s0 + i * p.ql_s1 + h * p.ql_s2 + g * 8;
-      const uint16_t* qp = p.q_pe + rq * p.qp_s0 + i * p.qp_s1 + h * p.qp_s2 + g * 8;
+      const uint16_t* ql = p.q_lat + q_lat0 + i * p.ql_s1 + h * p.ql_s2 + g * 8;
+      const uint16_t* qp = p.q_pe + q_pe0 + i * p.qp_s1 + h * p.qp_s2 + g * 8;
 #pragma unroll
       for (int ks = 0; ks < 16; ++ks) qb[rg][ks] = *(const bf16x8_t*)(ql + ks * 32);
 #pragma unroll
@@ -1189,8 +1212,14 @@ void partial_kernel(const PartialParams p) {
   int n_tok = 0;  // token selections: the listed tokens (n_valid counts virtual blocks)
   Window win{};
   if constexpr (WIN) {
-    win = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
-    n_valid = compact_window<L, 6>(p, p.table + r * p.table_s0, s_idx, n_of, i0, n_i, L::kPerRowCap, win, smem, tid);
+    const int32_t* table = p.table + r * p.table_s0;
+    if constexpr (GRP) {
+      win = prefix_window(p, item);
+      table = item.prefix ? p.grp_table + item.job * p.grp_table_s0 : p.table + item.job * p.table_s0;
+    } else {
+      win = window_of(p, p.win_lens[r], p.win_qlens ? p.win_qlens[r] : p.Mq);
+    }
+    n_valid = compact_window<L, 6>(p, table, s_idx, n_of, i0, n_i, L::kPerRowCap, win, smem, tid);
   } else if constexpr (PR) {
     n_valid = compact_per_row<L>(p, r, c_slot0, c_nslots, p.split_by_id ? s_idx : 0,
                                    p.split_by_id ? p.n_splits : 1, i0, n_i, first_id, smem, list,
@@ -1255,6 +1284,10 @@ void partial_kernel(const PartialParams p) {
     if constexpr (WIN) {
       hi_row[rg] = win.hi_of(div_by(row, p.by_H));
       lo_row[rg] = win.lo_of(div_by(row, p.by_H));
+    }
+    if constexpr (GRP) {
+      if (item.prefix && p.win_qlens && prefix_row_empty(p, item.i0 + div_by(row, p.by_H))) hi_row[rg] = -1;
+      if (__ballot(hi_row[rg] < 0) != 0) win.hi_all = -1;
     }
     row_bit[rg] = PR ? min(max(div_by(row, p.by_H) - i0, 0), 63) : 0;
   }
@@ -1664,9 +1697,11 @@ void partial_kernel(const PartialParams p) {
   // back; those
   // rows are transposed through LDS (a 32 KiB area per wave, 16-byte chunk c
   // of row rr in slot c ^ rr) and stored as contiguous 1 KiB rows.
-  const bool direct = p.n_splits == 1;
+  const bool direct = !GRP && p.n_splits == 1;
   const bool half = !direct && p.ws_f16;
   const int64_t part = (WIN ? part0 : (int64_t)r * p.n_splits) + s_idx;
+  // the tile's rows in the workspace, less `row`
+  const int64_t ws_row0 = GRP ? prefix_ws_row(p, item) : part * p.rows;
   if constexpr (WIN) {
     if (p.ws_share && rt == 0 && s_idx == 0 && tid == 0) {
       p.ws_share[2 * r] = part0;
@@ -1686,7 +1721,7 @@ void partial_kernel(const PartialParams p) {
     const float lse = some ? (m_run[rg] + __log2f(l_tot)) * kLn2 : -INFINITY;
     const float inv = some ? 1.f / l_tot : 0.f;
     if (!half) {
-      if (g == 0 && row < p.rows) {
+      if (g == 0 && row < n_rows) {
         if (direct) {
           const int i = div_by(row, p.by_H), hd = row - i * p.H;
           const int64_t lo = r * p.lse_s0 + i * p.lse_s1 + hd * p.lse_s2;
@@ -1701,11 +1736,11 @@ void partial_kernel(const PartialParams p) {
             p.lse[lo] = lse;
           }
         } else {
-          p.ws_lse[part * p.rows + row] = lse;
-          if (p.out_wire) p.ws_max[part * p.rows + row] = m_true[rg];
+          p.ws_lse[ws_row0 + row] = lse;
+          if (p.out_wire) p.ws_max[ws_row0 + row] = m_true[rg];
         }
       }
-      if (row < p.rows && direct && p.out_wire) {
+      if (row < n_rows && direct && p.out_wire) {
         // bf16 rows: 8-byte runs per row and instruction
         const int i = div_by(row, p.by_H), hd = row - i * p.H;
         uint16_t* dst = p.out16 + r * p.out_s0 + i * p.out_s1 + hd * p.out_s2;
@@ -1715,13 +1750,13 @@ void partial_kernel(const PartialParams p) {
           asm volatile("" : "+a"(v));  // read in place, no copy back
           *(u16x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_bf16(v * inv);
         }
-      } else if (row < p.rows) {
+      } else if (row < n_rows) {
         float* dst;
         if (direct) {
           const int i = div_by(row, p.by_H), hd = row - i * p.H;
           dst = p.out + r * p.out_s0 + i * p.out_s1 + hd * p.out_s2;
         } else {
-          dst = p.ws_o32 + (part * p.rows + row) * kDLat;
+          dst = p.ws_o32 + (ws_row0 + row) * kDLat;
         }
 #pragma unroll
         for (int dt = 0; dt < 32; ++dt) {
@@ -1744,10 +1779,10 @@ void partial_kernel(const PartialParams p) {
     }
     amax = xor_max(amax);
     const float row_scale = amax > 0.f ? amax : 1.f;
-    if (g == 0 && row < p.rows) {
-      p.ws_lse[part * p.rows + row] = lse;
-      p.ws_scale[part * p.rows + row] = row_scale;
-      if (p.out_wire) p.ws_max[part * p.rows + row] = m_true[rg];
+    if (g == 0 && row < n_rows) {
+      p.ws_lse[ws_row0 + row] = lse;
+      p.ws_scale[ws_row0 + row] = row_scale;
+      if (p.out_wire) p.ws_max[ws_row0 + row] = m_true[rg];
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS writes are done
     // lane ln stores 16-byte chunk ln of row rr's 1 KiB fp16 row: columns
@@ -1756,7 +1791,7 @@ void partial_kernel(const PartialParams p) {
 #pragma unroll
     for (int rr = 0; rr < 16; ++rr) {
       const int rw = row0 + rr;
-      if (rw >= p.rows) break;
+      if (rw >= n_rows) break;
       // lane rr holds row rr's scale; a constant lane index reads it into a
       // scalar register
       const float is = __builtin_bit_cast(
@@ -1768,7 +1803,7 @@ void partial_kernel(const PartialParams p) {
       h[1] = pack_f16(a[2] * is, a[3] * is);
       h[2] = pack_f16(b[0] * is, b[1] * is);
       h[3] = pack_f16(b[2] * is, b[3] * is);
-      *(u32x4_t*)(p.ws_o16 + (part * p.rows + rw) * kDLat + 8 * ln) = h;
+      *(u32x4_t*)(p.ws_o16 + (ws_row0 + rw) * kDLat + 8 * ln) = h;
     }
     __builtin_amdgcn_s_waitcnt(0xc07f);  // reads of this row group done before it is overwritten
   }
@@ -1783,13 +1818,13 @@ void partial_kernel(const PartialParams p) {
     for (int rg = 0; rg < RG; ++rg) {
       const int row0 = row_wg0 + wave * 16 * RG + rg * 16;
       const int row = row0 + n16;
-      const bool none = xor_sum(l_run[rg]) == 0.f && row < p.rows;
+      const bool none = xor_sum(l_run[rg]) == 0.f && row < n_rows;
       const uint32_t rows_none = (uint32_t)__ballot(none) & 0xffffu;
       if (rows_none == 0) continue;
       if (half) {
 #pragma unroll 1
         for (int rr = 0; rr < 16; ++rr)
-          if (rows_none >> rr & 1) *(u32x4_t*)(p.ws_o16 + (part * p.rows + row0 + rr) * kDLat + 8 * ln) = u32x4_t{};
+          if (rows_none >> rr & 1) *(u32x4_t*)(p.ws_o16 + (ws_row0 + row0 + rr) * kDLat + 8 * ln) = u32x4_t{};
       } else if (none) {
         const int i = div_by(row, p.by_H), hd = row - i * p.H;
         const int64_t oo = r * p.out_s0 + i * p.out_s1 + hd * p.out_s2;
@@ -1797,7 +1832,7 @@ void partial_kernel(const PartialParams p) {
 #pragma unroll 1
           for (int dt = 0; dt < 32; ++dt) *(u16x4_t*)(p.out16 + oo + 4 * (4 * dt + g)) = u16x4_t{};
         } else {
-          float* const dst = direct ? p.out + oo : p.ws_o32 + (part * p.rows + row) * kDLat;
+          float* const dst = direct ? p.out + oo : p.ws_o32 + (ws_row0 + row) * kDLat;
 #pragma unroll 1
           for (int dt = 0; dt < 32; ++dt) *(f32x4_t*)(dst + 4 * (4 * dt + g)) = f32x4_t{};
         }
@@ -2369,10 +2404,8 @@ void tile64_kernel(const PartialParams p) {
     if constexpr (GRP) {
       // a prefix's rows that their requests do not have see nothing
       if (item.prefix && p.win_qlens) {
-        const int iv = item.i0 + i_row, b = min(div_by(iv, p.by_Mq), p.q_jobs - 1);
-        const bool none = iv - b * p.Mq >= p.win_qlens[b];
-        if (none) hi_row = -1;
-        if (__ballot(none) != 0) win.hi_all = -1;
+        if (prefix_row_empty(p, item.i0 + i_row)) hi_row = -1;
+        if (__ballot(hi_row < 0) != 0) win.hi_all = -1;
       }
     }
   } else if constexpr (PR) {
@@ -2921,8 +2954,7 @@ void tile64_kernel(const PartialParams p) {
   const bool half = !direct && p.ws_f16;
   const int64_t part = (WIN ? part0 : (int64_t)r * p.n_splits) + s_idx;
   // the tile's rows in the workspace, less `row`
-  const int64_t ws_row0 = GRP ? (item.prefix ? s_idx : p.grp_splits + s_idx) * (int64_t)p.all_rows + (int64_t)item.i0 * p.H
-                              : part * p.rows;
+  const int64_t ws_row0 = GRP ? prefix_ws_row(p, item) : part * p.rows;
   if constexpr (WIN) {
     if (p.ws_share && rt == 0 && s_idx == 0 && tid == 0) {
       p.ws_share[2 * r] = part0;
@@ -3186,10 +3218,14 @@ static void launch_kv(const PartialParams& p, int grid, int row_groups, hipStrea
     launch_items(tile64_kernel<KV, SEL, 2>, p, grid, 512, s);
 }
 
-// Prefixes of groups and own tokens: 64-row tiles, one launch.
-hipError_t launch_prefix(const PartialParams& p, int kv, hipStream_t s) {
-  const dim3 grid((uint32_t)(p.grp_grid + p.own_items)), wg(512);
-  if (kv == kKvMx4) hipLaunchKernelGGL((tile64_kernel<kKvMx4, kSelPrefix, 2>), grid, wg, 0, s, p);
+// Prefixes of groups and own tokens, one launch.
+hipError_t launch_prefix(const PartialParams& p, int kv, int row_groups, hipStream_t s) {
+  const dim3 grid((uint32_t)(p.grp_grid + p.own_items)), wg(row_groups == 2 ? 256 : 512);
+  if (row_groups == 2) {
+    if (kv == kKvFp8Shared) hipLaunchKernelGGL((partial_kernel<2, kKvFp8Shared, kSelPrefix>), grid, wg, 0, s, p);
+    else if (kv == kKvFp8Split) hipLaunchKernelGGL((partial_kernel<2, kKvFp8Split, kSelPrefix>), grid, wg, 0, s, p);
+    else hipLaunchKernelGGL((partial_kernel<2, kKvBf16, kSelPrefix>), grid, wg, 0, s, p);
+  } else if (kv == kKvMx4) hipLaunchKernelGGL((tile64_kernel<kKvMx4, kSelPrefix, 2>), grid, wg, 0, s, p);
   else if (kv == kKvFp8Shared) hipLaunchKernelGGL((tile64_kernel<kKvFp8Shared, kSelPrefix, 2>), grid, wg, 0, s, p);
   else if (kv == kKvFp8Split) hipLaunchKernelGGL((tile64_kernel<kKvFp8Split, kSelPrefix, 2>), grid, wg, 0, s, p);
   else hipLaunchKernelGGL((tile64_kernel<kKvBf16, kSelPrefix, 2>), grid, wg, 0, s, p);

@@ -293,15 +293,16 @@ struct Planner {
   }
 };
 
-// The plan of attention behind shared prefixes: 64-row tiles of the groups' rows over
-// the prefixes and of each request's rows over its own tokens, in one launch.
+// The plan of attention behind shared prefixes: tiles of the groups' rows over the
+// prefixes and of each request's rows over its own tokens, in one launch.
 struct PrefixArgs {
   int64_t B, G, NBP, NB, rows;  // rows: of a request
   int64_t cus;
-  int32_t n_splits, own_splits;  // the caller's, or 0
+  int32_t n_splits, own_splits, row_tile;  // the caller's, or 0
   bool fp8, mx4;
 };
 struct PrefixPlan {
+  int row_groups;                        // of 64 rows a tile: 1 or 2
   int64_t S, tiles, prefix_grid;         // splits of a prefix, tiles of all groups' rows, their workgroups
   int64_t own_S, own_tiles, own_items;   // splits and tiles of a request's own tokens
   int64_t tile_step, grid;
@@ -312,15 +313,24 @@ struct PrefixPlan {
 inline PrefixPlan plan_prefix(const PrefixArgs& a) {
   PrefixPlan q{};
   auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
-  // Group g's rows begin with tile floor(first row / 64) + g, or where every request fills
-  // whole tiles with that of its first row.
-  q.tile_step = a.rows % 64 ? 1 : 0;
-  q.tiles = up(a.B * a.rows, 64) + q.tile_step * (a.G - 1);
-  q.own_tiles = up(a.rows, 64);
-  const int64_t own = a.B * q.own_tiles, cap = kWindowList / 2;
+  // Group g's rows begin with tile floor(first row / tile) + g, or where every request
+  // fills whole tiles with that of its first row.
+  auto shape = [&](int rg) {
+    PrefixPlan c{};
+    c.row_groups = rg;
+    c.tile_step = a.rows % (64 * rg) ? 1 : 0;
+    c.tiles = up(a.B * a.rows, 64 * rg) + c.tile_step * (a.G - 1);
+    c.own_tiles = up(a.rows, 64 * rg);
+    return c;
+  };
+  const int64_t cap = kWindowList / 2;
   const int64_t nbp = std::max<int64_t>(a.NBP, 1), nb = std::max<int64_t>(a.NB, 1);
-  // (rates of the 64-row kernel's windows, see Planner::plan_of)
-  const double fixed = a.mx4 ? 11.0 : a.fp8 ? 9.4 : 8.2, block = a.fp8 || a.mx4 ? 2.3 : 1.85;
+  // Times of a work item's fixed part and of a block, as in Planner::plan_of, but the
+  // 64-row tiles' with the chip full of long items: 64 requests of 128 rows behind 256
+  // blocks take 319 us in two splits of them, 274 in four of 128-row ones.
+  auto fixed = [&](int rg) { return rg == 2 ? 14.0 : a.mx4 ? 11.0 : a.fp8 ? 9.4 : 8.2; };
+  auto block = [&](int rg) { return rg == 2 ? (a.fp8 ? 4.16 : 3.27) : a.fp8 || a.mx4 ? 2.4 : 2.15; };
+  auto share = [&](int64_t n, int64_t S) { return 0.5 * (double)up(2 * n, S); };  // (splits are cut by half blocks)
   // What the launch takes: prefix items go out first, one to a compute unit at a time,
   // the requests' own where compute units come free.
   auto span = [&](int64_t n, double p, int64_t m, double o) {
@@ -330,14 +340,17 @@ inline PrefixPlan plan_prefix(const PrefixArgs& a) {
     const int64_t beside = free * (int64_t)(p / o);
     return m <= beside ? base + p : base + p + (double)up(m - beside, a.cus) * o;
   };
-  auto offer = [&](int64_t S, int64_t T) {
+  auto offer = [&](int rg, int64_t S, int64_t T) {
     S = std::max<int64_t>({1, up(a.NBP, cap), a.n_splits ? std::min<int64_t>(a.n_splits, nbp) : std::min(S, nbp)});
     T = std::max<int64_t>({1, up(a.NB, cap), a.own_splits ? std::min<int64_t>(a.own_splits, nb) : std::min(T, nb)});
     const uint64_t rows = (uint64_t)(S + T) * a.B * a.rows;
     const bool half = rows * kDLat * 4 >= kWsHalfMinBytes;
-    PrefixPlan c = q;
-    c.us = span(q.tiles * S, fixed + block * (double)up(nbp, S), own * T, fixed + block * (double)up(nb, T)) +
-           0.4e-6 * (double)(rows * kDLat * (half ? 2 : 4)) + (S + T > 16 ? 0.2 * (double)(S + T - 16) : 0.0);
+    PrefixPlan c = shape(rg);
+    // (a row's splits come in one trip up to 16 of them: 4 requests of 16 rows behind 32
+    // blocks take 17.1 us in 12 + 2 splits, 18.7 in 16 + 4)
+    c.us = span(c.tiles * S, fixed(rg) + block(rg) * share(nbp, S), a.B * c.own_tiles * T,
+                fixed(rg) + block(rg) * share(nb, T)) +
+           0.4e-6 * (double)(rows * kDLat * (half ? 2 : 4)) + (S + T > 16 ? 1.5 + 0.2 * (double)(S + T - 16) : 0.0);
     if (q.S != 0 && c.us >= q.us) return;
     c.S = S;
     c.own_S = T;
@@ -345,14 +358,19 @@ inline PrefixPlan plan_prefix(const PrefixArgs& a) {
     c.ws_bytes = rows * (kDLat * (half ? 2 : 4) + 3 * 4);
     q = c;
   };
-  static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
-  for (int64_t T = 1; T == 1 || (T <= a.NB && own * T <= 2 * a.cus); T *= 2) {
-    for (int64_t S : kCounts)
-      if (S == 1 || (S <= nbp && q.tiles * S <= 3 * a.cus)) offer(S, T);
-    for (int waves = 1; waves <= 4; ++waves) offer(std::max<int64_t>(1, waves * a.cus / q.tiles), T);
+  static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 14, 16, 20, 24, 32, 48, 64};
+  for (int rg = 1; rg <= (a.mx4 ? 1 : 2); ++rg) {
+    // (tiles of 128 rows where there are as many)
+    if (a.row_tile ? a.row_tile != 64 * rg : rg == 2 && a.rows < 128) continue;
+    const int64_t tiles = shape(rg).tiles, own = a.B * shape(rg).own_tiles;
+    for (int64_t T = 1; T == 1 || (T <= a.NB && own * T <= 2 * a.cus); T *= 2) {
+      for (int64_t S : kCounts)
+        if (S == 1 || (S <= nbp && tiles * S <= 3 * a.cus)) offer(rg, S, T);
+      for (int waves = 1; waves <= 4; ++waves) offer(rg, std::max<int64_t>(1, waves * a.cus / tiles), T);
+    }
   }
   q.prefix_grid = up(q.tiles * q.S, 8) * 8;
-  q.own_items = own * q.own_S;
+  q.own_items = a.B * q.own_tiles * q.own_S;
   q.grid = q.prefix_grid + q.own_items;
   return q;
 }

@@ -101,8 +101,8 @@ class ScoresOpts(ctypes.Structure):
 
 
 class PrefixOpts(ctypes.Structure):
-    _fields_ = [("n_splits", ctypes.c_int32), ("own_splits", ctypes.c_int32),
-                ("out_format", ctypes.c_int32), ("reserved", ctypes.c_int32 * 5)]
+    _fields_ = [("n_splits", ctypes.c_int32), ("own_splits", ctypes.c_int32), ("out_format", ctypes.c_int32),
+                ("row_tile", ctypes.c_int32), ("reserved", ctypes.c_int32 * 4)]
 
 
 class RopeOpts(ctypes.Structure):
@@ -403,13 +403,13 @@ def window_attn(q_lat, q_pe, ckv_pool, kpe_pool, block_table, seq_lens, scale, w
 
 def prepare_prefix(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table,
                    seq_lens, scale, q_lens=None, out_lat=None, out_lse=None, ckv_scale=None,
-                   kpe_scale=None, n_splits=0, own_splits=0, stream=None, wire=False):
+                   kpe_scale=None, n_splits=0, own_splits=0, stream=None, wire=False, row_tile=0):
     """prefix_attn with every argument fixed (see prepare_partial)."""
     out = _attn_outputs(block_table.shape[0], q_lat, out_lat, out_lse, wire)
     keep = (q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table, seq_lens,
             q_lens, ckv_scale, kpe_scale)
     dev = _on_current_gpu(*keep, *out, stream=stream)
-    o = PrefixOpts(int(n_splits), int(own_splits), OUT_BF16_WIRE if wire else OUT_FP32)
+    o = PrefixOpts(int(n_splits), int(own_splits), OUT_BF16_WIRE if wire else OUT_FP32, int(row_tile))
     d = (describe(q_lat), describe(q_pe), _describe_latent(ckv_pool, ckv_scale), describe(kpe_pool, kpe_scale),
          *[describe(t) for t in keep[4:10]])
     do = tuple(describe(t) for t in out)
@@ -420,7 +420,7 @@ def prepare_prefix(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, g
 
 def prefix_attn(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts, block_table,
                 seq_lens, scale, q_lens=None, out_lat=None, out_lse=None, ckv_scale=None, kpe_scale=None,
-                n_splits=0, own_splits=0, stream=None, wire=False):
+                n_splits=0, own_splits=0, stream=None, wire=False, row_tile=0):
     """Attention of each request's rows over the prefix that its group shares
     (prefix_table [G, NBP], prefix_lens [G]; group g is the requests
     group_starts[g] .. group_starts[g + 1] - 1), read once for all of them, and
@@ -428,7 +428,7 @@ def prefix_attn(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, grou
     window_attn, causal).  Pools and results as there."""
     return prepare_prefix(q_lat, q_pe, ckv_pool, kpe_pool, prefix_table, prefix_lens, group_starts,
                           block_table, seq_lens, scale, q_lens, out_lat, out_lse, ckv_scale, kpe_scale,
-                          n_splits, own_splits, stream, wire)()
+                          n_splits, own_splits, stream, wire, row_tile)()
 
 
 def prepare_block_means(ckv_pool, kpe_pool, slots, means, ckv_scale=None, kpe_scale=None, stream=None):

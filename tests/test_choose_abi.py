@@ -22,7 +22,7 @@ def opts(cls, **kw):
     o = cls()
     for k, v in kw.items():
         if k == "reserved":
-            o.reserved[4] = v
+            o.reserved[3] = v
         else:
             setattr(o, k, v)
     return o
@@ -250,6 +250,9 @@ PREFIX = [
     ("n_splits", dict(opts=opts(mla.PrefixOpts, n_splits=-1)), INVALID, "n_splits"),
     ("own_splits", dict(opts=opts(mla.PrefixOpts, own_splits=-1)), INVALID, "own_splits"),
     ("out_format", dict(opts=opts(mla.PrefixOpts, out_format=2)), INVALID, "out_format"),
+    ("row_tile", dict(opts=opts(mla.PrefixOpts, row_tile=96)), INVALID, "row_tile"),
+    ("128 rows of a 4-bit cache", dict(ckv=z(8, 64, 272, dt=U8), opts=opts(mla.PrefixOpts, row_tile=128)), UNSUPPORTED,
+     "64-row"),
     ("reserved", dict(opts=opts(mla.PrefixOpts, reserved=1)), INVALID, "reserved"),
     ("groups", dict(ptable=z(4097, 6, dt=I32), plens=z(4097, dt=I32), starts=z(4098, dt=I32)), UNSUPPORTED, "4096"),
 ]

@@ -71,12 +71,29 @@ def test_one_group(kv, H):
 
 @pytest.mark.parametrize("kv", T.KVS)
 @pytest.mark.parametrize("wire", [False, True])
-def test_groups_of_any_size(kv, wire):
+@pytest.mark.parametrize("row_tile", [64, 128])
+def test_groups_of_any_size(kv, wire, row_tile):
     """Groups of none, one and several requests, whose rows end inside tiles; rows
     that see nothing but the prefix, nothing but their own, nothing at all."""
-    print(f"case: groups {kv} {wire}", flush=True)
+    print(f"case: groups {kv} {wire} {row_tile}", flush=True)
     a = Case(7, 9, 3, 11, [0, 0, 4, 5, 5, 9, 9], 4, 3, kv)
-    a.check([256, 100, 0, 7, 64, 1], [3, 192, 0, 77, 1, 0, 2, 130, 64], [3, 2, 0, 1, 3, 3, 1, 0, 2], wire=wire)
+    args = [256, 100, 0, 7, 64, 1], [3, 192, 0, 77, 1, 0, 2, 130, 64], [3, 2, 0, 1, 3, 3, 1, 0, 2]
+    if kv == "mx4" and row_tile == 128:
+        with pytest.raises(mla.MlaError, match="64-row"):
+            a.run(*args, wire=wire, row_tile=128)
+        return
+    a.check(*args, wire=wire, row_tile=row_tile)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "fp8split"])
+@pytest.mark.parametrize("B,Mq,H,starts", [(4, 1, 128, [0, 1, 4]), (3, 2, 128, [0, 0, 3]), (5, 1, 100, [0, 2, 5]),
+                                           (2, 3, 64, [0, 1, 2]), (9, 1, 300, [0, 4, 9])])
+def test_tiles_of_128_rows(kv, B, Mq, H, starts):
+    print(f"case: 128 rows {kv} {B} {Mq} {H} {starts}", flush=True)
+    a = Case(B + H, B, Mq, H, starts, 6, 3, kv)
+    lens = np.random.default_rng(H).integers(0, 193, B)
+    for n_splits, own_splits in ((0, 0), (1, 1), (5, 3)):
+        a.check([384, 200], lens, row_tile=128, n_splits=n_splits, own_splits=own_splits)
 
 
 @pytest.mark.parametrize("n_splits,own_splits", [(1, 1), (2, 1), (7, 3), (30, 30), (0, 2), (5, 0)])
@@ -84,7 +101,8 @@ def test_groups_of_any_size(kv, wire):
 def test_splits(kv, n_splits, own_splits):
     print(f"case: splits {kv} {n_splits} {own_splits}", flush=True)
     a = Case(3, 4, 2, 20, [0, 1, 4], 11, 5, kv)
-    a.check([700, 390], [320, 33, 200, 2], n_splits=n_splits, own_splits=own_splits)
+    for row_tile in (64, 64 if kv == "mx4" else 128):
+        a.check([700, 390], [320, 33, 200, 2], n_splits=n_splits, own_splits=own_splits, row_tile=row_tile)
 
 
 @pytest.mark.parametrize("plen", [0, 1, 31, 32, 33, 63, 64, 65, 128])
