@@ -386,7 +386,7 @@ typedef struct {
  * not detected: rows of the batch may then come out undefined.  One launch for
  * prefixes and own tokens, one that joins them; the workspace, its limits and graph
  * capture as in mla_sparse_partial_attn (nothing to fall back on where it cannot
- * grow).  G at most 4096, B Mq H less than 2^30, tables less than 2^25 blocks wide
+ * grow).  G at most 4096, B Mq H less than 2^26, tables less than 2^25 blocks wide
  * (MLA_ERR_UNSUPPORTED). */
 mla_status_t mla_prefix_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
                              const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
@@ -643,7 +643,8 @@ typedef struct {
  * sums fp32; a logit of a row and block it may choose that is NaN or +inf makes all
  * its scores NaN.  Splits leave two floats a row and split in the workspace of
  * mla_sparse_partial_attn; where that cannot grow (graph capture) the call takes
- * one split.  NB less than 2^25 blocks, Mq x H at most 2^24 (MLA_ERR_UNSUPPORTED). */
+ * one split.  NB less than 2^25 blocks, Mq x H at most 2^24, B times the groups of
+ * 128 rows of a request (heads padded to 16) at most 2^22 (MLA_ERR_UNSUPPORTED). */
 mla_status_t mla_block_scores(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
                               const mla_tensor_t* means, const mla_tensor_t* block_table,
                               const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,

@@ -526,7 +526,7 @@ mla_status_t prefix_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   if (!(std::fabs(scale) <= 18446744073709551616.0f)) return bad("scale must be finite with |scale| <= 2^64");
   if (G > 4096) return fail(MLA_ERR_UNSUPPORTED, "more than 4096 groups");
   if (B > INT32_MAX || Mq * H > (1 << 24) || NB > (INT32_MAX >> 6) || NBP > (INT32_MAX >> 6) || P > (INT32_MAX >> 1) ||
-      B * Mq * H >= (1 << 30))
+      B * Mq * H >= (1 << 26))
     return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the int32 index range");
   const Extent outs[2] = {extent(*out_lat), extent(*out_lse)};
   const bool fp8 = ckv_pool->dtype == MLA_DTYPE_FP8_E4M3FN, mx4 = ckv_pool->dtype == MLA_DTYPE_MXFP4;

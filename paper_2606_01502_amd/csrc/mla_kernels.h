@@ -288,6 +288,7 @@ struct TopkParams {
   int32_t* ids;
   int64_t x_s0, x_s1, ids_s0, ids_s1;  // element strides over (request, Mq)
   int64_t rows;
+  int64_t first_row;      // of a launch (set by it)
   int32_t N, K;
   Div by_Mq;
   int32_t Mq;

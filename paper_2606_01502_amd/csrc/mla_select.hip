@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "mla_kernels.h"
@@ -669,7 +670,7 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
   __shared__ int n_taken;
   __shared__ int found;
   __shared__ uint32_t left, in_bin;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.first_row + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
   const int first = (int)blockIdx.y * (THREADS * E), N = min(p.N - first, THREADS * E);
@@ -800,7 +801,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
   __shared__ int wave_above[kTopThreads / 64], wave_equal[kTopThreads / 64];
   __shared__ int found;
   __shared__ uint32_t left, in_bin;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.first_row + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
   const float* const x = p.x + b * p.x_s0 + i * p.x_s1;
@@ -894,9 +895,8 @@ hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_topk(const TopkParams& p, int pieces, hipStream_t s) {
-  if (p.rows <= 0) return hipSuccess;
-  const dim3 g((uint32_t)p.rows, (uint32_t)pieces);
+static hipError_t launch_topk_rows(const TopkParams& p, int64_t rows, int pieces, hipStream_t s) {
+  const dim3 g((uint32_t)rows, (uint32_t)pieces);
   if (pieces > 1) {
     static_assert(kTopPiece == 1024 * 8, "a piece of the kernel");
     hipLaunchKernelGGL((topk_kernel<1024, 8>), g, dim3(1024), 0, s, p);
@@ -915,6 +915,18 @@ hipError_t launch_topk(const TopkParams& p, int pieces, hipStream_t s) {
     hipLaunchKernelGGL(topk_row_kernel, g, dim3(kTopThreads), 0, s, p);
   }
   return hipGetLastError();
+}
+
+hipError_t launch_topk(const TopkParams& p0, int pieces, hipStream_t s) {
+  // one launch holds less than 2^32 threads (past that its size wraps, without an
+  // error): 2^31 at a time
+  TopkParams p = p0;
+  const int64_t most = std::max<int64_t>(1, (1 << 21) / pieces);
+  for (p.first_row = 0; p.first_row < p.rows; p.first_row += most) {
+    const hipError_t e = launch_topk_rows(p, std::min<int64_t>(most, p.rows - p.first_row), pieces, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace mla

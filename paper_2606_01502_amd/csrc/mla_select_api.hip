@@ -125,7 +125,9 @@ mla_status_t scores_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   const int64_t tiles = (NB + mla::kScoreCols - 1) / mla::kScoreCols, items = B * n_groups;
   int64_t S = opts->n_splits ? opts->n_splits : (device_cus() + items - 1) / items;
   S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
-  if (items * S > INT32_MAX) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
+  // (one launch holds less than 2^32 threads)
+  if (items > (1 << 22)) return fail(MLA_ERR_UNSUPPORTED, "grid too large");
+  S = std::min<int64_t>(S, (1 << 22) / items);
   p.shape = shape;
   p.row_chunks = (int32_t)C;
   p.group_rows = (int32_t)group_rows;

@@ -303,6 +303,31 @@ def test_binding_refuses_host_tensors():
         mla.select_topk(z(2, 9, dt=F32))
 
 
+@pytest.mark.parametrize("k", range(6))
+def test_tensors_and_streams_of_another_device(monkeypatch, k):
+    from tests.test_devices import Fake, Stream
+
+    def calls(on, stream=None):
+        def t(*shape):
+            return Fake(*shape, on=on)
+        q, qp, pool, kpool, table, lens = t(1, 1, 1, 512), t(1, 1, 1, 64), t(1, 64, 512), t(1, 64, 64), t(1, 1), t(1)
+        out, lse = t(1, 1, 1, 512), t(1, 1, 1)
+        return [
+            lambda: mla.rope_append(t(1, 512), t(1, 64), lens, lens, pool, kpool, stream=stream),
+            lambda: mla.block_means(pool, kpool, lens, t(1, 576), stream=stream),
+            lambda: mla.block_scores(q, qp, t(1, 576), table, lens, 1.0, scores=t(1, 1, 1), stream=stream),
+            lambda: mla.select_topk(t(1, 5), ids=t(1, 3), stream=stream),
+            lambda: mla.prefix_attn(q, qp, pool, kpool, table, lens, t(2), table, lens, 1.0, out_lat=out, out_lse=lse,
+                                    stream=stream),
+            lambda: mla.prepare_prefix(q, qp, pool, kpool, table, lens, t(2), table, lens, 1.0, out_lat=out,
+                                       out_lse=lse, stream=stream)]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="cuda:1, which is not the current device"):
+        calls(1)[k]()
+    with pytest.raises(ValueError, match="the stream is on cuda:1"):
+        calls(0, Stream(1))[k]()
+
+
 # ---- the references
 def test_scores_reference_is_the_shares_of_attention():
     """Scores of a row sum to the number of heads; blocks of one key repeated

@@ -303,6 +303,15 @@ def test_topk_of_long_rows_captured_without_a_workspace():
             s.synchronize()
 
 
+def test_topk_of_more_rows_than_a_launch_holds():
+    """2^21 rows a launch: the rows on either side of the border and the last ones."""
+    n = (1 << 21) + 1000
+    x = torch.rand((n, 6), device="cuda")
+    got = mla.select_topk(x, 2)
+    want = torch.sort(torch.sort(x, dim=-1, descending=True, stable=True).indices[:, :2], dim=-1).values
+    assert torch.equal(got.long(), want)
+
+
 def test_topk_strided_rows_and_given_ids():
     x = torch.randn((3, 5, 90), device="cuda")
     ids = torch.full((3, 5, 20), 9, dtype=torch.int32, device="cuda")

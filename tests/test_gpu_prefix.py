@@ -111,6 +111,17 @@ def test_prefix_lengths(plen):
     a.check([plen], [1, 64])
 
 
+@pytest.mark.parametrize("row_tile", [64, 128])
+def test_tables_of_no_blocks(row_tile):
+    """No prefix, or nothing of the requests' own: neither is read."""
+    a = Case(17, 3, 2, 16, [0, 1, 3], 2, 2)
+    a.table = a.table[:, :0]
+    a.check([100, 128], [70, 2, 0], row_tile=row_tile)
+    a = Case(18, 3, 2, 16, [0, 1, 3], 2, 2)
+    a.ptable = a.ptable[:, :0]
+    a.check([100, 128], [70, 2, 0], row_tile=row_tile)
+
+
 def test_lengths_past_the_tables_and_below_zero():
     a = Case(5, 3, 2, 8, [0, 2, 3], 2, 1)
     a.check([1000, -7], [100, -3, 64], [2, 2, 5])
