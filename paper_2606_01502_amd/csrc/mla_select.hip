@@ -589,9 +589,8 @@ __global__ __launch_bounds__(kScoreThreads, 2) void scores_kernel(const ScoresPa
 //
 // Values are ordered as 32-bit keys that grow with them (NaN above all, -0 as 0).  A
 // workgroup holds a row's keys in registers and narrows down the range in which the
-// K-th largest lies: a histogram of the keys in the range over 256 bins (an eighth of
-// the range's bits at a time, so that the bins follow the values there are), then the
-// bin that holds it.  All keys above the range are then taken, and those in it where
+// K-th largest lies: a histogram of the keys in the range (the upper bits of where in it
+// they lie, so that the bins follow the values there are), then the bin that holds it.  All keys above the range are then taken, and those in it where
 // it comes down to one key, the first ones in the order of their places.  -inf is
 // never taken.
 //
@@ -604,8 +603,6 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 constexpr uint32_t kLowestKey = 0x007FFFFFu;  // of -inf
-constexpr int kBins = 256;
-
 // op over a wave, in every lane: by rotations within 16 lanes, then by the row swaps.
 template <class Op>
 __device__ __forceinline__ uint32_t over_wave(uint32_t v, Op op) {
@@ -633,25 +630,40 @@ __device__ __forceinline__ int lanes_up(int v) {
   return v;
 }
 
-// Of a histogram of `bins`, the bin that holds the `want`-th key from the top, and how
-// many of the wanted lie in it (by the first wave; want <= the number of keys).
+// Of a histogram, the bin that holds the `want`-th key from the top, and how many of the
+// wanted lie in it (by the first wave; want <= the number of keys).
+template <int BINS>
 __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, int lane, int* bin, uint32_t* left,
                                          uint32_t* in_bin) {
-  // lane l holds bins 255 - 4 l .. 252 - 4 l, from the top
-  uint32_t c[4], sum = 0;
+  // lane l holds the l-th BINS / 64 bins from the top, the lowest first
+  constexpr int kPer = BINS / 64;
+  const u32x4_t* const at = (const u32x4_t*)(hist + BINS - kPer * (lane + 1));
+  u32x4_t c[kPer / 4];
+  uint32_t sum = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    c[j] = hist[kBins - 1 - 4 * lane - j];
-    sum += c[j];
+  for (int j = 0; j < kPer / 4; ++j) {
+    c[j] = at[j];
+    sum += (c[j][0] + c[j][1]) + (c[j][2] + c[j][3]);
   }
   uint32_t past = (uint32_t)lanes_up((int)sum) - sum;  // in the bins above the lane's
   const uint64_t few = __ballot(past < want);
   if (lane == 63 - __builtin_clzll(few)) {  // the last lane with fewer than `want` above it
-    int j = 0;
-    while (j < 3 && past + c[j] < want) past += c[j++];
-    *bin = kBins - 1 - 4 * lane - j;
+    int b = kPer - 1;
+    uint32_t here = 0;
+#pragma unroll
+    for (int j = kPer - 1; j >= 0; --j) {
+      const uint32_t n = c[j / 4][j % 4];
+      if (j == b) {
+        here = n;
+        if (j > 0 && past + n < want) {
+          past += n;
+          b = j - 1;
+        }
+      }
+    }
+    *bin = BINS - kPer * (lane + 1) + b;
     *left = want - past;
-    *in_bin = c[j];
+    *in_bin = here;
   }
 }
 
@@ -661,8 +673,10 @@ __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, in
 // more than K can be among the row's K best.
 template <int THREADS, int E>
 __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
-  constexpr int kWaves = THREADS / 64;
-  __shared__ uint32_t hist[2][kBins];
+  // (bins: of a range over both signs and all exponents 1024 still tell eight values of an
+  // exponent apart; few threads clear and search 256 faster)
+  constexpr int kWaves = THREADS / 64, kBits = THREADS > 256 ? 10 : 8, kBins = 1 << kBits;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[2][kBins];
   __shared__ uint32_t wave_lo[kWaves], wave_hi[kWaves];
   __shared__ int wave_n[kWaves];
   // of 64 neighbours: (above, equal << 16), then the places taken before them; equal ones before them
@@ -721,12 +735,12 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
     want = 0;
   }
   for (int turn = 0; lo < hi; turn ^= 1) {
-    const int bits = 32 - __builtin_clz(hi - lo), shift = max(bits - 8, 0);
+    const int bits = 32 - __builtin_clz(hi - lo), shift = max(bits - kBits, 0);
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (key[e] >= lo && key[e] <= hi) atomicAdd(&hist[turn][(key[e] - lo) >> shift], 1u);
     __syncthreads();
-    if (wave == 0) find_bin(hist[turn], want, lane, &found, &left, &in_bin);
+    if (wave == 0) find_bin<kBins>(hist[turn], want, lane, &found, &left, &in_bin);
     for (int t = tid; t < kBins; t += THREADS) hist[turn ^ 1][t] = 0;
     __syncthreads();
     want = left;
@@ -797,7 +811,8 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
 // found before.
 constexpr int kTopThreads = 1024;
 __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams p) {
-  __shared__ uint32_t hist[kBins];
+  constexpr int kBins = 256;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
   __shared__ int wave_above[kTopThreads / 64], wave_equal[kTopThreads / 64];
   __shared__ int found;
   __shared__ uint32_t left, in_bin;
@@ -816,7 +831,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
       if (shift == 24 || k >> (shift + 8) == top >> (shift + 8)) atomicAdd(&hist[k >> shift & 255], 1u);
     }
     __syncthreads();
-    if (wave == 0) find_bin(hist, (uint32_t)want, lane, &found, &left, &in_bin);
+    if (wave == 0) find_bin<kBins>(hist, (uint32_t)want, lane, &found, &left, &in_bin);
     __syncthreads();
     top |= (uint32_t)found << shift;
     want = (int)left;
@@ -898,14 +913,16 @@ hipError_t launch_scores(const ScoresParams& p, int B, hipStream_t s) {
 static hipError_t launch_topk_rows(const TopkParams& p, int64_t rows, int pieces, hipStream_t s) {
   const dim3 g((uint32_t)rows, (uint32_t)pieces);
   if (pieces > 1) {
-    static_assert(kTopPiece == 1024 * 8, "a piece of the kernel");
-    hipLaunchKernelGGL((topk_kernel<1024, 8>), g, dim3(1024), 0, s, p);
+    static_assert(kTopPiece == 512 * 16, "a piece of the kernel");
+    hipLaunchKernelGGL((topk_kernel<512, 16>), g, dim3(512), 0, s, p);
   } else if (p.N <= 256) {
     hipLaunchKernelGGL((topk_kernel<64, 4>), g, dim3(64), 0, s, p);
   } else if (p.N <= 1024) {
     hipLaunchKernelGGL((topk_kernel<256, 4>), g, dim3(256), 0, s, p);
   } else if (p.N <= 4096) {
     hipLaunchKernelGGL((topk_kernel<512, 8>), g, dim3(512), 0, s, p);
+  } else if (p.N <= 8192) {
+    hipLaunchKernelGGL((topk_kernel<512, 16>), g, dim3(512), 0, s, p);
   } else if (p.N <= 16384) {
     hipLaunchKernelGGL((topk_kernel<1024, 16>), g, dim3(1024), 0, s, p);
   } else if (p.N <= kTopMost) {
