@@ -51,9 +51,11 @@ __device__ __forceinline__ uint32_t to_codes(u32x4_t v, float s) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2_t, w3), s, 3);
 }
 
-// ROPE: the RoPE part of a token, two tokens to a wave, a pair of its dims to a lane:
-// lane l < rot / 2 of a half turns its pair (see mla_rope.hip: the same products and
-// one rounding), the others copy what is not turned.
+// With RopeAppendParams the RoPE part is turned on the way, two tokens to a wave, a pair
+// of its dims to a lane: lane l < rot / 2 of a half turns its pair (see mla_rope.hip: the
+// angle reduced in fp64, fp32 products, one rounding), the others copy what is not
+// turned.  30,001 tokens take 12.8 us (69 MB, 5.4 TB/s, a copy's rate), where cache_append
+// of tokens turned before takes 11.2; 64 take 4.3.
 struct RopeLane {
   int c0, c1;      // the lane's columns
   double turns;    // of its pair a position (0: copied)

@@ -7,8 +7,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "mla_kernels.h"
 #include "mla_mx4.h"
+#include "mla_select.h"
 
 namespace mla {
 namespace {
@@ -32,7 +32,9 @@ __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(
 // there in their order, so that each has its part both of a prompt's tokens, every
 // 64th of which ends a block, and of a list of ends.  A block's 18 loads a thread are
 // all out before the first sum: a stream through HBM, bound by the launch and two
-// trips where few blocks are whole.
+// trips where few blocks are whole.  100,003 tokens that complete 1562 fp8 blocks (58
+// MB) take 16.1 us, 3.7 TB/s (20.9 with every n-th slot to a workgroup, which gave some
+// of them three blocks and others none); 128 tokens that complete two 3.6.
 constexpr int kMeanCols = kDLat + kDPe;
 
 // Adds the eight bf16 of v to a.
@@ -192,12 +194,20 @@ __global__ __launch_bounds__(kThreads) void means_kernel(const MeansParams p) {
 // is one split).  Logits kept between the passes would move 8 bytes a head and
 // block, the keys again 1152 a block for all heads, mostly out of the caches.
 //
-// A workgroup takes a tile of blocks at a time in LDS, the next tile's keys on their
-// way (direct-to-LDS loads); its waves share out 16-row chunks (the heads of one query row,
-// padded) and the tile's columns of 16 blocks.  bf16 MFMA 16x16x32 with the query
-// rows in registers for the whole kernel.  128 rows a workgroup where there are as
-// many, and two workgroups a compute unit: one's loads and exponentials run beside the
-// other's products.
+// A workgroup of eight waves, two on a SIMD, takes 64 blocks at a time in LDS, the next
+// 64's keys on their way (direct-to-LDS loads spread over the products); its waves share
+// out 16-row chunks (the heads of one query row, padded) and the columns of 16 blocks.
+// bf16 MFMA 16x16x32 with the query rows in registers for the whole kernel, fp32 sums.
+//
+// What bounds it: for decode rows the keys out of HBM and the chain before the first
+// tile, in each of two launches (64 requests of 128 rows over 1024 blocks, 84 MB a pass:
+// 36 us, of which 18 a pass in one tile's chain and 3.4 tiles at 1.3 to 2); for prompts a
+// tile's 2 us, 1.1 of them products, the rest LDS (each wave reads its columns' keys for
+// 32 rows only) and exponentials.  From there: the table's entry read under a condition
+// was waited for in every tile, and query rows taken from memory as the products need
+// them (64 bytes of 16 rows a load) cost 7 us a launch: 49 us with both.  Four waves with
+// the exponentials of a tile beside the next one's products took 101 us where eight plain
+// ones take 69 (one split).
 constexpr int kKeyBytes = 2 * kMeanCols;       // 1152: 72 chunks of 16 bytes
 constexpr int kSteps = kMeanCols / 32;         // of a product: 18
 
@@ -594,8 +604,11 @@ __global__ __launch_bounds__(kScoreThreads, 2) void scores_kernel(const ScoresPa
 // it comes down to one key, the first ones in the order of their places.  -inf is
 // never taken.
 //
-// Read once, written once; few rows are bound by the launch and by the dependent
-// steps of the search.
+// Read once, written once; bound by the launch and by the dependent steps of the search:
+// 64 rows of 1024 values take 4.3 us, one of 8192 8.7, of 16,384 11.7.  A search bit by
+// bit over a wave's registers took 10.1 us for 64 rows of 1024, one that reads the row
+// again for each byte of the key 111 for 32 of 65,536, which now go in eight pieces of
+// 8192 and then in one row of 16,384: 22 us.
 
 __device__ __forceinline__ uint32_t order_key(float v) {
   if (v != v) return 0xFFFFFFFFu;

@@ -10,7 +10,7 @@
 
 #include "../../include/mla_sparse.h"
 #include "mla_host.h"
-#include "mla_kernels.h"
+#include "mla_select.h"
 
 using namespace mla::host;
 
@@ -122,6 +122,8 @@ mla_status_t scores_call(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe, co
   const int64_t slots = mla::kScoreChunksOf[shape];
   const int64_t group_rows = C >= slots ? 1 : std::min<int64_t>(Mq, slots / C);
   const int64_t n_groups = (Mq + group_rows - 1) / group_rows;
+  // one workgroup a compute unit, which it fills (64 x 128 rows over 1024 blocks: 69 us in
+  // one split, 46 in two, 36 in four, 51 in six)
   const int64_t tiles = (NB + mla::kScoreCols - 1) / mla::kScoreCols, items = B * n_groups;
   int64_t S = opts->n_splits ? opts->n_splits : (device_cus() + items - 1) / items;
   S = std::max<int64_t>(1, std::min<int64_t>(S, tiles));
