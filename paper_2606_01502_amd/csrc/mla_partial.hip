@@ -48,8 +48,10 @@
 // at a time into the same stage layout, each with its own block's fp8
 // scales; or no list but positions (kSelWindow): the rows are the last tokens
 // of sequences, each sees the tokens of its window and the first few, and a
-// tile reads the blocks that any of its rows sees.  Splits of a workspace of a megabyte or more store their rows as
-// fp16 scaled by the row's largest magnitude.
+// tile reads the blocks that any of its rows sees; or (kSelPrefix) a prefix that
+// all requests of a group see, whose tiles hold the rows of all of them, and
+// beside those each request's own tokens.  Splits of a workspace of a megabyte
+// or more store their rows as fp16 scaled by the row's largest magnitude.
 //
 // 4-bit caches (64-row tiles only): 272 bytes of E2M1 codes and exponents a
 // token, converted to bf16 on the way from one LDS ring to another, exactly,
@@ -802,7 +804,17 @@ __device__ __forceinline__ Window window_of(const PartialParams& p, int len, int
 }
 
 // Shared prefixes (kSelPrefix): jobs are groups, whose rows are those of all requests
-// of a group, next to each other, and requests, over what they have of their own.
+// of a group, next to each other, and requests, over what they have of their own.  A
+// row's softmax is a sum over both kinds of tokens, so every split of either leaves a
+// row in the workspace, and one combine joins them: rows lie there split by split, each
+// with all rows of the batch, in whose numbers a group's are one range.
+//
+// Bound by the products: a prefix block's 72 KiB serve 64 or 128 rows a workgroup and
+// meet in the L2 of the XCDs that hold its splits.  64 requests of 128 rows behind 256
+// blocks, with 1 to 8 of their own, take 272 us (282 GFLOP, 1.04 PFLOP/s) in 128-row
+// tiles, 319 in 64-row ones; 40 x 3 x 32 rows in five groups behind 200 fp8 blocks 166.
+// A tile more than the rows fill, as groups that start inside tiles need, gave one XCD
+// 33 work items for its 32 compute units where there was none to need: 540 us.
 struct PrefixItem {
   bool prefix;
   int job;              // group, or request
