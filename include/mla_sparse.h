@@ -660,8 +660,8 @@ mla_status_t mla_block_scores(const mla_tensor_t* q_lat, const mla_tensor_t* q_p
  *                                     rising order; of equal ones the first are
  *                                     taken; -inf is never taken: -1 follows the
  *                                     last place of a row that has fewer than K
- * NaN ranks above all other values, -0 equals 0.  N and K may be any size (K more
- * than N too); at most 2^29 rows (MLA_ERR_UNSUPPORTED). */
+ * NaN ranks above all other values, -0 equals 0.  N and K up to 2^31 - 4097 (K more
+ * than N too), at most 2^29 rows; more of either is MLA_ERR_UNSUPPORTED. */
 mla_status_t mla_select_topk(const mla_tensor_t* scores, const mla_tensor_t* ids, void* stream);
 
 /*

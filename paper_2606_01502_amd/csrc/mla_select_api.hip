@@ -165,7 +165,7 @@ mla_status_t topk_call(const mla_tensor_t* scores, const mla_tensor_t* ids, void
   if (overlaps(extent(*ids), extent(*scores))) return bad("an output overlaps an input");
   const int64_t B = scores->shape[0], Mq = nd == 3 ? scores->shape[1] : 1;
   const int64_t N = scores->shape[nd - 1], K = ids->shape[nd - 1];
-  if (B > INT32_MAX || Mq > INT32_MAX || N > INT32_MAX - 4096 || K > INT32_MAX || B * Mq > INT32_MAX / 4)
+  if (B > INT32_MAX || Mq > INT32_MAX || N > INT32_MAX - 4096 || K > INT32_MAX - 4096 || B * Mq > INT32_MAX / 4)
     return fail(MLA_ERR_UNSUPPORTED, "sizes beyond the int32 index range");
   if (B * Mq == 0 || K == 0) return MLA_OK;
   mla::TopkParams p{};

@@ -207,6 +207,15 @@ def test_topk_overlap_and_size_refused():
     assert st == UNSUPPORTED and "index range" in msg
 
 
+def test_topk_more_places_than_an_index_refused():
+    """Places past a row's values are filled 1024 at a time: K within that of 2^31 would wrap."""
+    x, ids = mla.describe(z(1, 4, dt=F32)), mla.describe(z(1, 1, dt=I32))
+    ids.shape[1] = ids.stride[0] = (1 << 31) - 1
+    ids.data += 1 << 40
+    st, msg = answer("mla_select_topk", ctypes.byref(x), ctypes.byref(ids), None)
+    assert st == UNSUPPORTED and "index range" in msg
+
+
 # ---- prefix_attn
 def prefix_args(kv="bf16", wire=False):
     row, dt = (272 if kv == "mx4" else 512), (BF16 if kv == "bf16" else U8)
