@@ -821,7 +821,8 @@ __global__ __launch_bounds__(THREADS) void topk_kernel(const TopkParams p) {
 
 // A row of any length by one workgroup, read from memory in each round: eight bits
 // of the K-th largest key a round, by a histogram of the values that share the bits
-// found before.
+// found before.  Rows that went in pieces come here too, where they are still longer
+// than the kernel above holds.
 constexpr int kTopThreads = 1024;
 __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams p) {
   constexpr int kBins = 256;
@@ -833,6 +834,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = div_by((int)row, p.by_Mq), i = row - b * p.Mq;
   const float* const x = p.x + b * p.x_s0 + i * p.x_s1;
+  const int32_t* const places = p.places ? p.places + row * p.N : nullptr;
   int32_t* const ids = p.ids + b * p.ids_s0 + i * p.ids_s1;
   uint32_t top = 0;
   int want = min(p.K, p.N);  // of the values that share top's bits so far, so many are taken
@@ -878,7 +880,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_row_kernel(const TopkParams 
     // places taken before this one: those above, and of those equal at most `want`
     const int eq_before = q0 + (int)__popcll(eq & before);
     const bool take = k > top || (k == top && eq_before < want);
-    if (take) ids[at + a0 + (int)__popcll(gt & before) + min(eq_before, want)] = e;
+    if (take) ids[at + a0 + (int)__popcll(gt & before) + min(eq_before, want)] = places ? places[e] : e;
     at += an + min(qn, want);
     want -= min(qn, want);
     __syncthreads();
