@@ -274,6 +274,13 @@ constexpr int kSelWindow = 3;
 // A group's shared prefix, which all of its requests' rows see, and each request's own
 // tokens.
 constexpr int kSelPrefix = 4;
+// The last token that query row i sees of n_tok, the sequence's row 0 at token pos0:
+// min(pos0 + i, n_tok - 1) without that sum, which passes 2^31 where a group's rows
+// count up from the last token of a long prefix.
+__host__ __device__ constexpr int last_token(int pos0, int i, int n_tok) {
+  const int most = n_tok - 1 - pos0;
+  return pos0 + (i < most ? i : most);
+}
 // half blocks that one split of a window lists
 constexpr int kWindowList = kPerRowListShort;
 // Requests that splits are shared out between by length: four to a lane.

@@ -769,7 +769,7 @@ struct Window {
   int n_sink;
   int hi_all, lo_all;   // every row of the tile sees lo_all .. hi_all
   // of query row i: the last token it sees (-1: none), and the first in its window
-  __device__ __forceinline__ int hi_of(int i) const { return i < qn ? min(pos0 + i, n_tok - 1) : -1; }
+  __device__ __forceinline__ int hi_of(int i) const { return i < qn ? last_token(pos0, i, n_tok) : -1; }
   __device__ __forceinline__ int lo_of(int i) const {
     return window ? (int)max((int64_t)pos0 + i - window + 1, (int64_t)0) & lo_mask : 0;
   }
