@@ -616,8 +616,9 @@ mla_status_t mla_block_means(const mla_tensor_t* ckv_pool, const mla_tensor_t* k
 /* Options of mla_block_scores. */
 typedef struct {
   int32_t window;   /* the last tokens up to a row's own, which it attends anyway:
-                       as mla_window_attn's with whole_blocks (0: none but those
-                       of a block that is not whole yet)                         */
+                       from 1 on as mla_window_attn's with whole_blocks.  0: a row
+                       may choose all blocks that are whole at its position, which
+                       is not what 0 says there (all tokens are attended)        */
   int32_t n_sink;   /* first tokens of the sequence that every row attends anyway */
   int32_t n_splits; /* splits of a request's blocks (0 = automatic)               */
   int32_t reserved[5]; /* must be zero                                            */
@@ -637,14 +638,18 @@ typedef struct {
  * lies in [0, P): with s_hj = scale (q_lat,h . k_lat,j + q_pe,h . k_pe,j) and k_j the
  * block's mean key,
  *   scores[b, i, j] = sum over h of exp(s_hj) / sum over those j' of exp(s_hj'),
- * and -inf for every other block.  So with n_sink a multiple of 64 a row's choice
- * and what mla_window_attn with whole_blocks = 1 attends share no token, and cover
- * all if all are chosen.  Logits are bf16 products summed in fp32, weights and
- * sums fp32; a logit of a row and block it may choose that is NaN or +inf makes all
- * its scores NaN.  Splits leave two floats a row and split in the workspace of
- * mla_sparse_partial_attn; where that cannot grow (graph capture) the call takes
- * one split.  NB less than 2^25 blocks, Mq x H at most 2^24, B times the groups of
- * 128 rows of a request (heads padded to 16) at most 2^22 (MLA_ERR_UNSUPPORTED). */
+ * and -inf for every other block.  So with one window of at least 1 in both, and
+ * n_sink a multiple of 64, a row's choice and what mla_window_attn with whole_blocks =
+ * 1 attends share no token, and cover all if all are chosen.  With window 0 they do
+ * share: a row may choose every whole block up to its position, and mla_window_attn
+ * attends all tokens, so that a merge of the two counts the chosen ones twice (window
+ * 1 attends no more than the block of a row's own token).  Logits are bf16 products
+ * summed in fp32, weights and sums fp32; a logit of a row and block it may choose that
+ * is NaN or +inf makes all its scores NaN.  Splits leave two floats a row and split in
+ * the workspace of mla_sparse_partial_attn; where that cannot grow (graph capture) the
+ * call takes one split.  NB less than 2^25 blocks, Mq x H at most 2^24, B times the
+ * groups of 128 rows of a request (heads padded to 16) at most 2^22
+ * (MLA_ERR_UNSUPPORTED). */
 mla_status_t mla_block_scores(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
                               const mla_tensor_t* means, const mla_tensor_t* block_table,
                               const mla_tensor_t* seq_lens, const mla_tensor_t* q_lens, float scale,

@@ -465,8 +465,11 @@ def block_scores(q_lat, q_pe, means, block_table, seq_lens, scale, window=0, n_s
     query row: the share of its attention that each head would give a block if
     its keys were their mean (means [P, 576] of block_means), summed over the
     heads; -inf for blocks that are not whole, that the last `window` tokens
-    reach into (window_attn with whole_blocks attends those) or the first
-    n_sink.  For select_topk."""
+    reach into or the first n_sink.  For select_topk.  With the same window of
+    at least 1, and n_sink a multiple of 64, window_attn with whole_blocks
+    attends what may not be chosen; with window 0 all whole blocks may be
+    chosen, and window_attn attends all tokens: merged, the chosen ones would
+    count twice."""
     return prepare_block_scores(q_lat, q_pe, means, block_table, seq_lens, scale, window, n_sink, q_lens,
                                 scores, n_splits, stream)()
 
