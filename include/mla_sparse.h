@@ -646,8 +646,9 @@ typedef struct {
  * 1 attends no more than the block of a row's own token).  Logits are bf16 products
  * summed in fp32, weights and sums fp32; a logit of a row and block it may choose that
  * is NaN or +inf makes all its scores NaN.  Splits leave two floats a row and split in
- * the workspace of mla_sparse_partial_attn; where that cannot grow (graph capture) the
- * call takes one split.  NB less than 2^25 blocks, Mq x H at most 2^24, B times the
+ * the workspace of mla_sparse_partial_attn; where that cannot grow (graph capture) a
+ * call with n_splits 0 takes one split, and one that asks for several is refused
+ * (MLA_ERR_UNSUPPORTED).  NB less than 2^25 blocks, Mq x H at most 2^24, B times the
  * groups of 128 rows of a request (heads padded to 16) at most 2^22
  * (MLA_ERR_UNSUPPORTED). */
 mla_status_t mla_block_scores(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,

@@ -82,3 +82,37 @@ def test_window_0_says_all_in_the_one_and_none_in_the_other(Mq):
     live = np.isfinite(la)
     assert live.any() and (got[live] > lf[live] + 1e-3).all()
     assert np.allclose(got[live], np.logaddexp(la, lf)[live], rtol=0, atol=1e-4)
+
+
+def test_scores_of_given_splits_are_refused_without_a_workspace():
+    """A stream that is being captured cannot grow its workspace: the call takes one
+    split where the number is left to it (see test_gpu_choose.py) and is refused
+    where several are asked for; the capture goes on."""
+    s = Step(1)
+    # 256 query rows of 128 heads in 4096 splits: a gigabyte of statistics
+    q = torch.zeros((1, 256, 128, 512), dtype=torch.bfloat16, device="cuda")
+    wide = torch.zeros((1, 1 << 18), dtype=torch.int32, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        many = mla.prepare_block_scores(q, q[..., :64].contiguous(), s.means, wide, T.i32([1]), SCALE, n_splits=4096)
+        many.result.fill_(7.0)
+        out = torch.zeros((B, 1, NB), device="cuda")
+        one = mla.prepare_block_scores(*s.q, s.means, s.tab, s.lens, SCALE, scores=out, n_splits=1)
+        # (a table of one tile holds one split, which needs no workspace)
+        two = mla.prepare_block_scores(*s.q, s.means, s.tab, s.lens, SCALE, n_splits=2)
+        stream.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            with pytest.raises(mla.MlaError, match="capture"):
+                many()
+            one()
+            two()
+        for _ in range(3):
+            out.zero_()
+            g.replay()
+            stream.synchronize()
+            want = s.scores(n_splits=1)
+            stream.synchronize()
+            assert torch.equal(out, want) and torch.equal(two.result, want)
+        assert (many.result == 7.0).all()
