@@ -386,8 +386,10 @@ typedef struct {
  * not detected: rows of the batch may then come out undefined.  One launch for
  * prefixes and own tokens, one that joins them; the workspace, its limits and graph
  * capture as in mla_sparse_partial_attn (nothing to fall back on where it cannot
- * grow).  G at most 4096, B Mq H less than 2^26, tables less than 2^25 blocks wide
- * (MLA_ERR_UNSUPPORTED). */
+ * grow).  G at most 4096, B Mq H less than 2^26, tables less than 2^25 blocks wide, and
+ * at most 2^22 work items: tiles of 64 or 128 rows of the batch (one more for each group
+ * but the first) times splits of at most 256 blocks of a prefix, and those of each
+ * request's rows times splits of its own tokens (MLA_ERR_UNSUPPORTED). */
 mla_status_t mla_prefix_attn(const mla_tensor_t* q_lat, const mla_tensor_t* q_pe,
                              const mla_tensor_t* ckv_pool, const mla_tensor_t* kpe_pool,
                              const mla_tensor_t* prefix_table, const mla_tensor_t* prefix_lens,
