@@ -3,7 +3,6 @@ with g++ (which stops at a signed sum that wraps) against Python's integers, up 
 the longest sequences and prefixes that tables hold."""
 import os
 import random
-import re
 import subprocess
 
 import pytest
@@ -58,10 +57,3 @@ def test_rows_of_windows(exe):
         held = min(n, rng.choice([0, 64, rng.randint(0, MOST), MOST, n]))
         calls.append((n - qn, rng.choice([0, qn - 1, rng.randint(0, qn - 1)]), held))
     assert answers(exe, calls) == [min(p + i, n - 1) for p, i, n in calls]
-
-
-def test_the_kernels_take_it():
-    with open(os.path.join(B.CSRC, "mla_partial.hip")) as f:
-        text = f.read()
-    assert re.search(r"int hi_of\(int i\) const \{ return i < qn \? last_token\(pos0, i, n_tok\) : -1; \}", text)
-    assert not re.search(r"pos0 \+ i(?! - window)\b", re.sub(r"//.*", "", text).replace("(int64_t)pos0 + i", ""))
